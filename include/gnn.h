@@ -341,6 +341,149 @@ int gnn_debug_graph_pool(gnn_ctx* ctx, int64_t chunks);
 int gnn_csr_build_noalloc(const int32_t* edge_index, int64_t n_nodes, int64_t n_edges, int32_t* rowptr,
                           int32_t* perm, int32_t* src_sorted, gnn_stream_t stream);
 
+/*
+ * Hits as a sequence.  An event's hits in order (of azimuth, or along a track) can be read as a
+ * sequence: queries and keys of every hit are normalised for each head and rotated by their
+ * positions, and a hit attends to a window of the order and to a few first tokens that stay
+ * visible.  The calls below are those three steps, for a batch of whole events at once and for new
+ * hits over a cache of earlier ones.  (Library operators: the paper has no counterpart.)  They need
+ * no gnn_ctx.
+ *
+ * gnn_heads -- a view of a device array [rows, n_heads, head_dim] of one of the types below: element
+ * (r, h, d) at data + r * row_stride + h * head_stride + d, strides in elements, so that slices of a
+ * packed projection and either order of rows and heads are views.  Strides are not negative.
+ */
+enum gnn_dtype {
+  GNN_DTYPE_FP32 = 0,
+  GNN_DTYPE_BF16 = 1,
+  GNN_DTYPE_FP16 = 2,
+};
+
+typedef struct gnn_heads {
+  void* data;
+  int64_t row_stride, head_stride;
+  int32_t n_heads;
+  int32_t reserved;            /* 0 */
+} gnn_heads;
+
+/*
+ * gnn_rotary_init -- the table of a rotation, computed on the host (no device work): frequencies
+ * f_i = base^(-2 i / rot_dim), i < rot_dim / 2, in radians a position, scaled for positions beyond
+ * those a model was made for:
+ *   GNN_ROTARY_PLAIN    f_i
+ *   GNN_ROTARY_LINEAR   f_i / factor
+ *   GNN_ROTARY_BY_TURNS f_i (g + (1 - g) / factor), g = clamp((n_i - slow) / (fast - slow), 0, 1), with
+ *                       n_i = length f_i / 2 pi the turns pair i makes over `length` positions: fast
+ *                       pairs stay, slow ones are stretched
+ * Pair i is the elements i and i + rot_dim / 2 of a head (GNN_ROTARY_HALF) or 2 i and 2 i + 1
+ * (GNN_ROTARY_INTERLEAVED); elements from rot_dim on pass unrotated.  A pair (u, w) at position x
+ * becomes amplitude * (u cos - w sin, w cos + u sin) of the angle x f_i.  The table is the caller's;
+ * every field of it is read-only after this call.  Errors: INVALID_ARG (null pointer, rot_dim odd or
+ * outside 2..256, unknown layout or scaling, base or factor not positive and finite, amplitude not finite,
+ * by turns: length <= 0, slow < 0 or fast <= slow).
+ */
+enum gnn_rotary_layout { GNN_ROTARY_HALF = 0, GNN_ROTARY_INTERLEAVED = 1 };
+enum gnn_rotary_scaling { GNN_ROTARY_PLAIN = 0, GNN_ROTARY_LINEAR = 1, GNN_ROTARY_BY_TURNS = 2 };
+
+typedef struct gnn_rotary_config {
+  int32_t rot_dim, layout, scaling;
+  int32_t reserved;            /* 0 */
+  double base, factor, length, slow, fast, amplitude;
+} gnn_rotary_config;
+
+typedef struct gnn_rotary {
+  int32_t rot_dim, layout;
+  float amplitude;
+  int32_t magic;               /* set by gnn_rotary_init */
+  uint64_t turn_fixed[128];          /* f_i / 2 pi, modulo 1, in units of 2^-64 */
+  float turn_hi[128], turn_lo[128];  /* f_i / 2 pi as a sum of two floats */
+} gnn_rotary;
+
+int gnn_rotary_init(const gnn_rotary_config* cfg, gnn_rotary* out);
+
+/*
+ * gnn_rope -- rotate every head of x by its row's position.
+ *   x, y       views of n_rows rows with the same n_heads; y may be x itself (same strides), otherwise
+ *              they do not overlap
+ *   positions  device, int32 [n_rows] or, with positions_float != 0, float32 [n_rows]; NULL: row number
+ * head_dim 1..256, at least rot_dim, even.  Angles keep fp32 accuracy at any int32 position and at
+ * float32 ones up to 2^24; the arithmetic is fp32, rounded once.  Enqueued on `stream`.  n_rows == 0 is a no-op.
+ * Errors: INVALID_ARG (null pointer, table not made by gnn_rotary_init, unknown type, head_dim, n_heads < 1 or
+ * unequal, negative stride, data not aligned to its elements, sizes above GNN_MAX_COUNT), CUDA.
+ *
+ * gnn_qk_norm_rope -- q and k of every row: x / sqrt(mean(x^2) + eps) over each head, times the gain of each
+ * element, then the rotation, rounded once; v is copied.  One launch.
+ *   q, k, v              input views of n_rows rows; v may be NULL (then v_out is NULL too); k and v have
+ *                        the same n_heads
+ *   q_gain, k_gain       device float32 [head_dim], or NULL: 1
+ *   q_out, k_out, v_out  output views; each may be its input (rows == NULL, same strides), otherwise
+ *                        outputs overlap nothing
+ *   rows                 device int64 [n_rows], or NULL: row r of k and v goes to row rows[r] of k_out and
+ *                        v_out (the rows of a cache), of which there are out_rows; a row outside [0, out_rows) is
+ *                        not written; no two may be equal.  NULL: row r (out_rows is not read)
+ * eps > 0.  positions, types, limits and errors as for gnn_rope.
+ */
+int gnn_rope(const gnn_rotary* rot, int dtype, int head_dim, const gnn_heads* x, const gnn_heads* y,
+             const void* positions, int positions_float, int64_t n_rows, gnn_stream_t stream);
+int gnn_qk_norm_rope(const gnn_rotary* rot, int dtype, int head_dim, float eps, const float* q_gain,
+                     const float* k_gain, const gnn_heads* q, const gnn_heads* k, const gnn_heads* v,
+                     const gnn_heads* q_out, const gnn_heads* k_out, const gnn_heads* v_out, const void* positions,
+                     int positions_float, const int64_t* rows, int64_t out_rows, int64_t n_rows,
+                     gnn_stream_t stream);
+
+/*
+ * gnn_attention_run -- attention with a sliding window and first tokens that stay visible, for n_seqs
+ * sequences at once.  Sequence b has the query rows q_start[b] .. q_start[b + 1] - 1 and the kv_len[b] key
+ * (and value) rows from kv_start[b] on.  Its queries are the last ones of the sequence: query i of nq stands at
+ * position p = kv_len[b] - nq + i and sees key j when
+ *   j <= p + right  and  (j >= p - left  or  j < sinks);      left, right < 0: no bound.
+ * out = sum over the visible j of softmax_j(scale * q . k_j) v_j, head by head; query head h reads key head
+ * h / (q.n_heads / k.n_heads).  A query that sees no key, or whose visible scores are all -inf, gets zeros.
+ * Keys that a query does not see take no part in its result, whatever they hold (NaN and infinities too),
+ * nor do rows outside the sequence.
+ *   dtype           GNN_DTYPE_BF16 or GNN_DTYPE_FP16, of q, k, v and out; scores, sums and outputs are held in
+ *                   fp32, the weights that multiply v are rounded to dtype (their sum is not)
+ *   head_dim        a multiple of 8, 8..128
+ *   q, k, v, out    views of n_q_rows (q, out) and n_kv_rows (k, v) rows; data 16-byte aligned, strides
+ *                   multiples of 8 elements below 2^39; q.n_heads a multiple of k.n_heads == v.n_heads.
+ *                   out overlaps no input
+ *   q_start         device int32 [n_seqs + 1], not decreasing; rows before the first and from the last on are
+ *                   not written
+ *   kv_start, kv_len  device int32 [n_seqs]; both NULL: a sequence's keys are the rows of its queries
+ *   max_q, max_kv   the most queries and keys of a sequence; 0: not known (n_q_rows, n_kv_rows).  A sequence with
+ *                   more queries than max_q is INDEX_RANGE and its rows are undefined; max_kv only shapes the launch
+ * Device arrays of offsets that point outside the views are cut to them and reported as INDEX_RANGE by
+ * gnn_attention_status.  Enqueued on `stream`; only enqueues kernels (it can be captured).  The same inputs
+ * give bitwise-identical outputs.
+ * Errors: INVALID_ARG (null pointer, any limit above, scale not finite, sinks < 0, sizes above GNN_MAX_COUNT), CUDA.
+ *
+ * gnn_attention_create -- a handle on the current device: the workspace of calls with few queries and the
+ * device error word.  Synchronous.  One handle per stream: it is not safe for concurrent use.  Errors:
+ * INVALID_ARG, OOM, CUDA.
+ * gnn_attention_status -- synchronise `stream`, then return and clear the handle's error word: GNN_OK,
+ * GNN_ERR_INDEX_RANGE, GNN_ERR_DEVICE_TIMEOUT or GNN_ERR_CUDA.
+ * gnn_attention_destroy -- wait for the device and free the handle.  NULL is a no-op.
+ */
+typedef struct gnn_attention gnn_attention;
+
+typedef struct gnn_attention_call {
+  int32_t dtype, head_dim;
+  gnn_heads q, k, v, out;
+  const int32_t* q_start;
+  const int32_t* kv_start;
+  const int32_t* kv_len;
+  int64_t n_q_rows, n_kv_rows;
+  int32_t n_seqs, max_q, max_kv;
+  int32_t left, right, sinks;
+  float scale;
+  int32_t reserved;            /* 0 */
+} gnn_attention_call;
+
+int gnn_attention_create(gnn_attention** out);
+int gnn_attention_run(gnn_attention* att, const gnn_attention_call* call, gnn_stream_t stream);
+int gnn_attention_status(gnn_attention* att, gnn_stream_t stream);
+void gnn_attention_destroy(gnn_attention* att);
+
 #ifdef __cplusplus
 }
 #endif

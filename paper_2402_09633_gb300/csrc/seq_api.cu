@@ -1,0 +1,282 @@
+// Entry points for hits read as a sequence: rotary positions, norms of queries and keys with the rotation, and
+// attention with a sliding window (include/gnn.h).
+#include <cuda_runtime.h>
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+
+#include "../../include/gnn.h"
+#include "attend.cuh"
+#include "host.cuh"
+#include "rotary.cuh"
+
+using namespace gnn;
+
+struct gnn_attention {
+  int device = 0;
+  int n_sm = 0;
+  uint32_t* d_err = nullptr;
+};
+
+namespace {
+
+constexpr int32_t kRotaryMagic = 0x54524E47;       // "GNRT"
+constexpr double kTwoPi = 6.283185307179586476925286766559;
+
+int elem_bytes(int dtype) { return dtype == GNN_DTYPE_FP32 ? 4 : 2; }
+
+// A view whose elements are aligned, with strides that may be used; the furthest element stays within 2^62 bytes.
+bool view_ok(const gnn_heads* h, int dtype) {
+  if (!h || !h->data || h->n_heads < 1 || h->n_heads > (1 << 20) || h->reserved != 0) return false;
+  if ((uintptr_t)h->data % elem_bytes(dtype) != 0) return false;
+  return h->row_stride >= 0 && h->head_stride >= 0 && h->row_stride < (int64_t)1 << 39 &&
+         h->head_stride < (int64_t)1 << 39;
+}
+
+HeadsView view(const gnn_heads& h, int dtype) {
+  const int64_t e = elem_bytes(dtype);
+  return {static_cast<char*>(h.data), h.row_stride * e, h.head_stride * e};
+}
+
+// The most pairs a unit may have (8, 4 or 1) for head_dim, rot_dim and how the views lie.  A thread's accesses are
+// of `wide` pairs' elements: 16 bytes at most, as wide as every address allows.
+bool lies_on(const HeadsView& v, int64_t bytes) {
+  return (uintptr_t)v.data % bytes == 0 && v.row_bytes % bytes == 0 && v.head_bytes % bytes == 0;
+}
+
+template <typename T, int V>
+cudaError_t launch_rotary(const RotaryParams& p, bool inter, bool norm, unsigned grid, cudaStream_t st) {
+  if (norm)
+    return inter ? launch_pdl(rotary_kernel<T, V, true, true>, grid, kRotThreads, 0, st, p)
+                 : launch_pdl(rotary_kernel<T, V, false, true>, grid, kRotThreads, 0, st, p);
+  return inter ? launch_pdl(rotary_kernel<T, V, true, false>, grid, kRotThreads, 0, st, p)
+               : launch_pdl(rotary_kernel<T, V, false, false>, grid, kRotThreads, 0, st, p);
+}
+
+int device_sms() {
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+  if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+  return n;
+}
+
+// Fills the shared fields and launches; p.in, p.out, p.heads, p.gain, p.rows and p.eps are set.
+int run_rotary(const gnn_rotary* rot, int dtype, int head_dim, RotaryParams& p, bool norm, const void* positions,
+               int positions_float, int64_t n_rows, cudaStream_t st) {
+  p.dim = head_dim;
+  p.rot = rot->rot_dim;
+  p.tokens = n_rows;
+  p.pos = positions;
+  p.pos_float = positions && positions_float;
+  p.amplitude = rot->amplitude;
+  std::memcpy(p.fixed, rot->turn_fixed, sizeof p.fixed);
+  std::memcpy(p.hi, rot->turn_hi, sizeof p.hi);
+  std::memcpy(p.lo, rot->turn_lo, sizeof p.lo);
+  const bool inter = rot->layout == GNN_ROTARY_INTERLEAVED;
+  const int e = elem_bytes(dtype);
+  int V = dtype == GNN_DTYPE_FP32 ? 4 : 8;
+  for (;; V = V == 8 ? 4 : 1) {
+    bool ok = V == 1 || (head_dim % (2 * V) == 0 && p.rot % (2 * V) == 0);
+    for (int i = 0; i < 3 && V > 1; ++i)
+      if (p.heads[i]) ok = ok && lies_on(p.in[i], V * e) && lies_on(p.out[i], V * e);
+    if (ok) break;
+  }
+  p.units = head_dim / (2 * V);
+  p.group = 1;
+  while (p.group < p.units && p.group < 32) p.group *= 2;
+  const int sms = device_sms();
+  if (!sms) return cuda_fail(cudaGetLastError());
+  // As many heads to a group as leave the SMs their threads: a token's cosines are then computed once.
+  const int heads = p.heads[0] + p.heads[1] + p.heads[2];
+  const int64_t lanes = n_rows * heads * p.group, room = (int64_t)sms * 1024;
+  p.chunk = (int)std::min<int64_t>(heads, std::max<int64_t>(1, lanes / room));
+  p.chunks = (heads + p.chunk - 1) / p.chunk;
+  const int64_t blocks = (n_rows * p.chunks * p.group + kRotThreads - 1) / kRotThreads;
+  const unsigned grid = (unsigned)std::min<int64_t>(blocks, (int64_t)sms * 8);
+  cudaError_t err;
+  if (dtype == GNN_DTYPE_FP32)
+    err = V == 4 ? launch_rotary<float, 4>(p, inter, norm, grid, st) : launch_rotary<float, 1>(p, inter, norm, grid, st);
+  else if (dtype == GNN_DTYPE_BF16)
+    err = V == 8   ? launch_rotary<__nv_bfloat16, 8>(p, inter, norm, grid, st)
+          : V == 4 ? launch_rotary<__nv_bfloat16, 4>(p, inter, norm, grid, st)
+                   : launch_rotary<__nv_bfloat16, 1>(p, inter, norm, grid, st);
+  else
+    err = V == 8   ? launch_rotary<__half, 8>(p, inter, norm, grid, st)
+          : V == 4 ? launch_rotary<__half, 4>(p, inter, norm, grid, st)
+                   : launch_rotary<__half, 1>(p, inter, norm, grid, st);
+  return err == cudaSuccess ? GNN_OK : cuda_fail(err);
+}
+
+bool rotary_args_ok(const gnn_rotary* rot, int dtype, int head_dim, int64_t n_rows, const void* positions) {
+  if (!rot || rot->magic != kRotaryMagic || dtype < GNN_DTYPE_FP32 || dtype > GNN_DTYPE_FP16) return false;
+  if (head_dim < rot->rot_dim || head_dim > 2 * kRotMaxPairs || head_dim % 2 != 0) return false;
+  return count_ok(n_rows) && (uintptr_t)positions % 4 == 0;
+}
+
+}  // namespace
+
+extern "C" {
+
+int gnn_rotary_init(const gnn_rotary_config* cfg, gnn_rotary* out) {
+  if (!cfg || !out || cfg->reserved != 0) return GNN_ERR_INVALID_ARG;
+  const int R = cfg->rot_dim;
+  if (R < 2 || R > 2 * kRotMaxPairs || R % 2 != 0) return GNN_ERR_INVALID_ARG;
+  if (cfg->layout != GNN_ROTARY_HALF && cfg->layout != GNN_ROTARY_INTERLEAVED) return GNN_ERR_INVALID_ARG;
+  if (cfg->scaling < GNN_ROTARY_PLAIN || cfg->scaling > GNN_ROTARY_BY_TURNS) return GNN_ERR_INVALID_ARG;
+  auto positive = [](double x) { return std::isfinite(x) && x > 0; };
+  if (!positive(cfg->base) || !std::isfinite(cfg->amplitude)) return GNN_ERR_INVALID_ARG;
+  if (cfg->scaling != GNN_ROTARY_PLAIN && !positive(cfg->factor)) return GNN_ERR_INVALID_ARG;
+  if (cfg->scaling == GNN_ROTARY_BY_TURNS &&
+      (!positive(cfg->length) || !(cfg->slow >= 0) || !std::isfinite(cfg->fast) || !(cfg->fast > cfg->slow)))
+    return GNN_ERR_INVALID_ARG;
+  gnn_rotary r;
+  std::memset(&r, 0, sizeof r);
+  r.rot_dim = R;
+  r.layout = cfg->layout;
+  r.amplitude = (float)cfg->amplitude;
+  for (int i = 0; i < R / 2; ++i) {
+    double f = std::pow(cfg->base, -2.0 * i / R);
+    if (cfg->scaling == GNN_ROTARY_LINEAR) f /= cfg->factor;
+    if (cfg->scaling == GNN_ROTARY_BY_TURNS) {
+      const double g = std::min(1.0, std::max(0.0, (cfg->length * f / kTwoPi - cfg->slow) / (cfg->fast - cfg->slow)));
+      f *= g + (1.0 - g) / cfg->factor;
+    }
+    const double turns = f / kTwoPi;
+    r.turn_hi[i] = (float)turns;
+    r.turn_lo[i] = (float)(turns - (double)r.turn_hi[i]);
+    if (!std::isfinite(r.turn_hi[i])) return GNN_ERR_INVALID_ARG;
+    const double part = std::ldexp(turns - std::floor(turns), 64);     // [0, 2^64]: a whole turn is none
+    r.turn_fixed[i] = part >= 18446744073709551616.0 ? 0 : (uint64_t)part;
+  }
+  r.magic = kRotaryMagic;
+  *out = r;
+  return GNN_OK;
+}
+
+int gnn_rope(const gnn_rotary* rot, int dtype, int head_dim, const gnn_heads* x, const gnn_heads* y,
+             const void* positions, int positions_float, int64_t n_rows, gnn_stream_t stream) {
+  if (!rotary_args_ok(rot, dtype, head_dim, n_rows, positions)) return GNN_ERR_INVALID_ARG;
+  if (n_rows == 0) return GNN_OK;
+  if (!view_ok(x, dtype) || !view_ok(y, dtype) || x->n_heads != y->n_heads) return GNN_ERR_INVALID_ARG;
+  RotaryParams p = {};
+  p.in[0] = view(*x, dtype);
+  p.out[0] = view(*y, dtype);
+  p.heads[0] = x->n_heads;
+  return run_rotary(rot, dtype, head_dim, p, false, positions, positions_float, n_rows, (cudaStream_t)stream);
+}
+
+int gnn_qk_norm_rope(const gnn_rotary* rot, int dtype, int head_dim, float eps, const float* q_gain,
+                     const float* k_gain, const gnn_heads* q, const gnn_heads* k, const gnn_heads* v,
+                     const gnn_heads* q_out, const gnn_heads* k_out, const gnn_heads* v_out, const void* positions,
+                     int positions_float, const int64_t* rows, int64_t out_rows, int64_t n_rows,
+                     gnn_stream_t stream) {
+  if (!rotary_args_ok(rot, dtype, head_dim, n_rows, positions)) return GNN_ERR_INVALID_ARG;
+  if (!std::isfinite(eps) || !(eps > 0.f) || (uintptr_t)q_gain % 4 || (uintptr_t)k_gain % 4 || (uintptr_t)rows % 8)
+    return GNN_ERR_INVALID_ARG;
+  if ((rows && !count_ok(out_rows)) || (v != nullptr) != (v_out != nullptr)) return GNN_ERR_INVALID_ARG;
+  if (n_rows == 0) return GNN_OK;
+  const gnn_heads* in[3] = {q, k, v};
+  const gnn_heads* out[3] = {q_out, k_out, v_out};
+  RotaryParams p = {};
+  for (int i = 0; i < (v ? 3 : 2); ++i) {
+    if (!view_ok(in[i], dtype) || !view_ok(out[i], dtype) || in[i]->n_heads != out[i]->n_heads)
+      return GNN_ERR_INVALID_ARG;
+    p.in[i] = view(*in[i], dtype);
+    p.out[i] = view(*out[i], dtype);
+    p.heads[i] = in[i]->n_heads;
+  }
+  if (v && v->n_heads != k->n_heads) return GNN_ERR_INVALID_ARG;
+  p.gain[0] = q_gain;
+  p.gain[1] = k_gain;
+  p.rows = rows;
+  p.out_rows = out_rows;
+  p.eps = eps;
+  return run_rotary(rot, dtype, head_dim, p, true, positions, positions_float, n_rows, (cudaStream_t)stream);
+}
+
+int gnn_attention_create(gnn_attention** out) {
+  if (!out) return GNN_ERR_INVALID_ARG;
+  *out = nullptr;
+  gnn_attention* a = new (std::nothrow) gnn_attention;
+  if (!a) return GNN_ERR_OOM;
+  cudaError_t err = cudaGetDevice(&a->device);
+  if (err == cudaSuccess) err = cudaDeviceGetAttribute(&a->n_sm, cudaDevAttrMultiProcessorCount, a->device);
+  if (err == cudaSuccess) err = dev_alloc((void**)&a->d_err, 4);
+  if (err == cudaSuccess) err = cudaMemset(a->d_err, 0, 4);
+  if (err != cudaSuccess) {
+    if (a->d_err) cudaFree(a->d_err);
+    delete a;
+    return cuda_fail(err);
+  }
+  *out = a;
+  return GNN_OK;
+}
+
+int gnn_attention_run(gnn_attention* att, const gnn_attention_call* c, gnn_stream_t stream) {
+  if (!att || !c || c->reserved != 0) return GNN_ERR_INVALID_ARG;
+  if ((c->dtype != GNN_DTYPE_BF16 && c->dtype != GNN_DTYPE_FP16) || c->head_dim < 8 || c->head_dim > 128 ||
+      c->head_dim % 8 != 0 || !std::isfinite(c->scale) || c->sinks < 0)
+    return GNN_ERR_INVALID_ARG;
+  if (!count_ok(c->n_q_rows) || !count_ok(c->n_kv_rows) || !count_ok(c->n_seqs) || c->max_q < 0 || c->max_kv < 0 ||
+      (c->kv_start != nullptr) != (c->kv_len != nullptr))
+    return GNN_ERR_INVALID_ARG;
+  if (c->n_q_rows == 0 || c->n_seqs == 0) return GNN_OK;
+  if (!c->q_start || (uintptr_t)c->q_start % 4 || (uintptr_t)c->kv_start % 4 || (uintptr_t)c->kv_len % 4)
+    return GNN_ERR_INVALID_ARG;
+  gnn_heads views[4] = {c->q, c->k, c->v, c->out};
+  if (c->n_kv_rows == 0) views[1].data = views[2].data = c->out.data;   // nothing is read of them
+  for (const gnn_heads& v : views)
+    if (!view_ok(&v, c->dtype) || (uintptr_t)v.data % 16 || v.row_stride % 8 || v.head_stride % 8)
+      return GNN_ERR_INVALID_ARG;
+  if (c->k.n_heads != c->v.n_heads || c->q.n_heads != c->out.n_heads || c->q.n_heads % c->k.n_heads)
+    return GNN_ERR_INVALID_ARG;
+  AttendParams p = {};
+  p.q = view(c->q, c->dtype);
+  p.k = view(views[1], c->dtype);
+  p.v = view(views[2], c->dtype);
+  p.out = view(c->out, c->dtype);
+  p.q_start = c->q_start;
+  p.kv_start = c->kv_start;
+  p.kv_len = c->kv_len;
+  p.n_q_rows = (int)c->n_q_rows;
+  p.n_kv_rows = (int)c->n_kv_rows;
+  p.n_seqs = c->n_seqs;
+  p.heads = c->q.n_heads;
+  p.kv_heads = c->k.n_heads;
+  p.dim = c->head_dim;
+  p.left = c->left;
+  p.right = c->right;
+  p.sinks = c->sinks;
+  p.scale_log2 = (float)((double)c->scale * 1.4426950408889634);
+  p.err = att->d_err;
+  const int64_t warps = c->n_q_rows * c->q.n_heads;
+  const unsigned grid = (unsigned)std::min<int64_t>((warps + kRowWarps - 1) / kRowWarps, (int64_t)att->n_sm * 8);
+  const cudaError_t err =
+      c->dtype == GNN_DTYPE_BF16
+          ? launch_pdl(attend_rows_kernel<__nv_bfloat16>, grid, 32 * kRowWarps, 0, (cudaStream_t)stream, p)
+          : launch_pdl(attend_rows_kernel<__half>, grid, 32 * kRowWarps, 0, (cudaStream_t)stream, p);
+  return err == cudaSuccess ? GNN_OK : cuda_fail(err);
+}
+
+int gnn_attention_status(gnn_attention* att, gnn_stream_t stream) {
+  if (!att) return GNN_ERR_INVALID_ARG;
+  cudaError_t err = cudaStreamSynchronize((cudaStream_t)stream);
+  if (err != cudaSuccess) return cuda_fail(err);
+  uint32_t word = 0;
+  err = cudaMemcpy(&word, att->d_err, 4, cudaMemcpyDeviceToHost);
+  if (err == cudaSuccess) err = cudaMemset(att->d_err, 0, 4);
+  if (err != cudaSuccess) return cuda_fail(err);
+  if (word & DEV_ERR_TIMEOUT) return GNN_ERR_DEVICE_TIMEOUT;
+  if (word & DEV_ERR_INDEX_RANGE) return GNN_ERR_INDEX_RANGE;
+  return GNN_OK;
+}
+
+void gnn_attention_destroy(gnn_attention* att) {
+  if (!att) return;
+  cudaDeviceSynchronize();
+  if (att->d_err) cudaFree(att->d_err);
+  delete att;
+}
+
+}  // extern "C"
