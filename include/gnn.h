@@ -445,7 +445,7 @@ int gnn_qk_norm_rope(const gnn_rotary* rot, int dtype, int head_dim, float eps, 
  *                   fp32, the weights that multiply v are rounded to dtype (their sum is not)
  *   head_dim        a multiple of 8, 8..128
  *   q, k, v, out    views of n_q_rows (q, out) and n_kv_rows (k, v) rows; data 16-byte aligned, strides
- *                   multiples of 8 elements below 2^39; q.n_heads a multiple of k.n_heads == v.n_heads.
+ *                   positive multiples of 8 elements below 2^39; q.n_heads a multiple of k.n_heads == v.n_heads.
  *                   out overlaps no input
  *   q_start         device int32 [n_seqs + 1], not decreasing; rows before the first and from the last on are
  *                   not written
@@ -455,7 +455,8 @@ int gnn_qk_norm_rope(const gnn_rotary* rot, int dtype, int head_dim, float eps, 
  * Device arrays of offsets that point outside the views are cut to them and reported as INDEX_RANGE by
  * gnn_attention_status.  Enqueued on `stream`; only enqueues kernels (it can be captured).  The same inputs
  * give bitwise-identical outputs.
- * Errors: INVALID_ARG (null pointer, any limit above, scale not finite, sinks < 0, sizes above GNN_MAX_COUNT), CUDA.
+ * Errors: INVALID_ARG (null pointer, any limit above, scale not finite, sinks < 0, sizes above GNN_MAX_COUNT,
+ * n_seqs above 2^30), CUDA.
  *
  * gnn_attention_create -- a handle on the current device: the workspace of calls with few queries and the
  * device error word.  Synchronous.  One handle per stream: it is not safe for concurrent use.  Errors:

@@ -99,32 +99,4 @@ __device__ __forceinline__ void attend_row(const AttendParams& p, const Sequence
     if (lane + 32 * d < p.dim) out[lane + 32 * d] = from_f<T>(l == 0.f ? 0.f : o[d] / l);
 }
 
-constexpr int kRowWarps = 8;
-
-// A warp to each (row, head).
-template <typename T>
-__global__ void __launch_bounds__(32 * kRowWarps) attend_rows_kernel(const __grid_constant__ AttendParams p) {
-  __shared__ float qs[kRowWarps][128];
-  pdl_wait();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t n = (int64_t)p.n_q_rows * p.heads, step = (int64_t)gridDim.x * kRowWarps;
-  for (int64_t at = (int64_t)blockIdx.x * kRowWarps + warp; at < n; at += step) {
-    const int row = (int)(at / p.heads), head = (int)(at % p.heads);
-    int a = 0, z = p.n_seqs;                       // the last sequence that starts at or before the row
-    while (z - a > 1) {
-      const int mid = (a + z) / 2;
-      if (p.q_start[mid] <= row) a = mid; else z = mid;
-    }
-    bool bad;
-    const Sequence sq = sequence(p, a, &bad);
-    if (bad && lane == 0) atomicOr(p.err, DEV_ERR_INDEX_RANGE);
-    if (row < sq.q0 || row >= sq.q0 + sq.nq) continue;
-    const T* q = reinterpret_cast<const T*>(p.q.data + (int64_t)row * p.q.row_bytes + head * p.q.head_bytes);
-    __syncwarp();
-    for (int d = lane; d < p.dim; d += 32) qs[warp][d] = to_f(q[d]);
-    __syncwarp();
-    attend_row<T>(p, sq, row - sq.q0, head, qs[warp]);
-  }
-}
-
 }  // namespace gnn

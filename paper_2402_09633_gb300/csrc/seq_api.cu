@@ -1,5 +1,6 @@
 // Entry points for hits read as a sequence: rotary positions, norms of queries and keys with the rotation, and
 // attention with a sliding window (include/gnn.h).
+#include <cudaTypedefs.h>
 #include <cuda_runtime.h>
 #include <algorithm>
 #include <cmath>
@@ -8,6 +9,7 @@
 
 #include "../../include/gnn.h"
 #include "attend.cuh"
+#include "attend_tile.cuh"
 #include "host.cuh"
 #include "rotary.cuh"
 
@@ -17,6 +19,7 @@ struct gnn_attention {
   int device = 0;
   int n_sm = 0;
   uint32_t* d_err = nullptr;
+  PFN_cuTensorMapEncodeTiled_v12000 encode = nullptr;
 };
 
 namespace {
@@ -114,6 +117,50 @@ bool rotary_args_ok(const gnn_rotary* rot, int dtype, int head_dim, int64_t n_ro
   return count_ok(n_rows) && (uintptr_t)positions % 4 == 0;
 }
 
+// Boxes of 128 rows x 64 elements of one head, in the 128-byte swizzle; what lies outside reads as zeros.
+bool encode_map(const gnn_attention* a, CUtensorMap* map, const gnn_heads& h, int64_t rows, int dtype, int dim) {
+  const cuuint64_t size[3] = {(cuuint64_t)dim, (cuuint64_t)h.n_heads, (cuuint64_t)std::max<int64_t>(rows, 1)};
+  const cuuint64_t one = (cuuint64_t)(dim * 2 + 15) / 16 * 16;      // for a dimension of one, whose stride is not used
+  const cuuint64_t stride[2] = {h.n_heads > 1 ? (cuuint64_t)h.head_stride * 2 : one,
+                                rows > 1 ? (cuuint64_t)h.row_stride * 2 : one};
+  const cuuint32_t box[3] = {64, 1, 128}, step[3] = {1, 1, 1};
+  return a->encode(map, dtype == GNN_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
+                   h.data, size, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, int DP>
+cudaError_t launch_attend(unsigned grid, cudaStream_t st, const AttendParams& p, const AttendGrid& g,
+                          const CUtensorMap* maps) {
+  const cudaError_t err = cudaFuncSetAttribute(attend_tile_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               attend_smem_bytes<DP>());
+  if (err != cudaSuccess) return err;
+  return launch_pdl(attend_tile_kernel<T, DP>, grid, kAttendThreads, attend_smem_bytes<DP>(), st, p, g, maps[0], maps[1],
+                    maps[2]);
+}
+
+int run_tiles(gnn_attention* a, const gnn_attention_call* c, const gnn_heads* views, const AttendParams& p,
+              cudaStream_t st) {
+  CUtensorMap maps[3];
+  if (!encode_map(a, &maps[0], views[0], c->n_q_rows, c->dtype, c->head_dim) ||
+      !encode_map(a, &maps[1], views[1], c->n_kv_rows, c->dtype, c->head_dim) ||
+      !encode_map(a, &maps[2], views[2], c->n_kv_rows, c->dtype, c->head_dim))
+    return GNN_ERR_INVALID_ARG;
+  AttendGrid g = {};
+  g.pair_heads = p.heads / p.kv_heads % 2 == 0;
+  g.rows = g.pair_heads ? kTileQ : 2 * kTileQ;
+  g.heads = g.pair_heads ? p.heads / 2 : p.heads;
+  g.items = (c->n_q_rows / g.rows + c->n_seqs) * g.heads;
+  const unsigned grid = (unsigned)std::min<int64_t>(g.items, a->n_sm);
+  cudaError_t err;
+  if (c->dtype == GNN_DTYPE_BF16)
+    err = p.dim <= 64 ? launch_attend<__nv_bfloat16, 64>(grid, st, p, g, maps)
+                      : launch_attend<__nv_bfloat16, 128>(grid, st, p, g, maps);
+  else
+    err = p.dim <= 64 ? launch_attend<__half, 64>(grid, st, p, g, maps) : launch_attend<__half, 128>(grid, st, p, g, maps);
+  return err == cudaSuccess ? GNN_OK : cuda_fail(err);
+}
+
 }  // namespace
 
 extern "C" {
@@ -202,6 +249,10 @@ int gnn_attention_create(gnn_attention** out) {
   if (!a) return GNN_ERR_OOM;
   cudaError_t err = cudaGetDevice(&a->device);
   if (err == cudaSuccess) err = cudaDeviceGetAttribute(&a->n_sm, cudaDevAttrMultiProcessorCount, a->device);
+  cudaDriverEntryPointQueryResult found;
+  if (err == cudaSuccess)
+    err = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", (void**)&a->encode, 12000, cudaEnableDefault, &found);
+  if (err == cudaSuccess && (found != cudaDriverEntryPointSuccess || !a->encode)) err = cudaErrorNotSupported;
   if (err == cudaSuccess) err = dev_alloc((void**)&a->d_err, 4);
   if (err == cudaSuccess) err = cudaMemset(a->d_err, 0, 4);
   if (err != cudaSuccess) {
@@ -229,6 +280,9 @@ int gnn_attention_run(gnn_attention* att, const gnn_attention_call* c, gnn_strea
   for (const gnn_heads& v : views)
     if (!view_ok(&v, c->dtype) || (uintptr_t)v.data % 16 || v.row_stride % 8 || v.head_stride % 8)
       return GNN_ERR_INVALID_ARG;
+  if (c->n_seqs > 1 << 30) return GNN_ERR_INVALID_ARG;
+  for (const gnn_heads& v : views)                 // one row or head for several is not a view that can be read here
+    if ((v.n_heads > 1 && v.head_stride == 0) || v.row_stride == 0) return GNN_ERR_INVALID_ARG;
   if (c->k.n_heads != c->v.n_heads || c->q.n_heads != c->out.n_heads || c->q.n_heads % c->k.n_heads)
     return GNN_ERR_INVALID_ARG;
   AttendParams p = {};
@@ -248,15 +302,10 @@ int gnn_attention_run(gnn_attention* att, const gnn_attention_call* c, gnn_strea
   p.left = c->left;
   p.right = c->right;
   p.sinks = c->sinks;
-  p.scale_log2 = (float)((double)c->scale * 1.4426950408889634);
+  // a scale of zero as one too small to be seen, so that -inf, a score that is not seen, stays -inf
+  p.scale_log2 = c->scale == 0.f ? 1e-30f : (float)((double)c->scale * 1.4426950408889634);
   p.err = att->d_err;
-  const int64_t warps = c->n_q_rows * c->q.n_heads;
-  const unsigned grid = (unsigned)std::min<int64_t>((warps + kRowWarps - 1) / kRowWarps, (int64_t)att->n_sm * 8);
-  const cudaError_t err =
-      c->dtype == GNN_DTYPE_BF16
-          ? launch_pdl(attend_rows_kernel<__nv_bfloat16>, grid, 32 * kRowWarps, 0, (cudaStream_t)stream, p)
-          : launch_pdl(attend_rows_kernel<__half>, grid, 32 * kRowWarps, 0, (cudaStream_t)stream, p);
-  return err == cudaSuccess ? GNN_OK : cuda_fail(err);
+  return run_tiles(att, c, views, p, (cudaStream_t)stream);
 }
 
 int gnn_attention_status(gnn_attention* att, gnn_stream_t stream) {
