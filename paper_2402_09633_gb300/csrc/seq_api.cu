@@ -9,6 +9,7 @@
 
 #include "../../include/gnn.h"
 #include "attend.cuh"
+#include "attend_few.cuh"
 #include "attend_tile.cuh"
 #include "host.cuh"
 #include "rotary.cuh"
@@ -20,9 +21,19 @@ struct gnn_attention {
   int n_sm = 0;
   uint32_t* d_err = nullptr;
   PFN_cuTensorMapEncodeTiled_v12000 encode = nullptr;
+  int slots = 0;                     // results of parts of the keys that the workspace holds
+  float* d_parts = nullptr;
+  int* d_tickets = nullptr;
 };
 
 namespace {
+
+void free_attention(gnn_attention* a) {
+  if (a->d_err) cudaFree(a->d_err);
+  if (a->d_parts) cudaFree(a->d_parts);
+  if (a->d_tickets) cudaFree(a->d_tickets);
+  delete a;
+}
 
 constexpr int32_t kRotaryMagic = 0x54524E47;       // "GNRT"
 constexpr double kTwoPi = 6.283185307179586476925286766559;
@@ -161,6 +172,38 @@ int run_tiles(gnn_attention* a, const gnn_attention_call* c, const gnn_heads* vi
   return err == cudaSuccess ? GNN_OK : cuda_fail(err);
 }
 
+// Few queries to a sequence: the keys split over as many blocks as keep the SMs busy for several rounds, so that
+// sequences of different lengths even out.
+int run_few(gnn_attention* a, const gnn_attention_call* c, const AttendParams& p, int64_t max_q, cudaStream_t st) {
+  FewGrid f = {};
+  f.group = p.heads / p.kv_heads;
+  f.max_q = (int)max_q;
+  f.row_tiles = (int)((max_q * f.group + kFewRows - 1) / kFewRows);
+  int64_t keys = c->kv_len ? c->n_kv_rows : max_q;
+  if (c->max_kv > 0) keys = std::min<int64_t>(keys, c->max_kv);
+  if (p.left >= 0 && p.right >= 0) keys = std::min<int64_t>(keys, (int64_t)p.sinks + p.left + p.right + max_q);
+  const int64_t tiles = (int64_t)p.n_seqs * p.kv_heads * f.row_tiles, wanted = (int64_t)a->n_sm * 18;
+  f.chunk = (int)std::max<int64_t>(kFewStep, (keys * tiles / wanted + kFewStep - 1) / kFewStep * kFewStep);
+  f.splits = (int)std::max<int64_t>(1, std::min<int64_t>((keys + f.chunk - 1) / f.chunk, a->slots / tiles));
+  f.parts = a->d_parts;
+  f.tickets = a->d_tickets;
+  const unsigned grid = (unsigned)(tiles * f.splits);
+  cudaError_t err;
+  auto go = [&](auto kernel) { return launch_pdl(kernel, grid, 32 * kFewWarps, 0, st, p, f); };
+  const int nc = (p.dim + 31) / 32;
+  if (c->dtype == GNN_DTYPE_BF16)
+    err = nc == 1   ? go(attend_few_kernel<__nv_bfloat16, 1>)
+          : nc == 2 ? go(attend_few_kernel<__nv_bfloat16, 2>)
+          : nc == 3 ? go(attend_few_kernel<__nv_bfloat16, 3>)
+                    : go(attend_few_kernel<__nv_bfloat16, 4>);
+  else
+    err = nc == 1   ? go(attend_few_kernel<__half, 1>)
+          : nc == 2 ? go(attend_few_kernel<__half, 2>)
+          : nc == 3 ? go(attend_few_kernel<__half, 3>)
+                    : go(attend_few_kernel<__half, 4>);
+  return err == cudaSuccess ? GNN_OK : cuda_fail(err);
+}
+
 }  // namespace
 
 extern "C" {
@@ -255,9 +298,12 @@ int gnn_attention_create(gnn_attention** out) {
   if (err == cudaSuccess && (found != cudaDriverEntryPointSuccess || !a->encode)) err = cudaErrorNotSupported;
   if (err == cudaSuccess) err = dev_alloc((void**)&a->d_err, 4);
   if (err == cudaSuccess) err = cudaMemset(a->d_err, 0, 4);
+  a->slots = 32 * a->n_sm;
+  if (err == cudaSuccess) err = dev_alloc((void**)&a->d_parts, (size_t)a->slots * kFewRows * (128 + 2) * 4);
+  if (err == cudaSuccess) err = dev_alloc((void**)&a->d_tickets, (size_t)a->slots * 4);
+  if (err == cudaSuccess) err = cudaMemset(a->d_tickets, 0, (size_t)a->slots * 4);
   if (err != cudaSuccess) {
-    if (a->d_err) cudaFree(a->d_err);
-    delete a;
+    free_attention(a);
     return cuda_fail(err);
   }
   *out = a;
@@ -305,6 +351,10 @@ int gnn_attention_run(gnn_attention* att, const gnn_attention_call* c, gnn_strea
   // a scale of zero as one too small to be seen, so that -inf, a score that is not seen, stays -inf
   p.scale_log2 = c->scale == 0.f ? 1e-30f : (float)((double)c->scale * 1.4426950408889634);
   p.err = att->d_err;
+  const int64_t max_q = c->max_q > 0 ? std::min<int64_t>(c->max_q, c->n_q_rows) : c->n_q_rows;
+  const int group = p.heads / p.kv_heads;
+  if (max_q * group <= 2 * kFewRows && (int64_t)p.n_seqs * p.kv_heads <= 1 << 24)
+    return run_few(att, c, p, max_q, (cudaStream_t)stream);
   return run_tiles(att, c, views, p, (cudaStream_t)stream);
 }
 
@@ -324,8 +374,7 @@ int gnn_attention_status(gnn_attention* att, gnn_stream_t stream) {
 void gnn_attention_destroy(gnn_attention* att) {
   if (!att) return;
   cudaDeviceSynchronize();
-  if (att->d_err) cudaFree(att->d_err);
-  delete att;
+  free_attention(att);
 }
 
 }  // extern "C"
