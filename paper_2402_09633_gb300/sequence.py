@@ -7,11 +7,11 @@ from __future__ import annotations
 
 import ctypes
 import math
+import struct
 
 from . import binding
-from .binding import GNN_OK, GnnError, _stream_handle
+from .binding import GNN_OK, GnnError
 
-DTYPES = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2}
 LAYOUTS = {"half": 0, "interleaved": 1}
 _vp, _i64, _i32, _f32, _f64 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_float, ctypes.c_double
 
@@ -37,61 +37,78 @@ class GnnAttentionCall(ctypes.Structure):
                 ("right", _i32), ("sinks", _i32), ("scale", _f32), ("reserved", _i32)]
 
 
-_lib = None
+_HEADS = struct.Struct("PqqiI")                              # GnnHeads
+_CALL = struct.Struct("ii" + "PqqiI" * 4 + "PPPqqiiiiiifi")   # GnnAttentionCall
+assert _HEADS.size == ctypes.sizeof(GnnHeads) and _CALL.size == ctypes.sizeof(GnnAttentionCall)
+_AREA = ctypes.create_string_buffer(max(6 * _HEADS.size, _CALL.size))
+_AT = [ctypes.addressof(_AREA) + i * _HEADS.size for i in range(6)]
+_lib = _torch = _raw_stream = None
+DTYPES = {}
 
 
 def _library():
-    global _lib
+    """The library, loaded once more so that its calls keep the interpreter lock: they only enqueue work, and the one
+    area that their arguments are packed in is then not written by two threads."""
+    global _lib, _torch, _raw_stream
     if _lib is None:
-        lib = binding.load_library()
-        heads = ctypes.POINTER(GnnHeads)
-        rot = ctypes.POINTER(GnnRotary)
+        import torch
+        binding.load_library()
+        lib = ctypes.PyDLL(binding.LIB_PATH)
         i = ctypes.c_int
-        lib.gnn_rotary_init.argtypes = [ctypes.POINTER(GnnRotaryConfig), rot]
-        lib.gnn_rope.argtypes = [rot, i, i, heads, heads, _vp, i, _i64, _vp]
-        lib.gnn_qk_norm_rope.argtypes = [rot, i, i, _f32, _vp, _vp, heads, heads, heads, heads, heads, heads, _vp, i,
-                                         _vp, _i64, _i64, _vp]
+        lib.gnn_rotary_init.argtypes = [_vp, _vp]
+        lib.gnn_rope.argtypes = [_vp, i, i, _vp, _vp, _vp, i, _i64, _vp]
+        lib.gnn_qk_norm_rope.argtypes = [_vp, i, i, _f32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, i, _vp, _i64, _i64,
+                                         _vp]
         lib.gnn_attention_create.argtypes = [ctypes.POINTER(_vp)]
-        lib.gnn_attention_run.argtypes = [_vp, ctypes.POINTER(GnnAttentionCall), _vp]
-        lib.gnn_attention_status.argtypes = [_vp, _vp]
+        lib.gnn_attention_run.argtypes = [_vp, _vp, _vp]
         for f in (lib.gnn_rotary_init, lib.gnn_rope, lib.gnn_qk_norm_rope, lib.gnn_attention_create,
-                  lib.gnn_attention_run, lib.gnn_attention_status):
+                  lib.gnn_attention_run):
             f.restype = i
-        lib.gnn_attention_destroy.argtypes = [_vp]
-        lib.gnn_attention_destroy.restype = None
-        _lib = lib
+        waits = binding.load_library()                       # these wait for the device, without the lock
+        waits.gnn_attention_status.argtypes = [_vp, _vp]
+        waits.gnn_attention_status.restype = i
+        waits.gnn_attention_destroy.argtypes = [_vp]
+        waits.gnn_attention_destroy.restype = None
+        DTYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+        _raw_stream = torch._C._cuda_getCurrentRawStream
+        _lib, _torch = lib, torch
     return _lib
 
 
-def _heads(x, like=None):
-    """A view's struct; x: cuda tensor [rows, heads, dim], last stride 1."""
-    assert x.is_cuda and x.dim() == 3 and (x.stride(2) == 1 or x.shape[2] == 1), "a cuda tensor [rows, heads, dim], last stride 1"
-    if like is not None:
-        assert x.dtype == like.dtype and x.device == like.device and x.shape[2] == like.shape[2], "types, devices or head sizes differ"
-    return GnnHeads(x.data_ptr(), x.stride(0), x.stride(1), x.shape[1], 0)
+def _stream(stream, device):
+    return _raw_stream(device) if stream is None else stream.cuda_stream
 
 
-def _dtype(x):
-    d = DTYPES.get(str(x.dtype))
-    assert d is not None, f"type {x.dtype} is not taken"
-    return d
+def _heads(x, dtype, device, dim):
+    """A view's fields; x: cuda tensor [rows, heads, dim], last stride 1, of the given type, device and head size."""
+    shape, stride = x.shape, x.stride()
+    assert len(shape) == 3 and (stride[2] == 1 or shape[2] == 1), "a tensor [rows, heads, dim], last stride 1"
+    assert x.dtype == dtype and x.get_device() == device and shape[2] == dim, "types, devices or head sizes differ"
+    return x.data_ptr(), stride[0], stride[1], shape[1], 0
+
+
+def _kind(x):
+    """(type, its number, device, head size) of a cuda tensor."""
+    device, dtype = x.get_device(), x.dtype
+    assert device >= 0, "a cuda tensor"
+    assert dtype in DTYPES, f"type {dtype} is not taken"
+    return dtype, DTYPES[dtype], device, x.shape[2]
 
 
 def _vector(x, n, dtype, device):
     """A contiguous cuda vector's address, or None."""
     if x is None:
         return None
-    assert x.device == device and x.dtype == dtype and x.is_contiguous() and x.numel() == n, \
+    assert x.get_device() == device and x.dtype == dtype and x.numel() == n and x.is_contiguous(), \
         f"a contiguous {dtype} cuda tensor of {n} is wanted"
     return x.data_ptr()
 
 
 def _positions(pos, n, device):
-    import torch
     if pos is None:
         return None, 0
-    real = pos.dtype == torch.float32
-    return _vector(pos, n, torch.float32 if real else torch.int32, device), int(real)
+    real = pos.dtype == _torch.float32
+    return _vector(pos, n, _torch.float32 if real else _torch.int32, device), int(real)
 
 
 class Rotary:
@@ -109,20 +126,22 @@ class Rotary:
         rc = _library().gnn_rotary_init(ctypes.byref(cfg), ctypes.byref(self.table))
         if rc != GNN_OK:
             raise GnnError(rc, "gnn_rotary_init")
-        self.ref = ctypes.byref(self.table)
+        self.address = ctypes.addressof(self.table)
 
 
 def rope(rot: Rotary, x, positions=None, out=None, stream=None):
     """x [rows, heads, dim] rotated by positions (cuda int32 or float32 [rows]; None: row numbers).  out may be x."""
-    import torch
+    dtype, number, device, dim = _kind(x)
+    n = x.shape[0]
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = _torch.empty(x.shape, dtype=dtype, device=x.device)
     assert out.shape == x.shape
-    pos, real = _positions(positions, x.shape[0], x.device)
-    if x.shape[0] == 0:
+    pos, real = _positions(positions, n, device)
+    if n == 0:
         return out
-    rc = _library().gnn_rope(rot.ref, _dtype(x), x.shape[2], ctypes.byref(_heads(x)), ctypes.byref(_heads(out, x)), pos,
-                             real, x.shape[0], _stream_handle(stream))
+    _HEADS.pack_into(_AREA, 0, *_heads(x, dtype, device, dim))
+    _HEADS.pack_into(_AREA, _HEADS.size, *_heads(out, dtype, device, dim))
+    rc = _lib.gnn_rope(rot.address, number, dim, _AT[0], _AT[1], pos, real, n, _stream(stream, device))
     if rc != GNN_OK:
         raise GnnError(rc, "gnn_rope")
     return out
@@ -132,26 +151,33 @@ def qk_norm_rope(rot: Rotary, q, k, positions=None, v=None, q_gain=None, k_gain=
                  k_out=None, v_out=None, rows=None, stream=None):
     """(q_out, k_out, v_out): q and k normalised for each head and rotated, v copied.  With rows (cuda int64 [rows]),
     row r of k and v goes to row rows[r] of k_out and v_out, which are then given."""
-    import torch
-    n = q.shape[0]
-    assert k.shape[0] == n and (v is None or v.shape == k.shape)
+    dtype, number, device, dim = _kind(q)
+    n, k_shape = q.shape[0], k.shape
+    assert k_shape[0] == n and (v is None or v.shape == k_shape), "rows or key heads differ"
     assert rows is None or (k_out is not None and (v is None or v_out is not None)), "rows need k_out and v_out"
     assert v is not None or v_out is None, "v_out without v"
-    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
-    k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device) if k_out is None else k_out
+    if q_out is None:
+        q_out = _torch.empty(q.shape, dtype=dtype, device=q.device)
+    if k_out is None:
+        k_out = _torch.empty(k_shape, dtype=dtype, device=q.device)
     if v is not None and v_out is None:
-        v_out = torch.empty(v.shape, dtype=v.dtype, device=v.device)
-    assert q_out.shape == q.shape and k_out.shape[1:] == k.shape[1:] and (rows is not None or k_out.shape[0] == n)
-    assert v is None or (v_out.shape[1:] == v.shape[1:] and v_out.shape[0] == k_out.shape[0])
-    pos, real = _positions(positions, n, q.device)
-    at = _vector(rows, n, torch.int64, q.device)
-    gains = [_vector(g, q.shape[2], torch.float32, q.device) for g in (q_gain, k_gain)]
-    if n == 0 or k_out.shape[0] == 0:
-        assert n == 0, "k_out has no rows"
+        v_out = _torch.empty(k_shape, dtype=dtype, device=q.device)
+    m = k_out.shape[0]
+    assert q_out.shape == q.shape and (rows is not None or m == n), "outputs of other sizes"
+    assert v is None or v_out.shape[0] == m, "k_out and v_out differ"
+    pos, real = _positions(positions, n, device)
+    at = _vector(rows, n, _torch.int64, device)
+    gq, gk = _vector(q_gain, dim, _torch.float32, device), _vector(k_gain, dim, _torch.float32, device)
+    if n == 0:
         return q_out, k_out, v_out
-    views = [None if x is None else ctypes.byref(_heads(x, q)) for x in (q, k, v, q_out, k_out, v_out)]
-    rc = _library().gnn_qk_norm_rope(rot.ref, _dtype(q), q.shape[2], eps, *gains, *views, pos, real, at,
-                                     k_out.shape[0], n, _stream_handle(stream))
+    assert m > 0, "k_out has no rows"
+    size = _HEADS.size
+    for i, x in enumerate((q, k, v, q_out, k_out, v_out)):
+        if x is not None:
+            _HEADS.pack_into(_AREA, i * size, *_heads(x, dtype, device, dim))
+    a = _AT
+    rc = _lib.gnn_qk_norm_rope(rot.address, number, dim, eps, gq, gk, a[0], a[1], a[2] if v is not None else None, a[3], a[4],
+                               a[5] if v is not None else None, pos, real, at, m, n, _stream(stream, device))
     if rc != GNN_OK:
         raise GnnError(rc, "gnn_qk_norm_rope")
     return q_out, k_out, v_out
@@ -161,9 +187,8 @@ class WindowAttention:
     """One handle of gnn_attention_create on the current device (a stream's own; see include/gnn.h)."""
 
     def __init__(self):
-        self.lib = _library()
         h = _vp()
-        rc = self.lib.gnn_attention_create(ctypes.byref(h))
+        rc = _library().gnn_attention_create(ctypes.byref(h))
         if rc != GNN_OK:
             raise GnnError(rc, "gnn_attention_create")
         self.handle = h
@@ -174,26 +199,27 @@ class WindowAttention:
         fp16.  q_start: cuda int32 [sequences + 1]; kv_start, kv_len: cuda int32 [sequences], or None: a sequence's keys
         are the rows of its queries.  left, right: keys visible before and after a query's own position (-1: all),
         sinks: first keys that stay visible; max_q, max_kv: the most queries and keys of a sequence, when known."""
-        import torch
+        dtype, number, device, dim = _kind(q)
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        n = q_start.numel() - 1
-        assert n >= 0 and out.shape == q.shape and k.shape == v.shape
-        call = GnnAttentionCall(_dtype(q), q.shape[2], _heads(q), _heads(k, q), _heads(v, q), _heads(out, q),
-                                _vector(q_start, n + 1, torch.int32, q.device), _vector(kv_start, n, torch.int32, q.device),
-                                _vector(kv_len, n, torch.int32, q.device), q.shape[0], k.shape[0], n, max_q, max_kv, left,
-                                right, sinks, 1.0 / math.sqrt(q.shape[2]) if scale is None else scale, 0)
-        rc = self.lib.gnn_attention_run(self.handle, ctypes.byref(call), _stream_handle(stream))
+            out = _torch.empty(q.shape, dtype=dtype, device=q.device)
+        n, int32, rows = q_start.numel() - 1, _torch.int32, k.shape[0]
+        assert n >= 0 and out.shape == q.shape and v.shape[0] == rows, "outputs, keys or values of other sizes"
+        _CALL.pack_into(_AREA, 0, number, dim, *_heads(q, dtype, device, dim), *_heads(k, dtype, device, dim),
+                        *_heads(v, dtype, device, dim), *_heads(out, dtype, device, dim),
+                        _vector(q_start, n + 1, int32, device), _vector(kv_start, n, int32, device) or 0,
+                        _vector(kv_len, n, int32, device) or 0, q.shape[0], rows, n, max_q, max_kv, left, right, sinks,
+                        1.0 / math.sqrt(dim) if scale is None else scale, 0)
+        rc = _lib.gnn_attention_run(self.handle, _AT[0], _stream(stream, device))
         if rc != GNN_OK:
             raise GnnError(rc, "gnn_attention_run")
         return out
 
     def status(self, stream=None) -> int:
-        return self.lib.gnn_attention_status(self.handle, _stream_handle(stream))
+        return binding.load_library().gnn_attention_status(self.handle, binding._stream_handle(stream))
 
     def close(self):
         if getattr(self, "handle", None):
-            self.lib.gnn_attention_destroy(self.handle)
+            binding.load_library().gnn_attention_destroy(self.handle)
             self.handle = None
 
     def __del__(self):
