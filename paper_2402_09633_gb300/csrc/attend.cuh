@@ -55,7 +55,7 @@ __device__ __forceinline__ Seen seen_keys(int pos, int len, int left, int right,
 // One query row of one head by one warp: 32 keys at a time, a key to a lane for the scores, the head's
 // elements spread over the lanes for the values.  q: the row in fp32, in shared memory.
 template <typename T>
-__device__ __forceinline__ void attend_row(const AttendParams& p, const Sequence& sq, int i, int head, const float* q) {
+__device__ __noinline__ void attend_row(const AttendParams& p, const Sequence& sq, int i, int head, const float* q) {
   const int lane = threadIdx.x & 31, kv = head / (p.heads / p.kv_heads);
   const Seen s = seen_keys(sq.len - sq.nq + i, sq.len, p.left, p.right, p.sinks);
   const int n = s.first + (s.hi - s.lo);

@@ -8,32 +8,40 @@
 namespace gnn {
 
 constexpr int kTileQ = 128, kTileK = 128;          // queries of a tile, keys of a block of keys
-// Two softmax warpgroups, and one whose first warp issues the products and whose second the copies.  All are
-// launched with 168 registers a thread; the last one hands over what it does not need: 2 * 200 + 104 = 3 * 168.
-constexpr int kAttendThreads = 384, kSoftmaxRegs = 200, kControlRegs = 104;
+// Two softmax warpgroups, one to a tile, and one for control: one or two warps that issue the products, and
+// one that finds the work and issues the copies.  All are launched
+// with 168 registers a thread; the last one hands over what it does not need: 2 * 216 + 72 = 3 * 168.
+constexpr int kAttendThreads = 384, kSoftmaxRegs = 216, kControlRegs = 72;
+constexpr int kMmaWarp = 8, kCopyWarp = 10;
+constexpr int kItemSlots = 4;                      // items that the copy warp is ahead by, at most
 
 template <int DP>
 struct AttendShape {
   static constexpr bool kApart = DP == 64;         // P has columns of its own; otherwise it lies over S
+  // Apart, a tile's products wait for nothing of the other tile's: a warp to each.  Over S, a tile's P V and the next
+  // Q K^T are one chain, and two chains in turn keep the tensor cores busy while two side by side end together.
+  static constexpr int kMmaWarps = kApart ? 2 : 1;
   static constexpr int kQBufs = DP == 64 ? 2 : 1;
   static constexpr int kStages = DP == 64 ? 8 : 4; // of a block of keys or of values each
   static constexpr int kTileBytes = kTileQ * DP * 2;
   static constexpr int kS = 0, kP = kApart ? 256 : 0, kPStep = kApart ? 64 : 128, kO = kApart ? 384 : 256;
   static constexpr int kSmem = kQBufs * 2 * kTileBytes + kStages * kTileBytes;
 };
-struct AttendBars {
-  uint64_t q_full[2], q_empty[2], kv_full[8], kv_empty[8], s_full[2], s_free[2], p_full[2], pv_done[2], drain;
-  uint32_t tmem;
-  int abort;
-};
-template <int DP>
-constexpr int attend_smem_bytes() { return AttendShape<DP>::kSmem + 8 * 128 * 4 + (int)sizeof(AttendBars) + 1024; }
-
 // ------------------------------------------------------------------ PTX
 __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
       ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar)) : "memory");
+}
+// One try that may sleep for up to `ns`: a warp that waits takes no issue slots from those that compute.
+__device__ __forceinline__ bool mbar_wait_hint(uint64_t* bar, uint32_t parity, uint32_t ns) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2, %3;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}\n"
+      : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity), "r"(ns) : "memory");
+  return ok != 0;
 }
 template <int N> __device__ __forceinline__ void regs_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
@@ -60,6 +68,13 @@ __device__ __forceinline__ void tmem_wait_ld_32(float* v) {
                :
                : "memory");
 }
+__device__ __forceinline__ void tmem_st_32x16(uint32_t a, const uint32_t* v) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(a),
+      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+      "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+      : "memory");
+}
 // 32 lanes x 8 columns, scaled by each lane's factor, in place.
 __device__ __forceinline__ void tmem_scale_32x8(uint32_t a, float f) {
   float v[8];
@@ -75,20 +90,14 @@ __device__ __forceinline__ void tmem_scale_32x8(uint32_t a, float f) {
                "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
                : "memory");
 }
-__device__ __forceinline__ void tmem_st_32x32(uint32_t a, const uint32_t* v) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,"
-      "%30,%31,%32};" ::"r"(a),
-      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
-      "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]),
-      "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]),
-      "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
-      : "memory");
-}
 __device__ __forceinline__ float exp2_approx(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
   return y;
 }
 template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b);
@@ -99,7 +108,7 @@ template <> __device__ __forceinline__ uint32_t pack2<__half>(float a, float b) 
 }
 // Instruction descriptor, kind::f16: A and B of type T, D fp32, A K-major, B K-major or (b_mn) N-major.
 template <typename T>
-__device__ __forceinline__ uint32_t idesc_attend(uint32_t M, uint32_t N, bool b_mn) {
+__host__ __device__ constexpr uint32_t idesc_attend(uint32_t M, uint32_t N, bool b_mn) {
   const uint32_t f = sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
   return (1u << 4) | (f << 7) | (f << 10) | ((b_mn ? 1u : 0u) << 16) | ((N >> 3) << 17) | ((M >> 4) << 24);
 }
@@ -111,8 +120,10 @@ __device__ __forceinline__ uint64_t sdesc_nmajor_sw128(uint32_t saddr, uint32_t 
 }
 
 // ------------------------------------------------------------------ work
-// The rows of the sequence that a tile has, and the blocks of keys it goes through: [0, sinks) and [lo, hi).
-struct AttendTile { int row, n, pos, head, sinks, lo, hi; };
+// The rows of the sequence that a tile has, and the blocks of keys it goes through: [0, sinks) and [lo, hi).  A
+// block is seen whole by every row when it is below whole_hi and either from whole_lo on or below whole_sinks.
+// Row r of the tile sees the keys j <= top + r and (j >= low + r or j < sinks of the call).
+struct AttendTile { int row, n, head, sinks, lo, hi, whole_sinks, whole_lo, whole_hi, top, low; };
 struct AttendItem {
   Sequence sq;
   AttendTile t[2];
@@ -131,22 +142,30 @@ __device__ __forceinline__ bool tile_sees(const AttendTile& t, int kb) {
 }
 
 __device__ __forceinline__ AttendTile attend_tile(const AttendParams& p, const Sequence& sq, int row, int head) {
-  AttendTile t = {row, min(max(sq.nq - row, 0), kTileQ), sq.len - sq.nq + row, head, 0, 0, 0};
+  AttendTile t = {row, min(max(sq.nq - row, 0), kTileQ), head, 0, 0, 0, 0, 0, 0, 0, 0};
   if (t.n == 0) return t;
-  const Seen a = seen_keys(t.pos, sq.len, p.left, p.right, p.sinks);
-  const Seen z = seen_keys(t.pos + t.n - 1, sq.len, p.left, p.right, p.sinks);
+  const int pos = sq.len - sq.nq + row;
+  const Seen a = seen_keys(pos, sq.len, p.left, p.right, p.sinks);
+  const Seen z = seen_keys(pos + t.n - 1, sq.len, p.left, p.right, p.sinks);
   if (z.hi <= 0) return t;
   t.hi = (z.hi + kTileK - 1) / kTileK;
   t.lo = min(a.lo, z.hi) / kTileK;
   t.sinks = min((z.first + kTileK - 1) / kTileK, t.lo);
+  t.whole_hi = a.hi / kTileK;
+  t.whole_lo = (z.lo + kTileK - 1) / kTileK;
+  t.whole_sinks = p.sinks / kTileK;
+  // some row sees a key, so a negative pos + right is above -kTileQ
+  t.top = p.right < 0 ? INT_MAX - kTileQ : (int)min((int64_t)INT_MAX - kTileQ, (int64_t)pos + p.right);
+  t.low = p.left < 0 ? -kTileQ : (int)max((int64_t)-kTileQ, (int64_t)pos - p.left);
   return t;
 }
 
 // Item `at`: false when it has no rows.  A sequence's items start at slot q0 / rows + b, which leaves room for
 // ceil(nq / rows) of them and needs no sum over the sequences before it.
-__device__ __forceinline__ bool attend_item(const AttendParams& p, const AttendGrid& g, int64_t at, AttendItem& it) {
+__device__ __noinline__ bool attend_item(const AttendParams& p, const AttendGrid& g, int64_t at, AttendItem& it) {
   const int slot = (int)(at / g.heads), h = (int)(at - (int64_t)slot * g.heads);
   int a = 0, z = p.n_seqs;
+#pragma unroll 1
   while (z - a > 1) {
     const int mid = (int)(((int64_t)a + z) / 2);
     if (min(max(p.q_start[mid], 0), p.n_q_rows) / g.rows + mid <= slot) a = mid; else z = mid;
@@ -176,6 +195,16 @@ __device__ __forceinline__ bool attend_item(const AttendParams& p, const AttendG
 }
 
 // ------------------------------------------------------------------ kernel
+struct AttendBars {
+  uint64_t q_full[2], q_empty[2], kv_full[8], kv_empty[8], s_full[2], s_free[2], p_half[2], p_full[2], pv_done[2], drain[2];
+  uint64_t item_full[kItemSlots], item_empty[kItemSlots];
+  AttendItem item[kItemSlots];
+  uint32_t tmem;
+  int abort;
+};
+template <int DP>
+constexpr int attend_smem_bytes() { return AttendShape<DP>::kSmem + 8 * 128 * 4 + (int)sizeof(AttendBars) + 1024; }
+
 template <typename T, int DP>
 __global__ void __launch_bounds__(kAttendThreads, 1)
     attend_tile_kernel(const __grid_constant__ AttendParams p, const __grid_constant__ AttendGrid g,
@@ -188,185 +217,248 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
   uint8_t* kv_buf = smem + S::kQBufs * 2 * S::kTileBytes;
   float* q_rows = reinterpret_cast<float*>(smem + S::kSmem);             // a row per softmax warp, for the repair
   AttendBars& b = *reinterpret_cast<AttendBars*>(q_rows + 8 * 128);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
   volatile int* abort = &b.abort;
 
-  if (warp == 9 && lane == 0) {
+  if (warp == kCopyWarp && lane == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(&b.q_full[i], 1);
-      mbar_init(&b.q_empty[i], 1);
+      mbar_init(&b.q_empty[i], S::kMmaWarps);
       mbar_init(&b.s_full[i], 1);
       mbar_init(&b.s_free[i], 4);
+      mbar_init(&b.p_half[i], 4);
       mbar_init(&b.p_full[i], 4);
       mbar_init(&b.pv_done[i], 1);
+      mbar_init(&b.drain[i], 1);
     }
     for (int i = 0; i < 8; ++i) {
       mbar_init(&b.kv_full[i], 1);
-      mbar_init(&b.kv_empty[i], 1);
+      mbar_init(&b.kv_empty[i], S::kMmaWarps);
     }
-    mbar_init(&b.drain, 1);
+    for (int i = 0; i < kItemSlots; ++i) {
+      mbar_init(&b.item_full[i], 1);
+      mbar_init(&b.item_empty[i], 8 + S::kMmaWarps);
+    }
     b.abort = 0;
     fence_mbar_init();
   }
-  if (warp == 8) {
+  if (warp == kMmaWarp) {
     tmem_alloc(&b.tmem, 512);
     tmem_relinquish();
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&b.tmem);
+  const uint32_t tmem = (uint32_t)uniform((int)*reinterpret_cast<volatile uint32_t*>(&b.tmem));
   pdl_wait();
 
   const int halves = p.dim > 64 ? 2 : 1;
-  auto wait = [&](uint64_t* bar, int64_t phase) {  // the whole warp, for the completion of the bar's phase
-    return warp_all(bounded_wait(bar, (uint32_t)(phase & 1), abort, p.err));
+  // The whole warp, for the completion of the bar's phase, within the library's limit.
+  auto wait = [&](uint64_t* bar, uint32_t phase) {
+    uint64_t t0 = 0;
+#pragma unroll 1
+    for (;;) {
+      if (warp_all(mbar_wait_hint(bar, phase & 1, 200000))) return true;
+      const uint64_t now = global_timer_ns();
+      if (t0 == 0) t0 = now;
+      const bool late = now - t0 > kWaitLimitNs;
+      if (late) {
+        atomicOr(p.err, DEV_ERR_TIMEOUT);
+        *abort = 1;
+      }
+      if (__any_sync(0xffffffffu, late || *abort)) return false;
+    }
   };
   if (warp >= 8) {
     regs_down<kControlRegs>();
-    if (warp == 9) {
-      // ---------------- copies: queries, then keys and values block by block, through the ring
+    if (warp == kCopyWarp) {
+      // ---------------- the work, item by item; its queries, and its keys and values through the ring
       const uint32_t bytes = (uint32_t)halves * kTileQ * 128;
-      int64_t kv = 0, q = 0;
+      uint32_t kv = 0, q = 0, items = 0;
       bool ok = true;
-      for (int64_t at = blockIdx.x; ok && at < g.items; at += gridDim.x) {
+      for (int64_t at = blockIdx.x; ok; at += gridDim.x) {
         AttendItem it;
-        if (!attend_item(p, g, at, it) || it.n == 0) continue;
-        const int qb = (int)(q % S::kQBufs);
+        const bool end = at >= g.items;
+        if (end) it.n = -1;
+        else if (!attend_item(p, g, at, it)) continue;
+        const uint32_t slot = items % kItemSlots;
+        if (items >= kItemSlots) ok = wait(&b.item_empty[slot], items / kItemSlots - 1);
+        if (!ok) break;
+        if (lane == 0) {
+          b.item[slot] = it;
+          mbar_arrive(&b.item_full[slot]);
+        }
+        ++items;
+        if (end) break;
+        if (it.n == 0) continue;
+        const uint32_t qb = q % S::kQBufs;
         if (q >= S::kQBufs) ok = wait(&b.q_empty[qb], q / S::kQBufs - 1);
         if (!ok) break;
         if (lane == 0) {
           const bool two = it.t[1].hi > 0, one = it.t[0].hi > 0;
           mbar_arrive_expect_tx(&b.q_full[qb], bytes * ((one ? 1 : 0) + (two ? 1 : 0)));
-  #pragma unroll
+#pragma unroll
           for (int t = 0; t < 2; ++t)
             if (t ? two : one)
+#pragma unroll 1
               for (int h = 0; h < halves; ++h)
                 tma_load_3d(q_buf + (qb * 2 + t) * S::kTileBytes + h * kTileQ * 128, &map_q, 64 * h, it.t[t].head,
                             it.sq.q0 + it.t[t].row, &b.q_full[qb]);
         }
         ++q;
+#pragma unroll 1
         for (int i = 0; i < it.n && ok; ++i) {
           const int row = it.sq.k0 + it.block(i) * kTileK;
-          for (int kind = 0; kind < 2 && ok; ++kind, ++kv) {
-            const int st = (int)(kv % S::kStages);
+#pragma unroll 1
+          for (int kind = 0; kind < 2; ++kind, ++kv) {
+            const uint32_t st = kv % S::kStages;
             if (kv >= S::kStages) ok = wait(&b.kv_empty[st], kv / S::kStages - 1);
             if (!ok) break;
             if (lane == 0) {
               mbar_arrive_expect_tx(&b.kv_full[st], bytes);
               for (int h = 0; h < halves; ++h)
-                tma_load_3d(kv_buf + st * S::kTileBytes + h * kTileK * 128, kind ? &map_v : &map_k, 64 * h, it.kv_head, row,
-                            &b.kv_full[st]);
+                tma_load_3d(kv_buf + st * S::kTileBytes + h * kTileK * 128, kind ? &map_v : &map_k, 64 * h, it.kv_head,
+                            row, &b.kv_full[st]);
             }
           }
         }
         __syncwarp();
       }
       // every copy lands before the block leaves
-      for (int i = 0; i < S::kStages; ++i) {
-        const int64_t uses = (kv - i + S::kStages - 1) / S::kStages;
-        if (kv > i) drain_wait(&b.kv_full[i], (uint32_t)((uses - 1) & 1));
-      }
-      for (int i = 0; i < S::kQBufs; ++i) {
-        const int64_t uses = (q - i + S::kQBufs - 1) / S::kQBufs;
-        if (q > i) drain_wait(&b.q_full[i], (uint32_t)((uses - 1) & 1));
-      }
+#pragma unroll 1
+      for (uint32_t i = 0; i < S::kStages; ++i)
+        if (kv > i) drain_wait(&b.kv_full[i], (kv - 1 - i) / S::kStages & 1);
+#pragma unroll 1
+      for (uint32_t i = 0; i < S::kQBufs; ++i)
+        if (q > i) drain_wait(&b.q_full[i], (q - 1 - i) / S::kQBufs & 1);
       // offsets that point outside the views
+#pragma unroll 1
       for (int64_t s = (int64_t)blockIdx.x * 32 + lane; s < p.n_seqs; s += (int64_t)gridDim.x * 32) {
         bool bad;
         sequence(p, (int)s, &bad);
         if (bad) atomicOr(p.err, DEV_ERR_INDEX_RANGE);
       }
-    } else if (warp == 8) {
-      // ---------------- products
+    } else if (warp < kMmaWarp + S::kMmaWarps) {
+      // ---------------- the products: of one tile, or of both in turn
+      constexpr int NT = 2 / S::kMmaWarps;
+      const int first = warp - kMmaWarp;
       const int steps = (p.dim + 15) / 16;
-      const uint32_t id_qk = idesc_attend<T>(kTileQ, kTileK, false);
+      constexpr uint32_t id_qk = idesc_attend<T>(kTileQ, kTileK, false);
+      // Descriptors and addresses are computed by the whole warp, outside the elected thread's branch, so that they
+      // stay in uniform registers: inside it an MMA takes four times as long to issue.
+      const uint32_t q_base = (uint32_t)uniform((int)smem_u32(q_buf)), kv_base = (uint32_t)uniform((int)smem_u32(kv_buf));
+      const uint64_t q_desc = sdesc_kmajor_sw128(q_base), k_desc = sdesc_kmajor_sw128(kv_base),
+                     v_desc = sdesc_nmajor_sw128(kv_base, kTileK * 128);
       const uint32_t id_pv = idesc_attend<T>(kTileQ, (uint32_t)steps * 16, true);
-      int64_t kv = 0, q = 0;
-      int64_t qk_n[2] = {0, 0}, pv_n[2] = {0, 0};
+      uint32_t kv = 0, q = 0, items = 0, qk_n[NT] = {}, pv_n[NT] = {};
       bool ok = true;
-      for (int64_t at = blockIdx.x; ok && at < g.items; at += gridDim.x) {
-        AttendItem it;
-        if (!attend_item(p, g, at, it) || it.n == 0) continue;
-        const int qb = (int)(q % S::kQBufs);
-        bool fresh[2] = {true, true};
-        auto qk = [&](int t, int st) {                 // S_t = Q_t K^T, once S_t's last scores have been read
-          if (S::kApart && qk_n[t] > 0) ok = ok && wait(&b.s_free[t], qk_n[t] - 1);
+      while (ok) {
+        const uint32_t slot = items % kItemSlots;
+        ok = wait(&b.item_full[slot], items / kItemSlots);
+        if (!ok) break;
+        AttendTile tile[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          const AttendTile& from = b.item[slot].t[first + j];
+          tile[j].sinks = uniform(from.sinks);
+          tile[j].lo = uniform(from.lo);
+          tile[j].hi = uniform(from.hi);
+        }
+        const int n = uniform(b.item[slot].n), sinks = uniform(b.item[slot].sinks), lo = uniform(b.item[slot].lo),
+                  len = uniform(b.item[slot].sq.len);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&b.item_empty[slot]);
+        ++items;
+        if (n < 0) break;
+        if (n == 0) continue;
+        const uint32_t qb = q % S::kQBufs;
+        bool fresh[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) fresh[j] = true;
+        auto qk = [&](int j, uint32_t st) {          // S = Q K^T, once the last scores have been read
+          const int t = first + j;
+          if (S::kApart && qk_n[j] > 0) ok = wait(&b.s_free[t], qk_n[j] - 1);
           if (!ok) return;
           tc_fence_after();
+          const uint64_t qa = q_desc + ((qb * 2 + t) * S::kTileBytes >> 4), ka = k_desc + (st * S::kTileBytes >> 4);
           if (elect_one()) {
-            const uint32_t qa = smem_u32(q_buf + (qb * 2 + t) * S::kTileBytes), ka = smem_u32(kv_buf + st * S::kTileBytes);
-            for (int k = 0; k < steps; ++k) {
-              const uint32_t off = (k >> 2) * kTileQ * 128 + (k & 3) * 32;
-              mma_bf16_ss(tmem + S::kS + 128 * t, sdesc_kmajor_sw128(qa + off), sdesc_kmajor_sw128(ka + off), id_qk, k > 0);
+#pragma unroll
+            for (int k = 0; k < DP / 16; ++k) {
+              if (k >= steps) break;
+              const uint64_t off = ((k >> 2) * kTileQ * 128 + (k & 3) * 32) >> 4;
+              mma_bf16_ss(tmem + S::kS + 128 * t, qa + off, ka + off, id_qk, k > 0);
             }
             mma_commit(&b.s_full[t]);
           }
           __syncwarp();
-          ++qk_n[t];
+          ++qk_n[j];
         };
         ok = wait(&b.q_full[qb], q / S::kQBufs);
-        if (!ok) break;
-        for (int i = -1; i < it.n && ok; ++i) {
-          // keys of block i + 1
-          const bool more = i + 1 < it.n;
-          const int kb = i >= 0 ? it.block(i) : 0, next = more ? it.block(i + 1) : 0;
-          const int64_t kn = kv + 2 * (i + 1), vn = kv + 2 * i + 1;
-          const int ks = (int)(kn % S::kStages), vs = (int)(vn % S::kStages);
+        for (int i = -1; i < n && ok; ++i) {
+          const bool more = i + 1 < n;
+          const int kb = i < sinks ? i : lo + (i - sinks), next = i + 1 < sinks ? i + 1 : lo + (i + 1 - sinks);
+          const uint32_t kn = kv + 2 * (i + 1), vn = kv + 2 * i + 1;
+          const uint32_t ks = kn % S::kStages, vs = vn % S::kStages;
           if (more) ok = wait(&b.kv_full[ks], kn / S::kStages);
           if (!ok) break;
-          if (S::kApart && more)
-  #pragma unroll
-            for (int t = 0; t < 2; ++t)
-              if (tile_sees(it.t[t], next)) qk(t, ks);
+          if (S::kApart && more && tile_sees(tile[0], next)) qk(0, ks);
           if (!ok) break;
           if (i >= 0) {
             ok = wait(&b.kv_full[vs], vn / S::kStages);
             if (!ok) break;
-            // values of rows behind the sequence's last key: zeros, so that weights of zero leave no trace of them
-            const int have = it.sq.len - kb * kTileK;
+            // Values of rows behind the sequence's last key: zeros, so that weights of zero leave no trace of them.
+            // (Where two warps do this, each does before its own products.)
+            const int have = len - kb * kTileK;
             if (have < kTileK) {
-              for (int r = max(have, 0) * 8 + lane; r < kTileK * 8; r += 32)
+#pragma unroll 1
+              for (int r = have * 8 + lane; r < kTileK * 8; r += 32)
                 for (int h = 0; h < halves; ++h)
                   *reinterpret_cast<uint4*>(kv_buf + vs * S::kTileBytes + h * kTileK * 128 + r * 16) = make_uint4(0, 0, 0, 0);
               fence_async_shared();
               __syncwarp();
             }
           }
-  #pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            if (!ok) break;
-            if (i >= 0 && tile_sees(it.t[t], kb)) {
-              ok = wait(&b.p_full[t], pv_n[t]);
-              if (!ok) break;
-              tc_fence_after();
-              if (elect_one()) {
-                const uint32_t va = smem_u32(kv_buf + vs * S::kTileBytes);
-                for (int k = 0; k < kTileK / 16; ++k)
-                  mma_bf16_ts(tmem + S::kO + DP * t, tmem + S::kP + S::kPStep * t + 8 * k,
-                              sdesc_nmajor_sw128(va + k * 2048, kTileK * 128), id_pv, !fresh[t] || k > 0);
-                mma_commit(&b.pv_done[t]);
+#pragma unroll
+          for (int j = 0; j < NT; ++j) {
+            if (i >= 0 && tile_sees(tile[j], kb)) {  // O += P V, in halves of 64 keys
+              const int t = first + j;
+              const uint64_t va = v_desc + (vs * S::kTileBytes >> 4);
+              const uint32_t acc = fresh[j] ? 0u : 1u;
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                ok = ok && wait(h ? &b.p_full[t] : &b.p_half[t], pv_n[j]);
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+#pragma unroll
+                  for (int k = 4 * h; k < 4 * h + 4; ++k)
+                    mma_bf16_ts(tmem + S::kO + DP * t, tmem + S::kP + S::kPStep * t + 8 * k,
+                                va + (k * 2048 >> 4), id_pv, k > 0 ? 1u : acc);
+                  if (h) mma_commit(&b.pv_done[t]);
+                }
+                __syncwarp();
               }
-              __syncwarp();
-              fresh[t] = false;
-              ++pv_n[t];
+              if (!ok) break;
+              fresh[j] = false;
+              ++pv_n[j];
             }
-            if (!S::kApart && more && tile_sees(it.t[t], next)) qk(t, ks);
+            if (!S::kApart && more && tile_sees(tile[j], next)) qk(j, ks);
+            if (!ok) break;
           }
           if (!ok) break;
           if (elect_one()) {
             if (more) mma_commit(&b.kv_empty[ks]);
             if (i >= 0) mma_commit(&b.kv_empty[vs]);
-            if (i + 2 == it.n) mma_commit(&b.q_empty[qb]);   // the item's last Q K^T is out
+            if (i + 2 == n) mma_commit(&b.q_empty[qb]);      // the item's last Q K^T is out
           }
           __syncwarp();
         }
-        kv += 2 * (int64_t)it.n;
+        kv += 2 * n;
         ++q;
       }
-      if (elect_one()) mma_commit(&b.drain);
+      if (elect_one()) mma_commit(&b.drain[first]);
       __syncwarp();
-      drain_wait(&b.drain, 0);
+      drain_wait(&b.drain[first], 0);
     }
   } else {
     regs_up<kSoftmaxRegs>();
@@ -375,121 +467,191 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t ts = tmem + lanes + S::kS + 128 * wg, tp = tmem + lanes + S::kP + S::kPStep * wg,
                    to = tmem + lanes + S::kO + DP * wg;
-    const bool negative = p.scale_log2 < 0.f;
-    const float sign = negative ? -1.f : 1.f;
     const float scale = fabsf(p.scale_log2);
     const float slack = 8.f / scale;                 // scores may outgrow the running maximum by 2^8
-    int64_t n = 0;                                   // blocks this tile has gone through
+    uint32_t n = 0, items = 0;                       // blocks this tile has gone through
     bool ok = true, dirty = false;
-    for (int64_t at = blockIdx.x; ok && at < g.items; at += gridDim.x) {
-      AttendItem it;
-      if (!attend_item(p, g, at, it)) continue;
-      const AttendTile t = wg ? it.t[1] : it.t[0];
-      if (t.n == 0) continue;
-      const int pos = t.pos + row;
+    while (ok) {
+      const uint32_t slot = items % kItemSlots;
+      ok = wait(&b.item_full[slot], items / kItemSlots);
+      if (!ok) break;
+      const AttendItem& item = b.item[slot];
+      const int rows = item.t[wg].n, len = item.sq.len, item_n = item.n;
+      const int sinks = item.t[wg].sinks, lo = item.t[wg].lo, blocks = sinks + (item.t[wg].hi - lo);
+      const int whole_sinks = item.t[wg].whole_sinks, whole_lo = item.t[wg].whole_lo, whole_hi = item.t[wg].whole_hi;
+      const int top = row >= rows ? -1 : min(len - 1, item.t[wg].top + row), low = max(0, item.t[wg].low + row);
+      char* out = p.out.data + (int64_t)(item.sq.q0 + item.t[wg].row + row) * p.out.row_bytes +
+                  (int64_t)item.t[wg].head * p.out.head_bytes;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&b.item_empty[slot]);
+      ++items;
+      if (item_n < 0) break;
+      if (rows == 0) continue;
       float m = -INFINITY, l = 0.f;
-      bool first = true;
-      for (int i = 0; i < it.n && ok; ++i) {
-        const int kb = it.block(i);
-        if (!tile_sees(t, kb)) continue;
-        ok = wait(&b.s_full[wg], n);
-        if (!ok) break;
+      const float2 scale2 = make_float2(scale, scale);
+      auto read = [&](float* s) {                    // the block's scores
         tc_fence_after();
-        float s[128];
 #pragma unroll
         for (int c = 0; c < 4; ++c) tmem_ld_32x32(ts + 32 * c, s + 32 * c);
 #pragma unroll
         for (int c = 0; c < 4; ++c) tmem_wait_ld_32(s + 32 * c);
-        if (S::kApart) {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&b.s_free[wg]);
-        }
-        const int j0 = kb * kTileK, last = t.pos + t.n - 1;
-        const bool whole = j0 + kTileK <= it.sq.len && (p.right < 0 || j0 + kTileK - 1 <= (int64_t)t.pos + p.right) &&
-                           (p.left < 0 || j0 >= (int64_t)last - p.left || j0 + kTileK <= p.sinks);
-        if (!whole || negative) {
-          // columns c <= top and (c >= low or c < sink) are seen; as bits, 32 columns to a word
-          auto column = [&](int64_t j) { return (int)max((int64_t)-1, min((int64_t)kTileK, j - j0)); };
-          const int top = min(column(it.sq.len - 1), p.right < 0 ? kTileK : column((int64_t)pos + p.right));
-          const int low = p.left < 0 ? 0 : column((int64_t)pos - p.left), sink = column(p.sinks);
-          auto below = [](int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; };
-#pragma unroll
-          for (int c = 0; c < 128; c += 32) {
-            const uint32_t see = below(top + 1 - c) & (~below(low - c) | below(sink - c));
-#pragma unroll
-            for (int e = 0; e < 32; ++e) s[c + e] = see >> e & 1u ? s[c + e] * sign : -INFINITY;
-          }
-        }
-        float mx[4];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) mx[c] = s[c];
-#pragma unroll
-        for (int c = 4; c < 128; c += 8)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) mx[e] = fmaxf(fmaxf(mx[e], s[c + e]), s[min(c + 4 + e, 127)]);
-        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-        const bool grow = top > m + slack || (m == -INFINITY && top > m);
-        const float mn = grow ? top : m;
-        const float shrink = !grow ? 1.f : m == -INFINITY ? 0.f : exp2_approx((m - mn) * scale);
-        m = mn;
-        const float off = m == -INFINITY ? 0.f : -m * scale;
-        l *= shrink;
-        // the last product with these weights' columns, and into these outputs, is over
-        if (!first) ok = wait(&b.pv_done[wg], n - 1);
-        if (!ok) break;
-        tc_fence_after();
-        if (!first && __any_sync(0xffffffffu, grow)) {
-#pragma unroll 1
-          for (int c = 0; c < DP; c += 8) tmem_scale_32x8(to + c, shrink);
-        }
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t w[32];
-#pragma unroll
-          for (int c = 0; c < 32; ++c) {
-            const float a = exp2_approx(fmaf(s[64 * h + 2 * c], scale, off));
-            const float d = exp2_approx(fmaf(s[64 * h + 2 * c + 1], scale, off));
-            sum[(2 * c) & 3] += a;
-            sum[(2 * c + 1) & 3] += d;
-            w[c] = pack2<T>(a, d);
-          }
-          tmem_st_32x32(tp + 32 * h, w);
-        }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      };
+      auto scores_read = [&] {
+        if (!S::kApart) return;
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&b.s_free[wg]);
+      };
+      auto stored = [&](uint64_t* bar) {             // half of the weights are in place
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&b.p_full[wg]);
-        first = false;
-        ++n;
+        if (lane == 0) mbar_arrive(bar);
+      };
+      // 32 scores to weights, and their sum
+      auto weigh = [&](const float* s, float2 off2, float2* sum, uint32_t* w) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float2 x = __ffma2_rn(make_float2(s[2 * e], s[2 * e + 1]), scale2, off2);
+          x.x = exp2_approx(x.x);
+          x.y = exp2_approx(x.y);
+          sum[e & 1] = __fadd2_rn(sum[e & 1], x);
+          w[e] = pack2<T>(x.x, x.y);
+        }
+      };
+      // A block that every row sees whole, on the guess that its scores do not outgrow the running maximum (which they
+      // rarely do after the first block): the weights then do not wait for the maximum, and the two are computed
+      // side by side.  False, with nothing changed, when the guess was wrong.
+      auto guess = [&]() {
+        float s[128];
+        read(s);
+        const bool over = mbar_test_wait(&b.pv_done[wg], (n - 1) & 1);
+        const float off = -m * scale;                // m = -inf: the guess is wrong, or every score is -inf
+        const float2 off2 = make_float2(off, off);
+        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        uint32_t w[32];
+        float mx[4] = {s[0], s[1], s[2], s[3]};
+#pragma unroll
+        for (int c = 4; c < 124; c += 8)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) mx[x] = max3(mx[x], s[c + x], s[c + 4 + x]);
+        const float high = max3(max3(mx[0], mx[1], mx[2]), max3(mx[3], s[124], s[125]), fmaxf(s[126], s[127]));
+        weigh(s, off2, sum, w);
+        weigh(s + 32, off2, sum, w + 16);
+        if (!warp_all(high <= m + slack && m > -INFINITY)) return false;
+        scores_read();
+        if (!warp_all(over)) ok = wait(&b.pv_done[wg], n - 1);
+        if (!ok) return true;
+        tc_fence_after();
+        tmem_st_32x16(tp, w);
+        tmem_st_32x16(tp + 16, w + 16);
+        weigh(s + 64, off2, sum, w);
+        stored(&b.p_half[wg]);
+        tmem_st_32x16(tp + 32, w);
+        weigh(s + 96, off2, sum, w + 16);
+        tmem_st_32x16(tp + 48, w + 16);
+        l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+        stored(&b.p_full[wg]);
+        return true;
+      };
+      // Any block.
+      auto block = [&](int kb, bool start) {
+        float s[128];
+        read(s);
+        scores_read();
+        if (p.scale_log2 < 0.f) {
+#pragma unroll
+          for (int c = 0; c < 128; ++c) s[c] = -s[c];
+        }
+        uint32_t hidden = 0;                         // quarters of the block that no row of the warp sees
+        const int j0 = kb * kTileK, sink = min(p.sinks, len);
+        auto below = [](int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; };
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const int j = j0 + 32 * c;
+          const uint32_t see = below(top + 1 - j) & (~below(low - j) | below(sink - j));
+          if (warp_all(see == 0)) {
+            hidden |= 1u << c;
+          } else if (!warp_all(see == 0xffffffffu)) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) s[32 * c + e] = see >> e & 1u ? s[32 * c + e] : -INFINITY;
+          }
+        }
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (!(hidden >> c & 1u)) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 8)
+#pragma unroll
+              for (int x = 0; x < 4; ++x) mx[x] = max3(mx[x], s[32 * c + e + x], s[32 * c + e + 4 + x]);
+          }
+        const float high = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
+        const bool grow = high > m + slack || (m == -INFINITY && high > m);
+        // the last product with these weights' columns, and into these outputs, is over
+        if (!start && !wait(&b.pv_done[wg], n - 1)) return false;
+        tc_fence_after();
+        if (__any_sync(0xffffffffu, grow)) {
+          const float mn = grow ? high : m;
+          const float shrink = !grow ? 1.f : m == -INFINITY ? 0.f : exp2_approx((m - mn) * scale);
+          m = mn;
+          l *= shrink;
+          if (!start) {
+#pragma unroll 1
+            for (int c = 0; c < DP; c += 8) tmem_scale_32x8(to + c, shrink);
+          }
+        }
+        const float off = m == -INFINITY ? 0.f : -m * scale;
+        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t w[16];
+          if (hidden >> c & 1u) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) w[e] = 0u;
+          } else {
+            weigh(s + 32 * c, make_float2(off, off), sum, w);
+          }
+          if (c == 2) stored(&b.p_half[wg]);
+          tmem_st_32x16(tp + 16 * c, w);
+        }
+        l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+        stored(&b.p_full[wg]);
+        return true;
+      };
+      for (int i = 0; i < blocks; ++i, ++n) {
+        const int kb = i < sinks ? i : lo + (i - sinks);
+        ok = wait(&b.s_full[wg], n);
+        if (!ok) break;
+        if (i > 0 && kb < whole_hi && (kb >= whole_lo || kb < whole_sinks) && p.scale_log2 >= 0.f && guess()) {
+          if (!ok) break;
+          continue;
+        }
+        ok = block(kb, i == 0);
+        if (!ok) break;
       }
       if (!ok) break;
       // output
-      if (!first) {
+      if (blocks > 0) {
         ok = wait(&b.pv_done[wg], n - 1);
         if (!ok) break;
         tc_fence_after();
       }
-      const bool none = first || l == 0.f;
+      const bool none = blocks == 0 || l == 0.f;
       const float r = none ? 0.f : 1.f / l;
-      T* out = reinterpret_cast<T*>(p.out.data + (int64_t)(it.sq.q0 + t.row + min(row, t.n - 1)) * p.out.row_bytes +
-                                    (int64_t)t.head * p.out.head_bytes);
-      float odd = 0.f;                               // NaN once a value is not finite
+      float2 odd = make_float2(0.f, 0.f);            // not finite once a value is not
 #pragma unroll
       for (int c = 0; c < DP; c += 32) {
         float o[32];
-        if (!first) {
+        if (blocks > 0) {
           tmem_ld_32x32(to + c, o);
           tmem_wait_ld_32(o);
         }
 #pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          o[e] = none ? 0.f : o[e] * r;
-          odd = fmaf(o[e], 0.f, odd);
-        }
-        if (row < t.n)
+        for (int e = 0; e < 32; ++e) o[e] = none ? 0.f : o[e] * r;
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) odd = __fadd2_rn(odd, make_float2(o[e], o[e + 1]));
+        if (row < rows)
 #pragma unroll
           for (int e = 0; e < 32; e += 8)
             if (c + e < p.dim) {
@@ -498,11 +660,11 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
               u.y = pack2<T>(o[e + 2], o[e + 3]);
               u.z = pack2<T>(o[e + 4], o[e + 5]);
               u.w = pack2<T>(o[e + 6], o[e + 7]);
-              *reinterpret_cast<uint4*>(out + c + e) = u;
+              *reinterpret_cast<uint4*>(out + (c + e) * 2) = u;
             }
       }
       tc_fence_before();
-      dirty = dirty || (row < t.n && odd != odd);
+      dirty = dirty || (row < rows && !(fabsf(odd.x + odd.y) < INFINITY));
     }
     // A weight of zero times a value that is not finite is NaN: rows that hold one are done again, key by visible
     // key.  After everything else, so that nothing waits for it.
@@ -516,6 +678,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         if (row < t.n) {
           const T* out = reinterpret_cast<const T*>(p.out.data + (int64_t)(it.sq.q0 + t.row + row) * p.out.row_bytes +
                                                     (int64_t)t.head * p.out.head_bytes);
+#pragma unroll 1
           for (int d = 0; d < p.dim; ++d) again = again || !(fabsf(to_f(out[d])) < INFINITY);
         }
         for (uint32_t rows = __ballot_sync(0xffffffffu, again); rows; rows &= rows - 1) {
@@ -523,6 +686,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
           const T* q = reinterpret_cast<const T*>(p.q.data + (int64_t)(it.sq.q0 + i) * p.q.row_bytes +
                                                   (int64_t)t.head * p.q.head_bytes);
           __syncwarp();
+#pragma unroll 1
           for (int d = lane; d < p.dim; d += 32) qs[d] = to_f(q[d]);
           __syncwarp();
           attend_row<T>(p, it.sq, i, t.head, qs);
@@ -533,7 +697,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == 8) tmem_dealloc(tmem, 512);
+  if (warp == kMmaWarp) tmem_dealloc(tmem, 512);
 }
 
 }  // namespace gnn
