@@ -132,6 +132,7 @@ struct AttendItem {
 };
 struct AttendGrid {
   int pair_heads;                    // the two tiles: the same rows of two heads, or 256 rows of one
+  int single;                        // one tile to an item: few items, which then spread over more SMs
   int rows;                          // queries of an item: 128 or 256
   int heads;                         // items side by side: heads or pairs of heads
   int64_t items;
@@ -177,7 +178,8 @@ __device__ __noinline__ bool attend_item(const AttendParams& p, const AttendGrid
   const int head = g.pair_heads ? 2 * h : h;
   it.kv_head = head / (p.heads / p.kv_heads);
   it.t[0] = attend_tile(p, it.sq, (int)row, head);
-  it.t[1] = g.pair_heads ? attend_tile(p, it.sq, (int)row, head + 1) : attend_tile(p, it.sq, (int)row + kTileQ, head);
+  it.t[1] = g.pair_heads ? attend_tile(p, it.sq, (int)row, head + 1)
+                         : attend_tile(p, it.sq, g.single ? it.sq.nq : (int)row + kTileQ, head);
   int lo = INT_MAX, hi = 0;
   it.sinks = 0;
 #pragma unroll
@@ -479,7 +481,9 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
       const int rows = item.t[wg].n, len = item.sq.len, item_n = item.n;
       const int sinks = item.t[wg].sinks, lo = item.t[wg].lo, blocks = sinks + (item.t[wg].hi - lo);
       const int whole_sinks = item.t[wg].whole_sinks, whole_lo = item.t[wg].whole_lo, whole_hi = item.t[wg].whole_hi;
-      const int top = row >= rows ? -1 : min(len - 1, item.t[wg].top + row), low = max(0, item.t[wg].low + row);
+      // the row's keys, and the warp's: of its first row, and of its last that the tile has
+      const int tile_top = item.t[wg].top, tile_low = item.t[wg].low, w0 = (warp & 3) * 32, w1 = min(rows, w0 + 32) - 1;
+      const int top = min(len - 1, tile_top + row), low = max(0, tile_low + row);
       char* out = p.out.data + (int64_t)(item.sq.q0 + item.t[wg].row + row) * p.out.row_bytes +
                   (int64_t)item.t[wg].head * p.out.head_bytes;
       __syncwarp();
@@ -487,7 +491,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
       ++items;
       if (item_n < 0) break;
       if (rows == 0) continue;
-      float m = -INFINITY, l = 0.f;
+      float m = row < rows ? -INFINITY : INFINITY, l = 0.f;        // rows that the tile does not have weigh nothing
       const float2 scale2 = make_float2(scale, scale);
       auto read = [&](float* s) {                    // the block's scores
         tc_fence_after();
@@ -565,14 +569,15 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         }
         uint32_t hidden = 0;                         // quarters of the block that no row of the warp sees
         const int j0 = kb * kTileK, sink = min(p.sinks, len);
-        auto below = [](int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; };
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           const int j = j0 + 32 * c;
-          const uint32_t see = below(top + 1 - j) & (~below(low - j) | below(sink - j));
-          if (warp_all(see == 0)) {
+          const int first_top = min(len - 1, tile_top + w0), last_top = min(len - 1, tile_top + w1);
+          if (w1 < w0 || j > last_top || (j + 31 < tile_low + w0 && j >= sink)) {
             hidden |= 1u << c;
-          } else if (!warp_all(see == 0xffffffffu)) {
+          } else if (j + 31 > first_top || (j < tile_low + w1 && j + 32 > sink)) {
+            auto below = [](int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; };
+            const uint32_t see = below(top + 1 - j) & (~below(low - j) | below(sink - j));
 #pragma unroll
             for (int e = 0; e < 32; ++e) s[32 * c + e] = see >> e & 1u ? s[32 * c + e] : -INFINITY;
           }
