@@ -53,8 +53,6 @@ HeadsView view(const gnn_heads& h, int dtype) {
   return {static_cast<char*>(h.data), h.row_stride * e, h.head_stride * e};
 }
 
-// The most pairs a unit may have (8, 4 or 1) for head_dim, rot_dim and how the views lie.  A thread's accesses are
-// of `wide` pairs' elements: 16 bytes at most, as wide as every address allows.
 bool lies_on(const HeadsView& v, int64_t bytes) {
   return (uintptr_t)v.data % bytes == 0 && v.row_bytes % bytes == 0 && v.head_bytes % bytes == 0;
 }
@@ -89,10 +87,11 @@ int run_rotary(const gnn_rotary* rot, int dtype, int head_dim, RotaryParams& p, 
   std::memcpy(p.lo, rot->turn_lo, sizeof p.lo);
   const bool inter = rot->layout == GNN_ROTARY_INTERLEAVED;
   const int e = elem_bytes(dtype);
+  // the most pairs to a unit (8 in 16-bit types, 4, 2 or 1) that head_dim, rot_dim and how the views lie allow
   int V = dtype == GNN_DTYPE_FP32 ? 4 : 8;
-  for (;; V = V == 8 ? 4 : 1) {
-    bool ok = V == 1 || (head_dim % (2 * V) == 0 && p.rot % (2 * V) == 0);
-    for (int i = 0; i < 3 && V > 1; ++i)
+  for (; V > 1; V /= 2) {
+    bool ok = head_dim % (2 * V) == 0 && p.rot % (2 * V) == 0;
+    for (int i = 0; i < 3; ++i)
       if (p.heads[i]) ok = ok && lies_on(p.in[i], V * e) && lies_on(p.out[i], V * e);
     if (ok) break;
   }
@@ -101,23 +100,30 @@ int run_rotary(const gnn_rotary* rot, int dtype, int head_dim, RotaryParams& p, 
   while (p.group < p.units && p.group < 32) p.group *= 2;
   const int sms = device_sms();
   if (!sms) return cuda_fail(cudaGetLastError());
-  // As many heads to a group as leave the SMs their threads: a token's cosines are then computed once.
-  const int heads = p.heads[0] + p.heads[1] + p.heads[2];
-  const int64_t lanes = n_rows * heads * p.group, room = (int64_t)sms * 1024;
-  p.chunk = (int)std::min<int64_t>(heads, std::max<int64_t>(1, lanes / room));
-  p.chunks = (heads + p.chunk - 1) / p.chunk;
-  const int64_t blocks = (n_rows * p.chunks * p.group + kRotThreads - 1) / kRotThreads;
-  const unsigned grid = (unsigned)std::min<int64_t>(blocks, (int64_t)sms * 8);
+  // Blocks for one round of all tasks (two heads of a token), six to an SM at most, shared out by heads.
+  const int heads = p.heads[0] + p.heads[1] + p.heads[2], per_block = kRotThreads / p.group;
+  unsigned grid = 0;
+  for (int i = 0; i < 3; ++i) {
+    p.block0[i] = grid;
+    if (!p.heads[i]) continue;
+    const int64_t blocks = (n_rows * ((p.heads[i] + 1) / 2) + per_block - 1) / per_block;
+    grid += (unsigned)std::min<int64_t>(blocks, std::max<int64_t>(1, (int64_t)sms * 6 * p.heads[i] / heads));
+  }
+  p.block0[3] = grid;
   cudaError_t err;
   if (dtype == GNN_DTYPE_FP32)
-    err = V == 4 ? launch_rotary<float, 4>(p, inter, norm, grid, st) : launch_rotary<float, 1>(p, inter, norm, grid, st);
+    err = V == 4   ? launch_rotary<float, 4>(p, inter, norm, grid, st)
+          : V == 2 ? launch_rotary<float, 2>(p, inter, norm, grid, st)
+                   : launch_rotary<float, 1>(p, inter, norm, grid, st);
   else if (dtype == GNN_DTYPE_BF16)
     err = V == 8   ? launch_rotary<__nv_bfloat16, 8>(p, inter, norm, grid, st)
           : V == 4 ? launch_rotary<__nv_bfloat16, 4>(p, inter, norm, grid, st)
+          : V == 2 ? launch_rotary<__nv_bfloat16, 2>(p, inter, norm, grid, st)
                    : launch_rotary<__nv_bfloat16, 1>(p, inter, norm, grid, st);
   else
     err = V == 8   ? launch_rotary<__half, 8>(p, inter, norm, grid, st)
           : V == 4 ? launch_rotary<__half, 4>(p, inter, norm, grid, st)
+          : V == 2 ? launch_rotary<__half, 2>(p, inter, norm, grid, st)
                    : launch_rotary<__half, 1>(p, inter, norm, grid, st);
   return err == cudaSuccess ? GNN_OK : cuda_fail(err);
 }
