@@ -1,28 +1,34 @@
 // Attention of few queries over many keys: new tokens over a cache.
 //
-// The query heads that share a key head are the 16 rows of an mma.sync tile (row r: query r / G, head r % G of
-// the group), and the keys that any of them sees are split over blocks and, 16 at a time, over a block's warps.
-// Each warp keeps its own running maximum, sum and output; a block joins its warps', and the last block of a row
-// tile to finish joins the blocks', in order.
+// The query heads that share a key head are rows (row r: query r / G, head r % G of the group), 8 or 16 to a tile of
+// mma.sync, with the keys along M and the rows along N: S^T = K Q^T, O^T = V^T P^T.  Each warp keeps its own running
+// maximum, sum and output over 16 keys at a time; a block joins its warps', and where a row tile's keys are
+// split over blocks, the last of them to finish joins the blocks', in order.
 //
-// Bound by HBM: keys and values are read once, straight into the registers of the products.  A lane's 16 bytes
-// of a key are the k-indices it feeds, in an order that the queries follow; its 16 bytes of a value are eight
-// columns, pairs of keys being put together by byte permutes.  (tcgen05 would need 128 rows where there are
-// 16 at most, and the copy through shared memory.)
+// Bound by HBM: keys and values are read once, straight into the registers of the products.  A lane's 16 bytes of a key
+// are the k-indices it feeds, in an order that the queries follow; its 16 bytes of a value are eight columns, pairs
+// of keys being put together by byte permutes, and the weights turned over by movmatrix.  The next keys are loaded
+// before the softmax and the next values behind the products.  (tcgen05 would need 128 rows where there are 16 at
+// most, and the way through shared memory.)
+//
+// The work is split by what there is: every block sums up the sequences' lengths and takes an equal share of
+// all units of 64 keys, so that sequences of different lengths leave no SM idle.
 #pragma once
 #include "attend_tile.cuh"
 
 namespace gnn {
 
-constexpr int kFewWarps = 4, kFewRows = 16, kFewStep = 16 * kFewWarps;   // keys that a block takes at a time
+constexpr int kFewWarps = 4, kFewUnit = 16 * kFewWarps;      // keys that a block takes at a time
+constexpr int kFewSeqs = 1024;       // sequences whose lengths a block sums up; with more, blocks take whole row tiles
+constexpr int kFewRows = 16;         // rows of a tile, at most
 
 struct FewGrid {
   int group;                         // query heads to a key head
   int max_q;                         // queries of a sequence, at most
-  int row_tiles, splits;             // of 16 rows; blocks along the keys, at most
-  int chunk;                         // keys of a block, at least
-  float* parts;                      // [item][16][dim + 2]: outputs, maximum, sum
-  int* tickets;                      // per row tile, zero between calls
+  int row_tiles;
+  int least;                         // units that a block takes, at least
+  float* parts;                      // [block][2]: a tile's outputs [rows][dim], maxima [rows] and sums [rows]
+  int* tickets;                      // [block], zero between calls: of the tile that starts in the block and goes on
 };
 
 __device__ __forceinline__ void mma_16x8x16(float* d, const uint32_t* a, uint32_t b0, uint32_t b1, __nv_bfloat16) {
@@ -35,266 +41,398 @@ __device__ __forceinline__ void mma_16x8x16(float* d, const uint32_t* a, uint32_
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// 8 x 8 words of 16 bits, lane 4 r + c holding row r's columns 2c and 2c + 1, turned over.
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t a) {
+  uint32_t d;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  return d;
+}
 __device__ __forceinline__ uint4 load_once(const char* p) {
   uint4 v;
   asm volatile("ld.global.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];"
                : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
   return v;
 }
+__device__ __forceinline__ uint32_t word(const uint4& x, int i) { return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w; }
 
-// NC: 16-byte pieces of a key that a lane takes, a quarter of those of head_dim up to 32 NC.
-template <typename T, int NC>
-__global__ void __launch_bounds__(32 * kFewWarps, NC > 2 ? 3 : 4)
+// Keys that some query of the sequence sees: [0, first) and [lo, lo + n - first).
+struct FewKeys { int first, lo, n; };
+__device__ __forceinline__ FewKeys few_keys(const AttendParams& p, const Sequence& sq) {
+  const Seen a = seen_keys(sq.len - sq.nq, sq.len, p.left, p.right, p.sinks);
+  const Seen z = seen_keys(sq.len - 1, sq.len, p.left, p.right, p.sinks);
+  FewKeys k;
+  k.lo = min(a.lo, z.hi);
+  k.first = min(p.sinks, k.lo);
+  k.n = k.first + z.hi - k.lo;
+  return k;
+}
+__device__ __forceinline__ int few_units(const AttendParams& p, const Sequence& sq) {
+  return sq.nq == 0 ? 0 : max(1, (int)(((int64_t)few_keys(p, sq).n + kFewUnit - 1) / kFewUnit));
+}
+
+// NC: 16-byte pieces of a key that a lane takes, a quarter of those of head_dim up to 32 NC.  NR: rows of a tile / 8.
+template <typename T, int NC, int NR>
+__global__ void __launch_bounds__(32 * kFewWarps, NR == 2 && NC > 2 ? 2 : 3)
     attend_few_kernel(const __grid_constant__ AttendParams p, const __grid_constant__ FewGrid f) {
-  constexpr int NV = (NC + 1) / 2, DS = NV * 64 + 4;       // pieces of a value to a lane; a row in shared memory
-  __shared__ float o_s[kFewWarps][kFewRows][DS];
-  __shared__ float m_s[kFewWarps][kFewRows], l_s[kFewWarps][kFewRows];
+  constexpr int NV = (NC + 1) / 2, DS = NV * 64 + 4, ROWS = 8 * NR;   // pieces of a value to a lane; a row in shared memory
+  __shared__ __align__(16) float o_s[kFewWarps][ROWS][DS];
+  __shared__ float m_s[kFewWarps][ROWS], l_s[kFewWarps][ROWS], sum_s[ROWS];
+  __shared__ int pre[kFewSeqs + 1], scan_s[kFewWarps];
   __shared__ int last_s;
-  pdl_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int split = blockIdx.x % f.splits, tile = blockIdx.x / f.splits;   // tile: sequence, key head, row tile
-  const int rt = tile % f.row_tiles, at = tile / f.row_tiles, kv = at % p.kv_heads, b = at / p.kv_heads;
-  bool bad;
-  const Sequence sq = sequence(p, b, &bad);
-  if ((bad || sq.nq > f.max_q) && threadIdx.x == 0) atomicOr(p.err, DEV_ERR_INDEX_RANGE);
-  const int G = f.group, rows = min(min(sq.nq, f.max_q) * G - rt * kFewRows, kFewRows);
-  if (rows <= 0) return;
-  const int q_first = rt * kFewRows / G, q_last = (rt * kFewRows + rows - 1) / G;
-  // keys that some row sees: [0, first) and [lo, hi)
-  const int pos0 = sq.len - sq.nq;
-  const Seen sa = seen_keys(pos0 + q_first, sq.len, p.left, p.right, p.sinks);
-  const Seen sz = seen_keys(pos0 + q_last, sq.len, p.left, p.right, p.sinks);
-  const int hi = sz.hi, lo = min(sa.lo, hi), first = min(p.sinks, lo), n = first + hi - lo;
-  const int per = (n + f.splits - 1) / f.splits;
-  const int chunk = max(f.chunk, (per + kFewStep - 1) / kFewStep * kFewStep);
-  const int parts = max(1, (n + chunk - 1) / chunk);
-  if (split >= parts) return;
-  const int c_end = min(n, (split + 1) * chunk);
+  const int KR = p.kv_heads * f.row_tiles, G = f.group;
+  const float scale = fabsf(p.scale_log2), slack = 8.f / scale;       // as in the tiled kernel
+  const bool balanced = p.n_seqs <= kFewSeqs;
+  pdl_wait();
 
-  // queries: rows g and g + 8, the pieces 8 (t + 4 c) .. + 7 of a head
-  uint32_t q[NC][2][4];
-  int row_pos[2];
+  // units before each sequence
+  int64_t share = 1;
+  if (balanced) {
+    int before = 0;
+    for (int b0 = 0; b0 < p.n_seqs; b0 += 32 * kFewWarps) {
+      const int b = b0 + threadIdx.x;
+      int u = 0;
+      if (b < p.n_seqs) {
+        bool bad;
+        const Sequence sq = sequence(p, b, &bad);
+        if ((bad || sq.nq > f.max_q) && blockIdx.x == 0) atomicOr(p.err, DEV_ERR_INDEX_RANGE);
+        u = few_units(p, sq);
+      }
+      int x = u;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int r = rt * kFewRows + g + 8 * h, i = r / G, head = kv * G + r % G;
-    const bool have = g + 8 * h < rows;
-    row_pos[h] = have ? pos0 + i : INT_MIN;
-    const char* src = p.q.data + (int64_t)(sq.q0 + i) * p.q.row_bytes + (int64_t)head * p.q.head_bytes;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      uint4 v = make_uint4(0, 0, 0, 0);
-      if (have && 8 * (t + 4 * c) < p.dim) v = *reinterpret_cast<const uint4*>(src + 16 * (t + 4 * c));
-      q[c][h][0] = v.x; q[c][h][1] = v.y; q[c][h][2] = v.z; q[c][h][3] = v.w;
+      for (int d = 1; d < 32; d *= 2) {
+        const int y = __shfl_up_sync(0xffffffffu, x, d);
+        if (lane >= d) x += y;
+      }
+      if (lane == 31) scan_s[warp] = x;
+      __syncthreads();
+      int sums = before;
+      for (int w = 0; w < kFewWarps; ++w) {
+        if (w < warp) x += scan_s[w];
+        sums += scan_s[w];
+      }
+      if (b < p.n_seqs) pre[b] = before + x - u;
+      before = sums;
+      __syncthreads();
     }
+    if (threadIdx.x == 0) pre[p.n_seqs] = before;
+    __syncthreads();
+    share = max((int64_t)f.least, ((int64_t)before * KR + gridDim.x - 1) / gridDim.x);
   }
-  const char* kp = p.k.data + (int64_t)sq.k0 * p.k.row_bytes + (int64_t)kv * p.k.head_bytes;
-  const char* vp = p.v.data + (int64_t)sq.k0 * p.v.row_bytes + (int64_t)kv * p.v.head_bytes;
-  auto key_at = [&](int c) { return c < first ? c : lo + (c - first); };
-  uint4 k[2][NC], v[4][NV];
-  auto load_k = [&](int c0) {                              // keys g and g + 8 of the 16
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int c = c0 + g + 8 * h;
-      const char* src = kp + (int64_t)key_at(c) * p.k.row_bytes;
-#pragma unroll
-      for (int e = 0; e < NC; ++e) {
-        k[h][e] = make_uint4(0, 0, 0, 0);
-        if (c < c_end && 8 * (t + 4 * e) < p.dim) k[h][e] = load_once(src + 16 * (t + 4 * e));
-      }
-    }
-  };
-  auto load_v = [&](int c0) {                              // keys 2t, 2t + 1, 2t + 8, 2t + 9, pieces g + 8 e
-#pragma unroll
-    for (int h = 0; h < 4; ++h) {
-      const int c = c0 + 2 * t + (h & 1) + 8 * (h >> 1);
-      const char* src = vp + (int64_t)key_at(c) * p.v.row_bytes;
-#pragma unroll
-      for (int e = 0; e < NV; ++e) {
-        v[h][e] = make_uint4(0, 0, 0, 0);
-        if (c < c_end && 8 * (g + 8 * e) < p.dim) v[h][e] = load_once(src + 16 * (g + 8 * e));
-      }
-    }
-  };
-  float o[NV][8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-#pragma unroll
-  for (int e = 0; e < NV; ++e)
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) o[e][i][x] = 0.f;
 
-  int c0 = split * chunk + warp * 16;
-  if (c0 < c_end) {
-    load_k(c0);
-    load_v(c0);
-  }
-  for (; c0 < c_end; c0 += kFewStep) {
-    float s[2][4];
+  // Units [v0, v1) of the `units` of row tile kr of sequence b; u0: the tile's first unit among all.
+  auto process = [&](int b, int kr, int v0, int v1, int units, int64_t u0) {
+    bool bad;
+    const Sequence sq = sequence(p, b, &bad);
+    if (!balanced && (bad || sq.nq > f.max_q) && threadIdx.x == 0) atomicOr(p.err, DEV_ERR_INDEX_RANGE);
+    const int rt = kr % f.row_tiles, kv = kr / f.row_tiles, row0 = rt * ROWS;
+    const int rows = min(min(sq.nq, f.max_q) * G - row0, ROWS);
+    if (rows <= 0) return;
+    const FewKeys keys = few_keys(p, sq);
+    const int pos0 = sq.len - sq.nq, pos_first = pos0 + row0 / G, pos_last = pos0 + (row0 + rows - 1) / G;
+    // queries as the second operand: row g of each eight, pieces t + 4 c
+    uint4 q[NR][NC];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-#pragma unroll
-      for (int x = 0; x < 4; ++x) s[h][x] = 0.f;
+    for (int r = 0; r < NR; ++r) {
+      const int row = row0 + 8 * r + g;
+      const bool have = 8 * r + g < rows;
+      const char* src = p.q.data + (int64_t)(sq.q0 + row / G) * p.q.row_bytes + (int64_t)(kv * G + row % G) * p.q.head_bytes;
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        const uint32_t a0[4] = {q[c][0][0], q[c][1][0], q[c][0][1], q[c][1][1]};
-        const uint32_t a1[4] = {q[c][0][2], q[c][1][2], q[c][0][3], q[c][1][3]};
-        mma_16x8x16(s[h], a0, k[h][c].x, k[h][c].y, T());
-        mma_16x8x16(s[h], a1, k[h][c].z, k[h][c].w, T());
+        q[r][c] = make_uint4(0, 0, 0, 0);
+        if (have && 8 * (t + 4 * c) < p.dim) q[r][c] = *reinterpret_cast<const uint4*>(src + 16 * (t + 4 * c));
+        if (p.scale_log2 < 0.f) {
+          q[r][c].x ^= 0x80008000u; q[r][c].y ^= 0x80008000u; q[r][c].z ^= 0x80008000u; q[r][c].w ^= 0x80008000u;
+        }
       }
     }
-    if (c0 + kFewStep < c_end) load_k(c0 + kFewStep);
-    // s[h][x]: row g + 8 (x / 2), key 8 h + 2 t + x % 2
-    float top[2] = {-INFINITY, -INFINITY};
+    float o[NV][4][NR][4], m[NR][2], l[NR][2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const int c = c0 + 8 * h + 2 * t + (x & 1), j = key_at(c);
-        const int64_t pos = row_pos[x >> 1];
-        const bool see = c < c_end && row_pos[x >> 1] != INT_MIN && (p.right < 0 || j <= pos + p.right) &&
-                         (p.left < 0 || j >= pos - p.left || j < p.sinks);
-        s[h][x] = see ? s[h][x] * p.scale_log2 : -INFINITY;
-        top[x >> 1] = fmaxf(top[x >> 1], s[h][x]);
-      }
-    float shrink[2], ref[2];
-    bool grow = false;
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
-      top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
-      const float mn = fmaxf(m[r], top[r]);
-      grow = grow || mn > m[r];
-      ref[r] = mn == -INFINITY ? 0.f : mn;
-      shrink[r] = exp2_approx(m[r] - ref[r]);
-      m[r] = mn;
-    }
-    if (__any_sync(0xffffffffu, grow)) {
-#pragma unroll
-      for (int r = 0; r < 2; ++r) l[r] *= shrink[r];
+    for (int r = 0; r < NR; ++r) {
+      m[r][0] = m[r][1] = -INFINITY;
+      l[r][0] = l[r][1] = 0.f;
 #pragma unroll
       for (int e = 0; e < NV; ++e)
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int x = 0; x < 4; ++x) o[e][i][x] *= shrink[x >> 1];
+          for (int x = 0; x < 4; ++x) o[e][i][r][x] = 0.f;
     }
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        s[h][x] = exp2_approx(s[h][x] - ref[x >> 1]);
-        l[x >> 1] += s[h][x];
-      }
-    const uint32_t a[4] = {pack2<T>(s[0][0], s[0][1]), pack2<T>(s[0][2], s[0][3]), pack2<T>(s[1][0], s[1][1]),
-                           pack2<T>(s[1][2], s[1][3])};
-#pragma unroll
-    for (int e = 0; e < NV; ++e) {
-      auto word = [](const uint4& x, int i) { return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w; };
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {                        // column i of every lane's piece
-        const uint32_t pick = i & 1 ? 0x7632u : 0x5410u;
-        const uint32_t b0 = __byte_perm(word(v[0][e], i / 2), word(v[1][e], i / 2), pick);
-        const uint32_t b1 = __byte_perm(word(v[2][e], i / 2), word(v[3][e], i / 2), pick);
-        mma_16x8x16(o[e][i], a, b0, b1, T());
-      }
-    }
-    if (c0 + kFewStep < c_end) load_v(c0 + kFewStep);
-  }
+    // keys below full_hi and from full_lo on, or below the sinks, are seen by every row
+    const int full_hi = p.right < 0 ? INT_MAX : (int)min((int64_t)INT_MAX, (int64_t)pos_first + p.right + 1);
+    const int full_lo = p.left < 0 ? INT_MIN : (int)max((int64_t)INT_MIN, (int64_t)pos_last - p.left);
 
-  // the warps' results to shared memory: row g + 8 r, element 8 (2 t + x + 8 e) + i
+#pragma unroll 1
+    for (int part = 0; part < 2; ++part) {           // the sinks, the window
+      const int c0 = v0 * kFewUnit, c1 = min(keys.n, v1 * kFewUnit);
+      const int jb = part ? keys.lo + max(c0, keys.first) - keys.first : c0;
+      const int je = part ? keys.lo + c1 - keys.first : min(c1, keys.first);
+      int j = jb + 16 * warp;
+      if (j >= je) continue;
+      const char* kp = p.k.data + (int64_t)(sq.k0 + j + g) * p.k.row_bytes + (int64_t)kv * p.k.head_bytes + 16 * t;
+      const char* vp = p.v.data + (int64_t)(sq.k0 + j + 2 * t) * p.v.row_bytes + (int64_t)kv * p.v.head_bytes + 16 * g;
+      uint4 k[2][NC], v[4][NV];
+      auto load_k = [&](int at) {                    // keys g and g + 8 of the 16
 #pragma unroll
-  for (int r = 0; r < 2; ++r) {
-    l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
-    l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
-    if (t == 0) {
-      m_s[warp][g + 8 * r] = m[r];
-      l_s[warp][g + 8 * r] = l[r];
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < NC; ++e) {
+            k[h][e] = make_uint4(0, 0, 0, 0);
+            if (at + g + 8 * h < je && 8 * (t + 4 * e) < p.dim) k[h][e] = load_once(kp + 8 * h * p.k.row_bytes + 64 * e);
+          }
+      };
+      auto load_v = [&](int at) {                    // keys 2t, 2t + 1, 2t + 8, 2t + 9
+#pragma unroll
+        for (int h = 0; h < 4; ++h)
+#pragma unroll
+          for (int e = 0; e < NV; ++e) {
+            const int key = (h & 1) + 8 * (h >> 1);
+            v[h][e] = make_uint4(0, 0, 0, 0);
+            if (at + 2 * t + key < je && 8 * (g + 8 * e) < p.dim) v[h][e] = load_once(vp + key * p.v.row_bytes + 128 * e);
+          }
+      };
+      load_k(j);
+      load_v(j);
+      for (;;) {
+        float s[NR][4];                              // keys g (0, 1) and g + 8 (2, 3), rows 2t and 2t + 1 of each eight
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) s[r][x] = 0.f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const uint32_t a0[4] = {k[0][c].x, k[1][c].x, k[0][c].y, k[1][c].y};
+          const uint32_t a1[4] = {k[0][c].z, k[1][c].z, k[0][c].w, k[1][c].w};
+#pragma unroll
+          for (int r = 0; r < NR; ++r) {
+            mma_16x8x16(s[r], a0, q[r][c].x, q[r][c].y, T());
+            mma_16x8x16(s[r], a1, q[r][c].z, q[r][c].w, T());
+          }
+        }
+        const bool more = j + kFewUnit < je;
+        kp += (int64_t)kFewUnit * p.k.row_bytes;
+        if (more) load_k(j + kFewUnit);
+        if (j + 16 > je || j + 16 > full_hi || (j < full_lo && j + 16 > p.sinks)) {
+#pragma unroll
+          for (int r = 0; r < NR; ++r)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const int key = j + g + 8 * (x >> 1);
+              const int64_t pos = (int64_t)pos0 + (row0 + 8 * r + 2 * t + (x & 1)) / G;
+              const bool see = key < je && (p.right < 0 || key <= pos + p.right) &&
+                               (p.left < 0 || key >= pos - p.left || key < p.sinks);
+              s[r][x] = see ? s[r][x] : -INFINITY;
+            }
+        }
+        float high[NR][2];
+        bool grow = false;
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            float h = fmaxf(s[r][x], s[r][x + 2]);
+            h = fmaxf(h, __shfl_xor_sync(0xffffffffu, h, 4));
+            h = fmaxf(h, __shfl_xor_sync(0xffffffffu, h, 8));
+            high[r][x] = fmaxf(h, __shfl_xor_sync(0xffffffffu, h, 16));
+            grow = grow || high[r][x] > m[r][x] + slack || (m[r][x] == -INFINITY && high[r][x] > m[r][x]);
+          }
+        if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+          for (int r = 0; r < NR; ++r)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const float mn = fmaxf(m[r][x], high[r][x]);
+              const float shrink = m[r][x] == -INFINITY ? 0.f : exp2_approx((m[r][x] - mn) * scale);
+              m[r][x] = mn;
+              l[r][x] *= shrink;
+#pragma unroll
+              for (int e = 0; e < NV; ++e)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  o[e][i][r][x] *= shrink;
+                  o[e][i][r][x + 2] *= shrink;
+                }
+            }
+        }
+        uint32_t w[NR][2];
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const float off = m[r][x & 1] == -INFINITY ? 0.f : -m[r][x & 1] * scale;
+            s[r][x] = exp2_approx(fmaf(s[r][x], scale, off));
+            l[r][x & 1] += s[r][x];
+          }
+          w[r][0] = transpose_8x8(pack2<T>(s[r][0], s[r][1]));
+          w[r][1] = transpose_8x8(pack2<T>(s[r][2], s[r][3]));
+        }
+#pragma unroll
+        for (int e = 0; e < NV; ++e)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {              // columns 2i and 2i + 1 of every lane's piece
+            const uint32_t a[4] = {
+                __byte_perm(word(v[0][e], i), word(v[1][e], i), 0x5410), __byte_perm(word(v[0][e], i), word(v[1][e], i), 0x7632),
+                __byte_perm(word(v[2][e], i), word(v[3][e], i), 0x5410), __byte_perm(word(v[2][e], i), word(v[3][e], i), 0x7632)};
+#pragma unroll
+            for (int r = 0; r < NR; ++r) mma_16x8x16(o[e][i][r], a, w[r][0], w[r][1], T());
+          }
+        vp += (int64_t)kFewUnit * p.v.row_bytes;
+        if (!more) break;
+        load_v(j + kFewUnit);
+        j += kFewUnit;
+      }
     }
+
+    // the warps' results to shared memory: row 8 r + 2 t + x, element 8 (g + 8 e) + 2 i + y
+    __syncthreads();
 #pragma unroll
-    for (int e = 0; e < NV; ++e)
+    for (int r = 0; r < NR; ++r)
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        float* dst = &o_s[warp][g + 8 * r][8 * (2 * t + x + 8 * e)];
+        const int row = 8 * r + 2 * t + x;
 #pragma unroll
-        for (int i = 0; i < 8; i += 4)
-          *reinterpret_cast<float4*>(dst + i) =
-              make_float4(o[e][i][2 * r + x], o[e][i + 1][2 * r + x], o[e][i + 2][2 * r + x], o[e][i + 3][2 * r + x]);
+        for (int d = 4; d < 32; d *= 2) l[r][x] += __shfl_xor_sync(0xffffffffu, l[r][x], d);
+        if (g == 0) {
+          m_s[warp][row] = m[r][x];
+          l_s[warp][row] = l[r][x];
+        }
+#pragma unroll
+        for (int e = 0; e < NV; ++e) {
+          float* dst = &o_s[warp][row][8 * (g + 8 * e)];
+          *reinterpret_cast<float4*>(dst) = make_float4(o[e][0][r][x], o[e][0][r][x + 2], o[e][1][r][x], o[e][1][r][x + 2]);
+          *reinterpret_cast<float4*>(dst + 4) = make_float4(o[e][2][r][x], o[e][2][r][x + 2], o[e][3][r][x], o[e][3][r][x + 2]);
+        }
       }
-  }
-  __syncthreads();
-  const int width = p.dim + 2;
-  float* mine = f.parts + (int64_t)blockIdx.x * kFewRows * width;
-  auto store = [&](int r, int d, float sum, float val) {
-    T* out = reinterpret_cast<T*>(p.out.data + (int64_t)(sq.q0 + (rt * kFewRows + r) / G) * p.out.row_bytes +
-                                  (int64_t)(kv * G + (rt * kFewRows + r) % G) * p.out.head_bytes);
-    out[d] = from_f<T>(sum == 0.f ? 0.f : val / sum);
-  };
-  for (int x = threadIdx.x; x < rows * p.dim; x += 32 * kFewWarps) {
-    const int r = x / p.dim, d = x - r * p.dim;
-    float top = m_s[0][r];
-#pragma unroll
-    for (int w = 1; w < kFewWarps; ++w) top = fmaxf(top, m_s[w][r]);
-    const float ref = top == -INFINITY ? 0.f : top;
-    float sum = 0.f, val = 0.f;
-#pragma unroll
-    for (int w = 0; w < kFewWarps; ++w) {
-      const float z = exp2_approx(m_s[w][r] - ref);
-      sum = fmaf(l_s[w][r], z, sum);
-      val = fmaf(o_s[w][r][d], z, val);
-    }
-    if (parts == 1) {
-      store(r, d, sum, val);
-    } else {
-      mine[r * width + d] = val;
-      if (d == 0) {
-        mine[r * width + p.dim] = top;
-        mine[r * width + p.dim + 1] = sum;
-      }
-    }
-  }
-  if (parts > 1) {
-    __threadfence();
     __syncthreads();
-    if (threadIdx.x == 0) last_s = atomicAdd(&f.tickets[tile], 1) == parts - 1;
-    __syncthreads();
-    if (!last_s) return;
-    __threadfence();
-    if (threadIdx.x == 0) f.tickets[tile] = 0;
-    const float* all = f.parts + (int64_t)tile * f.splits * kFewRows * width;
-    const int64_t step = (int64_t)kFewRows * width;
-    for (int x = threadIdx.x; x < rows * p.dim; x += 32 * kFewWarps) {
-      const int r = x / p.dim, d = x - r * p.dim;
-      const float* at_r = all + r * width;
-      float top = -INFINITY;
-      for (int i = 0; i < parts; ++i) top = fmaxf(top, __ldcg(at_r + i * step + p.dim));
+    const bool whole = v0 == 0 && v1 == units;
+    const int64_t size = (int64_t)ROWS * (p.dim + 2);
+    float* mine = f.parts + ((int64_t)blockIdx.x * 2 + ((int64_t)blockIdx.x * share >= u0 ? 0 : 1)) * size;
+    auto store = [&](int r, int d, float sum, float4 val) {
+      char* out = p.out.data + (int64_t)(sq.q0 + (row0 + r) / G) * p.out.row_bytes +
+                  (int64_t)(kv * G + (row0 + r) % G) * p.out.head_bytes;
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      if (sum == 0.f) val = make_float4(0.f, 0.f, 0.f, 0.f);
+      *reinterpret_cast<uint2*>(out + 2 * d) = make_uint2(pack2<T>(val.x * inv, val.y * inv), pack2<T>(val.z * inv, val.w * inv));
+    };
+    const int quads = p.dim / 4;
+    for (int x = threadIdx.x; x < rows * quads; x += 32 * kFewWarps) {
+      const int r = x / quads, d = 4 * (x - r * quads);
+      float top = m_s[0][r];
+#pragma unroll
+      for (int w = 1; w < kFewWarps; ++w) top = fmaxf(top, m_s[w][r]);
       const float ref = top == -INFINITY ? 0.f : top;
-      float sum = 0.f, val = 0.f;
-      for (int i = 0; i < parts; ++i) {
-        const float z = exp2_approx(__ldcg(at_r + i * step + p.dim) - ref);
-        sum = fmaf(__ldcg(at_r + i * step + p.dim + 1), z, sum);
-        val = fmaf(__ldcg(at_r + i * step + d), z, val);
+      float sum = 0.f;
+      float4 val = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kFewWarps; ++w) {
+        const float z = exp2_approx((m_s[w][r] - ref) * scale);
+        const float4 y = *reinterpret_cast<const float4*>(&o_s[w][r][d]);
+        sum = fmaf(l_s[w][r], z, sum);
+        val.x = fmaf(y.x, z, val.x); val.y = fmaf(y.y, z, val.y); val.z = fmaf(y.z, z, val.z); val.w = fmaf(y.w, z, val.w);
       }
-      store(r, d, sum, val);
+      if (whole) {
+        store(r, d, sum, val);
+      } else {
+        *reinterpret_cast<float4*>(mine + r * p.dim + d) = val;
+        if (d == 0) {
+          mine[ROWS * p.dim + r] = top;
+          mine[ROWS * p.dim + ROWS + r] = sum;
+        }
+      }
     }
-  }
-  // Rows of several queries see different keys, and a weight of zero times a value that is not finite is NaN: such
-  // rows are done again, key by visible key.
-  if (q_last > q_first) {
-    __syncthreads();
-    for (int r = warp; r < rows; r += kFewWarps) {
-      const int i = (rt * kFewRows + r) / G, head = kv * G + (rt * kFewRows + r) % G;
-      const T* out = reinterpret_cast<const T*>(p.out.data + (int64_t)(sq.q0 + i) * p.out.row_bytes +
-                                                (int64_t)head * p.out.head_bytes);
-      bool odd = false;
-      for (int d = lane; d < p.dim; d += 32) odd = odd || !(fabsf(to_f(out[d])) < INFINITY);
-      if (!__any_sync(0xffffffffu, odd)) continue;
-      const T* src = reinterpret_cast<const T*>(p.q.data + (int64_t)(sq.q0 + i) * p.q.row_bytes +
-                                                (int64_t)head * p.q.head_bytes);
-      float* qs = &o_s[warp][0][0];
-      for (int d = lane; d < p.dim; d += 32) qs[d] = to_f(src[d]);
-      __syncwarp();
-      attend_row<T>(p, sq, i, head, qs);
-      __syncwarp();
+    if (!whole) {
+      const int64_t b0 = u0 / share, b1 = (u0 + units - 1) / share;   // the blocks that have a part of the tile
+      const int parts = (int)(b1 - b0) + 1;
+      __threadfence();
+      __syncthreads();
+      if (threadIdx.x == 0) last_s = atomicAdd(&f.tickets[b0], 1) == parts - 1;
+      __syncthreads();
+      if (!last_s) return;
+      __threadfence();
+      if (threadIdx.x == 0) f.tickets[b0] = 0;
+      // the first block's part may be its last piece of work, the others' is their first
+      const float* all = f.parts + b0 * 2 * size;
+      auto at = [&](int i) { return all + (2 * (int64_t)i + (i == 0 && b0 * share < u0 ? 1 : 0)) * size; };
+      float* z_s = &o_s[0][0][0];                    // [rows][parts]
+      const bool fits = rows * parts <= kFewWarps * ROWS * DS;
+      for (int r = warp; r < rows; r += kFewWarps) {
+        float top = -INFINITY, sum = 0.f;
+        for (int i = lane; i < parts; i += 32) top = fmaxf(top, __ldcg(at(i) + ROWS * p.dim + r));
+#pragma unroll
+        for (int d = 16; d > 0; d /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        const float ref = top == -INFINITY ? 0.f : top;
+        for (int i = lane; i < parts; i += 32) {
+          const float z = exp2_approx((__ldcg(at(i) + ROWS * p.dim + r) - ref) * scale);
+          sum = fmaf(__ldcg(at(i) + ROWS * p.dim + ROWS + r), z, sum);
+          if (fits) z_s[r * parts + i] = z;
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        if (lane == 0) {
+          sum_s[r] = sum;
+          m_s[0][r] = ref;
+        }
+      }
+      __syncthreads();
+      for (int x = threadIdx.x; x < rows * quads; x += 32 * kFewWarps) {
+        const int r = x / quads, d = 4 * (x - r * quads);
+        float4 val = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+        for (int i = 0; i < parts; ++i) {
+          const float z = fits ? z_s[r * parts + i] : exp2_approx((__ldcg(at(i) + ROWS * p.dim + r) - m_s[0][r]) * scale);
+          const float4 y = __ldcg(reinterpret_cast<const float4*>(at(i) + r * p.dim + d));
+          val.x = fmaf(y.x, z, val.x); val.y = fmaf(y.y, z, val.y); val.z = fmaf(y.z, z, val.z); val.w = fmaf(y.w, z, val.w);
+        }
+        store(r, d, sum_s[r], val);
+      }
+    }
+    // Rows of several queries see different keys, and a weight of zero times a value that is not finite is NaN: such
+    // rows are done again, key by visible key.
+    if (pos_last > pos_first) {
+      __syncthreads();
+      for (int r = warp; r < rows; r += kFewWarps) {
+        const int i = (row0 + r) / G, head = kv * G + (row0 + r) % G;
+        const T* out = reinterpret_cast<const T*>(p.out.data + (int64_t)(sq.q0 + i) * p.out.row_bytes +
+                                                  (int64_t)head * p.out.head_bytes);
+        bool odd = false;
+        for (int d = lane; d < p.dim; d += 32) odd = odd || !(fabsf(to_f(out[d])) < INFINITY);
+        if (!__any_sync(0xffffffffu, odd)) continue;
+        const T* src = reinterpret_cast<const T*>(p.q.data + (int64_t)(sq.q0 + i) * p.q.row_bytes +
+                                                  (int64_t)head * p.q.head_bytes);
+        float* qs = &o_s[warp][0][0];
+        __syncwarp();
+        for (int d = lane; d < p.dim; d += 32) qs[d] = to_f(src[d]);
+        __syncwarp();
+        attend_row<T>(p, sq, i, head, qs);
+        __syncwarp();
+      }
+    }
+  };
+
+  if (balanced) {
+    const int64_t end = min(((int64_t)blockIdx.x + 1) * share, (int64_t)pre[p.n_seqs] * KR);
+    for (int64_t u = blockIdx.x * share; u < end;) {
+      const int x = (int)(u / KR);
+      int a = 0, z = p.n_seqs;                       // the last sequence that starts at or before x has units
+      while (z - a > 1) {
+        const int mid = (a + z) / 2;
+        if (pre[mid] <= x) a = mid; else z = mid;
+      }
+      const int units = pre[a + 1] - pre[a];
+      const int64_t r = u - (int64_t)pre[a] * KR;
+      const int kr = (int)(r / units), v0 = (int)(r - (int64_t)kr * units), v1 = (int)min((int64_t)units, v0 + (end - u));
+      process(a, kr, v0, v1, units, u - v0);
+      u += v1 - v0;
+      __syncthreads();
+    }
+  } else {
+    for (int64_t tile = blockIdx.x; tile < (int64_t)p.n_seqs * KR; tile += gridDim.x) {
+      const int b = (int)(tile / KR);
+      bool bad;
+      const int units = few_units(p, sequence(p, b, &bad));
+      if (bad && threadIdx.x == 0) atomicOr(p.err, DEV_ERR_INDEX_RANGE);
+      if (units > 0) process(b, (int)(tile - (int64_t)b * KR), 0, units, units, 0);
+      __syncthreads();
     }
   }
 }

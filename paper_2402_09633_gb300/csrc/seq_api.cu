@@ -21,7 +21,6 @@ struct gnn_attention {
   int n_sm = 0;
   uint32_t* d_err = nullptr;
   PFN_cuTensorMapEncodeTiled_v12000 encode = nullptr;
-  int slots = 0;                     // results of parts of the keys that the workspace holds
   float* d_parts = nullptr;
   int* d_tickets = nullptr;
 };
@@ -181,35 +180,35 @@ int run_tiles(gnn_attention* a, const gnn_attention_call* c, const gnn_heads* vi
   return err == cudaSuccess ? GNN_OK : cuda_fail(err);
 }
 
-// Few queries to a sequence: the keys split over as many blocks as keep the SMs busy for several rounds, so that
-// sequences of different lengths even out.
+template <typename T>
+cudaError_t launch_few(unsigned grid, cudaStream_t st, const AttendParams& p, const FewGrid& f, bool sixteen) {
+  auto go = [&](auto kernel) { return launch_pdl(kernel, grid, 32 * kFewWarps, 0, st, p, f); };
+  switch ((p.dim + 31) / 32) {
+    case 1: return sixteen ? go(attend_few_kernel<T, 1, 2>) : go(attend_few_kernel<T, 1, 1>);
+    case 2: return sixteen ? go(attend_few_kernel<T, 2, 2>) : go(attend_few_kernel<T, 2, 1>);
+    case 3: return sixteen ? go(attend_few_kernel<T, 3, 2>) : go(attend_few_kernel<T, 3, 1>);
+    default: return sixteen ? go(attend_few_kernel<T, 4, 2>) : go(attend_few_kernel<T, 4, 1>);
+  }
+}
+
+// Few queries to a sequence: one round of blocks, which share the keys out among them.
 int run_few(gnn_attention* a, const gnn_attention_call* c, const AttendParams& p, int64_t max_q, cudaStream_t st) {
   FewGrid f = {};
   f.group = p.heads / p.kv_heads;
   f.max_q = (int)max_q;
-  f.row_tiles = (int)((max_q * f.group + kFewRows - 1) / kFewRows);
+  const bool sixteen = max_q * f.group > 8;
+  f.row_tiles = (int)((max_q * f.group + (sixteen ? 15 : 7)) / (sixteen ? 16 : 8));
+  f.least = 2;
+  f.parts = a->d_parts;
+  f.tickets = a->d_tickets;
+  // no more blocks than there are units of keys, where the keys are known to be few
   int64_t keys = c->kv_len ? c->n_kv_rows : max_q;
   if (c->max_kv > 0) keys = std::min<int64_t>(keys, c->max_kv);
   if (p.left >= 0 && p.right >= 0) keys = std::min<int64_t>(keys, (int64_t)p.sinks + p.left + p.right + max_q);
-  const int64_t tiles = (int64_t)p.n_seqs * p.kv_heads * f.row_tiles, wanted = (int64_t)a->n_sm * 18;
-  f.chunk = (int)std::max<int64_t>(kFewStep, (keys * tiles / wanted + kFewStep - 1) / kFewStep * kFewStep);
-  f.splits = (int)std::max<int64_t>(1, std::min<int64_t>((keys + f.chunk - 1) / f.chunk, a->slots / tiles));
-  f.parts = a->d_parts;
-  f.tickets = a->d_tickets;
-  const unsigned grid = (unsigned)(tiles * f.splits);
-  cudaError_t err;
-  auto go = [&](auto kernel) { return launch_pdl(kernel, grid, 32 * kFewWarps, 0, st, p, f); };
-  const int nc = (p.dim + 31) / 32;
-  if (c->dtype == GNN_DTYPE_BF16)
-    err = nc == 1   ? go(attend_few_kernel<__nv_bfloat16, 1>)
-          : nc == 2 ? go(attend_few_kernel<__nv_bfloat16, 2>)
-          : nc == 3 ? go(attend_few_kernel<__nv_bfloat16, 3>)
-                    : go(attend_few_kernel<__nv_bfloat16, 4>);
-  else
-    err = nc == 1   ? go(attend_few_kernel<__half, 1>)
-          : nc == 2 ? go(attend_few_kernel<__half, 2>)
-          : nc == 3 ? go(attend_few_kernel<__half, 3>)
-                    : go(attend_few_kernel<__half, 4>);
+  const int64_t units = (int64_t)p.n_seqs * p.kv_heads * f.row_tiles * ((keys + kFewUnit) / kFewUnit);
+  const unsigned grid = (unsigned)std::min<int64_t>(units, (int64_t)a->n_sm * (sixteen && p.dim > 64 ? 2 : 3));
+  const cudaError_t err = c->dtype == GNN_DTYPE_BF16 ? launch_few<__nv_bfloat16>(grid, st, p, f, sixteen)
+                                                     : launch_few<__half>(grid, st, p, f, sixteen);
   return err == cudaSuccess ? GNN_OK : cuda_fail(err);
 }
 
@@ -307,10 +306,10 @@ int gnn_attention_create(gnn_attention** out) {
   if (err == cudaSuccess && (found != cudaDriverEntryPointSuccess || !a->encode)) err = cudaErrorNotSupported;
   if (err == cudaSuccess) err = dev_alloc((void**)&a->d_err, 4);
   if (err == cudaSuccess) err = cudaMemset(a->d_err, 0, 4);
-  a->slots = 32 * a->n_sm;
-  if (err == cudaSuccess) err = dev_alloc((void**)&a->d_parts, (size_t)a->slots * kFewRows * (128 + 2) * 4);
-  if (err == cudaSuccess) err = dev_alloc((void**)&a->d_tickets, (size_t)a->slots * 4);
-  if (err == cudaSuccess) err = cudaMemset(a->d_tickets, 0, (size_t)a->slots * 4);
+  const size_t blocks = 3 * (size_t)a->n_sm;         // of a call with few queries: two parts and a ticket each
+  if (err == cudaSuccess) err = dev_alloc((void**)&a->d_parts, blocks * 2 * kFewRows * (128 + 2) * 4);
+  if (err == cudaSuccess) err = dev_alloc((void**)&a->d_tickets, blocks * 4);
+  if (err == cudaSuccess) err = cudaMemset(a->d_tickets, 0, blocks * 4);
   if (err != cudaSuccess) {
     free_attention(a);
     return cuda_fail(err);
