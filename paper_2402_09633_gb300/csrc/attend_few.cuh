@@ -21,12 +21,12 @@ namespace gnn {
 constexpr int kFewWarps = 4, kFewUnit = 16 * kFewWarps;      // keys that a block takes at a time
 constexpr int kFewSeqs = 1024;       // sequences whose lengths a block sums up; with more, blocks take whole row tiles
 constexpr int kFewRows = 16;         // rows of a tile, at most
+constexpr int kFewPadded = 8;        // shares up to which blocks have parts of one tile only
 
 struct FewGrid {
   int group;                         // query heads to a key head
   int max_q;                         // queries of a sequence, at most
   int row_tiles;
-  int least;                         // units that a block takes, at least
   float* parts;                      // [block][2]: a tile's outputs [rows][dim], maxima [rows] and sums [rows]
   int* tickets;                      // [block], zero between calls: of the tile that starts in the block and goes on
 };
@@ -79,51 +79,73 @@ __global__ void __launch_bounds__(32 * kFewWarps, NR == 2 && NC > 2 ? 2 : 3)
   __shared__ float m_s[kFewWarps][ROWS], l_s[kFewWarps][ROWS], sum_s[ROWS];
   __shared__ int pre[kFewSeqs + 1], scan_s[kFewWarps];
   __shared__ int last_s;
+  __shared__ Sequence seq_s[32 * kFewWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int KR = p.kv_heads * f.row_tiles, G = f.group;
   const float scale = fabsf(p.scale_log2), slack = 8.f / scale;       // as in the tiled kernel
   const bool balanced = p.n_seqs <= kFewSeqs;
   pdl_wait();
 
-  // units before each sequence
-  int64_t share = 1;
+  // Units before each sequence, and a block's share of all of them.  A block whose share is small would spend it
+  // on waiting if it had parts of two tiles: there each tile starts with a block of its own.
+  int share = 1;
   if (balanced) {
-    int before = 0;
-    for (int b0 = 0; b0 < p.n_seqs; b0 += 32 * kFewWarps) {
-      const int b = b0 + threadIdx.x;
-      int u = 0;
-      if (b < p.n_seqs) {
-        bool bad;
-        const Sequence sq = sequence(p, b, &bad);
-        if ((bad || sq.nq > f.max_q) && blockIdx.x == 0) atomicOr(p.err, DEV_ERR_INDEX_RANGE);
-        u = few_units(p, sq);
-      }
-      int x = u;
+    auto block_scan = [&](int x, int* sum) {         // the sum up to this thread's, and that of all
 #pragma unroll
       for (int d = 1; d < 32; d *= 2) {
         const int y = __shfl_up_sync(0xffffffffu, x, d);
         if (lane >= d) x += y;
       }
+      __syncthreads();
       if (lane == 31) scan_s[warp] = x;
       __syncthreads();
-      int sums = before;
+      *sum = 0;
+#pragma unroll
       for (int w = 0; w < kFewWarps; ++w) {
         if (w < warp) x += scan_s[w];
-        sums += scan_s[w];
+        *sum += scan_s[w];
       }
-      if (b < p.n_seqs) pre[b] = before + x - u;
-      before = sums;
-      __syncthreads();
+      return x;
+    };
+    int before = 0;
+    for (int b0 = 0; b0 < p.n_seqs; b0 += 32 * kFewWarps) {
+      const int b = b0 + threadIdx.x;
+      int u = 0, sum;
+      if (b < p.n_seqs) {
+        bool bad;
+        const Sequence sq = sequence(p, b, &bad);
+        if ((bad || sq.nq > f.max_q) && blockIdx.x == 0) atomicOr(p.err, DEV_ERR_INDEX_RANGE);
+        if (b < 32 * kFewWarps) seq_s[b] = sq;
+        u = few_units(p, sq);
+      }
+      int upto = block_scan(u, &sum);
+      if (p.n_seqs <= 32 * kFewWarps) {
+        share = max(1, (int)(((int64_t)sum * KR + gridDim.x - 1) / gridDim.x));
+        if (share <= kFewPadded) {
+          for (int s = share; s <= 2 * kFewPadded; ++s) {
+            int padded;
+            const int x = block_scan((u + s - 1) / s * s, &padded);
+            if ((int64_t)padded * KR > (int64_t)s * gridDim.x) continue;
+            upto = x;
+            u = (u + s - 1) / s * s;
+            sum = padded;
+            share = s;
+            break;
+          }
+        }
+      }
+      if (b < p.n_seqs) pre[b] = before + upto - u;
+      before += sum;
     }
     if (threadIdx.x == 0) pre[p.n_seqs] = before;
     __syncthreads();
-    share = max((int64_t)f.least, ((int64_t)before * KR + gridDim.x - 1) / gridDim.x);
+    if (p.n_seqs > 32 * kFewWarps) share = max(1, (int)(((int64_t)before * KR + gridDim.x - 1) / gridDim.x));
   }
 
   // Units [v0, v1) of the `units` of row tile kr of sequence b; u0: the tile's first unit among all.
   auto process = [&](int b, int kr, int v0, int v1, int units, int64_t u0) {
-    bool bad;
-    const Sequence sq = sequence(p, b, &bad);
+    bool bad = false;
+    const Sequence sq = balanced && b < 32 * kFewWarps ? seq_s[b] : sequence(p, b, &bad);
     if (!balanced && (bad || sq.nq > f.max_q) && threadIdx.x == 0) atomicOr(p.err, DEV_ERR_INDEX_RANGE);
     const int rt = kr % f.row_tiles, kv = kr / f.row_tiles, row0 = rt * ROWS;
     const int rows = min(min(sq.nq, f.max_q) * G - row0, ROWS);
@@ -353,37 +375,82 @@ __global__ void __launch_bounds__(32 * kFewWarps, NR == 2 && NC > 2 ? 2 : 3)
       // the first block's part may be its last piece of work, the others' is their first
       const float* all = f.parts + b0 * 2 * size;
       auto at = [&](int i) { return all + (2 * (int64_t)i + (i == 0 && b0 * share < u0 ? 1 : 0)) * size; };
-      float* z_s = &o_s[0][0][0];                    // [rows][parts]
+      float* z_s = &o_s[0][0][0];                    // [rows][parts]: what each part's sums are multiplied by
       const bool fits = rows * parts <= kFewWarps * ROWS * DS;
-      for (int r = warp; r < rows; r += kFewWarps) {
-        float top = -INFINITY, sum = 0.f;
-        for (int i = lane; i < parts; i += 32) top = fmaxf(top, __ldcg(at(i) + ROWS * p.dim + r));
+      if (parts <= 128 && fits) {                    // all maxima and sums at once: the loads wait for nothing
+        float pm[ROWS / kFewWarps][4], pl[ROWS / kFewWarps][4];
 #pragma unroll
-        for (int d = 16; d > 0; d /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-        const float ref = top == -INFINITY ? 0.f : top;
-        for (int i = lane; i < parts; i += 32) {
-          const float z = exp2_approx((__ldcg(at(i) + ROWS * p.dim + r) - ref) * scale);
-          sum = fmaf(__ldcg(at(i) + ROWS * p.dim + ROWS + r), z, sum);
-          if (fits) z_s[r * parts + i] = z;
+        for (int y = 0; y < ROWS / kFewWarps; ++y)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int r = warp + kFewWarps * y, i = lane + 32 * k;
+            const bool have = r < rows && i < parts;
+            pm[y][k] = have ? __ldcg(at(i) + ROWS * p.dim + r) : -INFINITY;
+            pl[y][k] = have ? __ldcg(at(i) + ROWS * p.dim + ROWS + r) : 0.f;
+          }
+#pragma unroll
+        for (int y = 0; y < ROWS / kFewWarps; ++y) {
+          const int r = warp + kFewWarps * y;
+          float top = fmaxf(fmaxf(pm[y][0], pm[y][1]), fmaxf(pm[y][2], pm[y][3])), sum = 0.f;
+#pragma unroll
+          for (int d = 16; d > 0; d /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+          const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float z = exp2_approx((pm[y][k] - ref) * scale);
+            sum = fmaf(pl[y][k], z, sum);
+            if (r < rows && lane + 32 * k < parts) z_s[r * parts + lane + 32 * k] = z;
+          }
+#pragma unroll
+          for (int d = 16; d > 0; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+          if (lane == 0 && r < rows) sum_s[r] = sum;
         }
+      } else {
+        for (int r = warp; r < rows; r += kFewWarps) {
+          float top = -INFINITY, sum = 0.f;
+          for (int i = lane; i < parts; i += 32) top = fmaxf(top, __ldcg(at(i) + ROWS * p.dim + r));
 #pragma unroll
-        for (int d = 16; d > 0; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-        if (lane == 0) {
-          sum_s[r] = sum;
-          m_s[0][r] = ref;
+          for (int d = 16; d > 0; d /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+          const float ref = top == -INFINITY ? 0.f : top;
+          for (int i = lane; i < parts; i += 32) {
+            const float z = exp2_approx((__ldcg(at(i) + ROWS * p.dim + r) - ref) * scale);
+            sum = fmaf(__ldcg(at(i) + ROWS * p.dim + ROWS + r), z, sum);
+            if (fits) z_s[r * parts + i] = z;
+          }
+#pragma unroll
+          for (int d = 16; d > 0; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+          if (lane == 0) {
+            sum_s[r] = sum;
+            m_s[0][r] = ref;
+          }
         }
       }
       __syncthreads();
-      for (int x = threadIdx.x; x < rows * quads; x += 32 * kFewWarps) {
-        const int r = x / quads, d = 4 * (x - r * quads);
+      // four outputs to a thread's place; eight parts' are loaded together
+      for (int place = threadIdx.x; place < rows * quads; place += 32 * kFewWarps) {
+        const int r = place / quads;
         float4 val = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-        for (int i = 0; i < parts; ++i) {
-          const float z = fits ? z_s[r * parts + i] : exp2_approx((__ldcg(at(i) + ROWS * p.dim + r) - m_s[0][r]) * scale);
-          const float4 y = __ldcg(reinterpret_cast<const float4*>(at(i) + r * p.dim + d));
-          val.x = fmaf(y.x, z, val.x); val.y = fmaf(y.y, z, val.y); val.z = fmaf(y.z, z, val.z); val.w = fmaf(y.w, z, val.w);
+        for (int i0 = 0; i0 < parts; i0 += 8) {
+          float4 x[8];
+          float z[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) x[k] = __ldcg(reinterpret_cast<const float4*>(at(min(i0 + k, parts - 1))) + place);
+          if (fits) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) z[k] = i0 + k < parts ? z_s[r * parts + i0 + k] : 0.f;
+          } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              z[k] = i0 + k < parts ? exp2_approx((__ldcg(at(i0 + k) + ROWS * p.dim + r) - m_s[0][r]) * scale) : 0.f;
+          }
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            if (i0 + k < parts) {
+              val.x = fmaf(x[k].x, z[k], val.x); val.y = fmaf(x[k].y, z[k], val.y);
+              val.z = fmaf(x[k].z, z[k], val.z); val.w = fmaf(x[k].w, z[k], val.w);
+            }
         }
-        store(r, d, sum_s[r], val);
+        store(r, 4 * (place - r * quads), sum_s[r], val);
       }
     }
     // Rows of several queries see different keys, and a weight of zero times a value that is not finite is NaN: such
@@ -411,7 +478,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, NR == 2 && NC > 2 ? 2 : 3)
 
   if (balanced) {
     const int64_t end = min(((int64_t)blockIdx.x + 1) * share, (int64_t)pre[p.n_seqs] * KR);
-    for (int64_t u = blockIdx.x * share; u < end;) {
+    for (int64_t u = (int64_t)blockIdx.x * share; u < end;) {
       const int x = (int)(u / KR);
       int a = 0, z = p.n_seqs;                       // the last sequence that starts at or before x has units
       while (z - a > 1) {
@@ -421,7 +488,9 @@ __global__ void __launch_bounds__(32 * kFewWarps, NR == 2 && NC > 2 ? 2 : 3)
       const int units = pre[a + 1] - pre[a];
       const int64_t r = u - (int64_t)pre[a] * KR;
       const int kr = (int)(r / units), v0 = (int)(r - (int64_t)kr * units), v1 = (int)min((int64_t)units, v0 + (end - u));
-      process(a, kr, v0, v1, units, u - v0);
+      // where tiles are padded to whole shares, `units` counts the padding too
+      const int real = share <= 2 * kFewPadded && p.n_seqs <= 32 * kFewWarps ? few_units(p, seq_s[a]) : units;
+      if (v0 < real) process(a, kr, v0, min(v1, real), real, u - v0);
       u += v1 - v0;
       __syncthreads();
     }

@@ -198,7 +198,6 @@ int run_few(gnn_attention* a, const gnn_attention_call* c, const AttendParams& p
   f.max_q = (int)max_q;
   const bool sixteen = max_q * f.group > 8;
   f.row_tiles = (int)((max_q * f.group + (sixteen ? 15 : 7)) / (sixteen ? 16 : 8));
-  f.least = 2;
   f.parts = a->d_parts;
   f.tickets = a->d_tickets;
   // no more blocks than there are units of keys, where the keys are known to be few
