@@ -13,6 +13,7 @@ constexpr int kTileQ = 128, kTileK = 128;          // queries of a tile, keys of
 // with 168 registers a thread; the last one hands over what it does not need: 2 * 216 + 72 = 3 * 168.
 constexpr int kAttendThreads = 384, kSoftmaxRegs = 216, kControlRegs = 72;
 constexpr int kMmaWarp = 8, kCopyWarp = 10;
+constexpr int kStageBytes = 32 * 64;
 constexpr int kItemSlots = 4;                      // items that the copy warp is ahead by, at most
 
 template <int DP>
@@ -205,7 +206,7 @@ struct AttendBars {
   int abort;
 };
 template <int DP>
-constexpr int attend_smem_bytes() { return AttendShape<DP>::kSmem + 8 * 128 * 4 + (int)sizeof(AttendBars) + 1024; }
+constexpr int attend_smem_bytes() { return AttendShape<DP>::kSmem + 8 * kStageBytes + (int)sizeof(AttendBars) + 1024; }
 
 template <typename T, int DP>
 __global__ void __launch_bounds__(kAttendThreads, 1)
@@ -217,8 +218,8 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   uint8_t* q_buf = smem;
   uint8_t* kv_buf = smem + S::kQBufs * 2 * S::kTileBytes;
-  float* q_rows = reinterpret_cast<float*>(smem + S::kSmem);             // a row per softmax warp, for the repair
-  AttendBars& b = *reinterpret_cast<AttendBars*>(q_rows + 8 * 128);
+  uint8_t* stage = smem + S::kSmem;                // 32 rows of 32 columns of output to a softmax warp
+  AttendBars& b = *reinterpret_cast<AttendBars*>(stage + 8 * kStageBytes);
   const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
   volatile int* abort = &b.abort;
 
@@ -484,7 +485,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
       // the row's keys, and the warp's: of its first row, and of its last that the tile has
       const int tile_top = item.t[wg].top, tile_low = item.t[wg].low, w0 = (warp & 3) * 32, w1 = min(rows, w0 + 32) - 1;
       const int top = min(len - 1, tile_top + row), low = max(0, tile_low + row);
-      char* out = p.out.data + (int64_t)(item.sq.q0 + item.t[wg].row + row) * p.out.row_bytes +
+      char* out = p.out.data + (int64_t)(item.sq.q0 + item.t[wg].row + w0) * p.out.row_bytes +   // the warp's first row's
                   (int64_t)item.t[wg].head * p.out.head_bytes;
       __syncwarp();
       if (lane == 0) mbar_arrive(&b.item_empty[slot]);
@@ -529,7 +530,6 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
       auto guess = [&]() {
         float s[128];
         read(s);
-        const bool over = mbar_test_wait(&b.pv_done[wg], (n - 1) & 1);
         const float off = -m * scale;                // m = -inf: the guess is wrong, or every score is -inf
         const float2 off2 = make_float2(off, off);
         float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
@@ -544,7 +544,8 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         weigh(s + 32, off2, sum, w + 16);
         if (!warp_all(high <= m + slack && m > -INFINITY)) return false;
         scores_read();
-        if (!warp_all(over)) ok = wait(&b.pv_done[wg], n - 1);
+        // the last product with these weights' columns, and into these outputs, is over
+        ok = wait(&b.pv_done[wg], n - 1);
         if (!ok) return true;
         tc_fence_after();
         tmem_st_32x16(tp, w);
@@ -645,28 +646,36 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
       const bool none = blocks == 0 || l == 0.f;
       const float r = none ? 0.f : 1.f / l;
       float2 odd = make_float2(0.f, 0.f);            // not finite once a value is not
-#pragma unroll
+      uint8_t* mine = stage + warp * kStageBytes;
+#pragma unroll 1
       for (int c = 0; c < DP; c += 32) {
+        // A thread has a row, and rows lie apart: written from here, every store would touch 32 lines.  Through shared
+        // memory, 16 bytes at a place that the row turns by its number, four threads write 64 bytes of a row.
         float o[32];
         if (blocks > 0) {
           tmem_ld_32x32(to + c, o);
           tmem_wait_ld_32(o);
         }
+        __syncwarp();
 #pragma unroll
-        for (int e = 0; e < 32; ++e) o[e] = none ? 0.f : o[e] * r;
+        for (int e = 0; e < 32; e += 8) {
+          uint32_t u[4];
 #pragma unroll
-        for (int e = 0; e < 32; e += 2) odd = __fadd2_rn(odd, make_float2(o[e], o[e + 1]));
-        if (row < rows)
+          for (int x = 0; x < 4; ++x) {
+            const float2 y = none ? make_float2(0.f, 0.f) : make_float2(o[e + 2 * x] * r, o[e + 2 * x + 1] * r);
+            odd = __fadd2_rn(odd, y);
+            u[x] = pack2<T>(y.x, y.y);
+          }
+          *reinterpret_cast<uint4*>(mine + lane * 64 + (e / 8 ^ lane / 2 % 4) * 16) = make_uint4(u[0], u[1], u[2], u[3]);
+        }
+        __syncwarp();
 #pragma unroll
-          for (int e = 0; e < 32; e += 8)
-            if (c + e < p.dim) {
-              uint4 u;
-              u.x = pack2<T>(o[e], o[e + 1]);
-              u.y = pack2<T>(o[e + 2], o[e + 3]);
-              u.z = pack2<T>(o[e + 4], o[e + 5]);
-              u.w = pack2<T>(o[e + 6], o[e + 7]);
-              *reinterpret_cast<uint4*>(out + (c + e) * 2) = u;
-            }
+        for (int i = 0; i < 4; ++i) {
+          const int at = 8 * i + lane / 4;
+          if (w0 + at < rows && c + lane % 4 * 8 < p.dim)
+            *reinterpret_cast<uint4*>(out + at * p.out.row_bytes + (c + lane % 4 * 8) * 2) =
+                *reinterpret_cast<const uint4*>(mine + at * 64 + (lane % 4 ^ at / 2 % 4) * 16);
+        }
       }
       tc_fence_before();
       dirty = dirty || (row < rows && !(fabsf(odd.x + odd.y) < INFINITY));
@@ -674,7 +683,8 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
     // A weight of zero times a value that is not finite is NaN: rows that hold one are done again, key by visible
     // key.  After everything else, so that nothing waits for it.
     if (ok && __any_sync(0xffffffffu, dirty)) {
-      float* qs = q_rows + warp * 128;
+      float* qs = reinterpret_cast<float*>(stage + warp * kStageBytes);
+      __syncwarp();
       for (int64_t at = blockIdx.x; at < g.items; at += gridDim.x) {
         AttendItem it;
         if (!attend_item(p, g, at, it)) continue;
