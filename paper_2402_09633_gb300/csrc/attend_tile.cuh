@@ -494,6 +494,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
       if (rows == 0) continue;
       float m = row < rows ? -INFINITY : INFINITY, l = 0.f;        // rows that the tile does not have weigh nothing
       const float2 scale2 = make_float2(scale, scale);
+      bool plain = false;                            // every row has a maximum that the next block may be weighed by
       auto read = [&](float* s) {                    // the block's scores
         tc_fence_after();
 #pragma unroll
@@ -524,39 +525,73 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
           w[e] = pack2<T>(x.x, x.y);
         }
       };
-      // A block that every row sees whole, on the guess that its scores do not outgrow the running maximum (which they
-      // rarely do after the first block): the weights then do not wait for the maximum, and the two are computed
-      // side by side.  False, with nothing changed, when the guess was wrong.
-      auto guess = [&]() {
+      // Quarter c of block kb: true when no row of the warp sees any of it; else what a row does not see becomes -inf.
+      const int sink = min(p.sinks, len);
+      auto hide = [&](int kb, int c, float* s) {
+        const int j = kb * kTileK + 32 * c;
+        const int first_top = min(len - 1, tile_top + w0), last_top = min(len - 1, tile_top + w1);
+        if (w1 < w0 || j > last_top || (j + 31 < tile_low + w0 && j >= sink)) return true;
+        if (j + 31 > first_top || (j < tile_low + w1 && j + 32 > sink)) {
+          auto below = [](int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; };
+          const uint32_t see = below(top + 1 - j) & (~below(low - j) | below(sink - j));
+#pragma unroll
+          for (int e = 0; e < 32; ++e) s[e] = see >> e & 1u ? s[e] : -INFINITY;
+        }
+        return false;
+      };
+      // A block on the guess that its scores do not outgrow the running maximum (which they
+      // rarely do after the first block).  In bf16 nothing depends on the guess: weights above 1 lose no precision,
+      // their sum tells whether the next block has to look for the maximum, and only scores that outgrow it by 2^100
+      // in one block would overflow, in a row that is then not finite and done again.  In fp16, whose weights end at
+      // 2^16, the maximum is computed beside the weights: false, with nothing changed, when the guess was wrong.
+      constexpr bool LOOSE = std::is_same<T, __nv_bfloat16>::value;
+      auto guess = [&](int kb, auto edge) {
+        constexpr bool EDGE = decltype(edge)::value;   // a block that not every row sees whole (bf16)
         float s[128];
         read(s);
-        const float off = -m * scale;                // m = -inf: the guess is wrong, or every score is -inf
+        if (LOOSE) scores_read();
+        const float off = -m * scale;
         const float2 off2 = make_float2(off, off);
         float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
         uint32_t w[32];
-        float mx[4] = {s[0], s[1], s[2], s[3]};
+        auto quarter = [&](int c, uint32_t* w) {
+          if (EDGE && hide(kb, c, s + 32 * c)) {
 #pragma unroll
-        for (int c = 4; c < 124; c += 8)
+            for (int e = 0; e < 16; ++e) w[e] = 0u;
+          } else {
+            weigh(s + 32 * c, off2, sum, w);
+          }
+        };
+        if (!LOOSE) {
+          float mx[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-          for (int x = 0; x < 4; ++x) mx[x] = max3(mx[x], s[c + x], s[c + 4 + x]);
-        const float high = max3(max3(mx[0], mx[1], mx[2]), max3(mx[3], s[124], s[125]), fmaxf(s[126], s[127]));
-        weigh(s, off2, sum, w);
-        weigh(s + 32, off2, sum, w + 16);
-        if (!warp_all(high <= m + slack && m > -INFINITY)) return false;
-        scores_read();
+          for (int c = 4; c < 124; c += 8)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) mx[x] = max3(mx[x], s[c + x], s[c + 4 + x]);
+          const float high = max3(max3(mx[0], mx[1], mx[2]), max3(mx[3], s[124], s[125]), fmaxf(s[126], s[127]));
+          quarter(0, w);
+          quarter(1, w + 16);
+          if (!warp_all(high <= m + slack)) return false;
+          scores_read();
+        } else {
+          quarter(0, w);
+        }
         // the last product with these weights' columns, and into these outputs, is over
         ok = wait(&b.pv_done[wg], n - 1);
         if (!ok) return true;
         tc_fence_after();
         tmem_st_32x16(tp, w);
+        if (LOOSE) quarter(1, w + 16);
         tmem_st_32x16(tp + 16, w + 16);
-        weigh(s + 64, off2, sum, w);
+        quarter(2, w);
         stored(&b.p_half[wg]);
         tmem_st_32x16(tp + 32, w);
-        weigh(s + 96, off2, sum, w + 16);
+        quarter(3, w + 16);
         tmem_st_32x16(tp + 48, w + 16);
-        l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+        const float all = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+        l += all;
         stored(&b.p_full[wg]);
+        if (LOOSE) plain = warp_all(all <= 256.f || row >= rows);
         return true;
       };
       // Any block.
@@ -569,20 +604,9 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
           for (int c = 0; c < 128; ++c) s[c] = -s[c];
         }
         uint32_t hidden = 0;                         // quarters of the block that no row of the warp sees
-        const int j0 = kb * kTileK, sink = min(p.sinks, len);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const int j = j0 + 32 * c;
-          const int first_top = min(len - 1, tile_top + w0), last_top = min(len - 1, tile_top + w1);
-          if (w1 < w0 || j > last_top || (j + 31 < tile_low + w0 && j >= sink)) {
-            hidden |= 1u << c;
-          } else if (j + 31 > first_top || (j < tile_low + w1 && j + 32 > sink)) {
-            auto below = [](int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; };
-            const uint32_t see = below(top + 1 - j) & (~below(low - j) | below(sink - j));
-#pragma unroll
-            for (int e = 0; e < 32; ++e) s[32 * c + e] = see >> e & 1u ? s[32 * c + e] : -INFINITY;
-          }
-        }
+        for (int c = 0; c < 4; ++c)
+          if (hide(kb, c, s + 32 * c)) hidden |= 1u << c;
         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
         for (int c = 0; c < 4; ++c)
@@ -623,15 +647,19 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         }
         l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
         stored(&b.p_full[wg]);
+        plain = warp_all(m > -INFINITY);
         return true;
       };
       for (int i = 0; i < blocks; ++i, ++n) {
         const int kb = i < sinks ? i : lo + (i - sinks);
         ok = wait(&b.s_full[wg], n);
         if (!ok) break;
-        if (i > 0 && kb < whole_hi && (kb >= whole_lo || kb < whole_sinks) && p.scale_log2 >= 0.f && guess()) {
-          if (!ok) break;
-          continue;
+        if (plain && p.scale_log2 >= 0.f) {
+          const bool whole = kb < whole_hi && (kb >= whole_lo || kb < whole_sinks);
+          if (whole ? guess(kb, std::false_type()) : LOOSE && guess(kb, std::bool_constant<LOOSE>())) {
+            if (!ok) break;
+            continue;
+          }
         }
         ok = block(kb, i == 0);
         if (!ok) break;
