@@ -7,26 +7,34 @@
 
 namespace gnn {
 
-constexpr int kTileQ = 128, kTileK = 128;          // queries of a tile, keys of a block of keys
-// Two softmax warpgroups, one to a tile, and one for control: one or two warps that issue the products, and
-// one that finds the work and issues the copies.  All are launched
-// with 168 registers a thread; the last one hands over what it does not need: 2 * 216 + 72 = 3 * 168.
-constexpr int kAttendThreads = 384, kSoftmaxRegs = 216, kControlRegs = 72;
-constexpr int kMmaWarp = 8, kCopyWarp = 10;
+constexpr int kTileQ = 128;                        // queries of a tile
+constexpr int kMostTiles = 2;                      // tiles of a block
+constexpr int kKeys = 128;                         // keys of a block of keys
 constexpr int kStageBytes = 32 * 64;
 constexpr int kItemSlots = 4;                      // items that the copy warp is ahead by, at most
 
+// A softmax warpgroup to a tile, and one for control: warps that issue the products and one that finds the work and
+// issues the copies.  All are launched with 168 registers a thread, of which the last hands over what it does not
+// need: 2 * 216 + 72 = 3 * 168.
+constexpr int kAttendThreads = 384, kSoftmaxRegs = 216, kControlRegs = 72;
+constexpr int kSoftmaxWarps = 8, kMmaWarp = 8, kCopyWarp = 10;
+
+// DP: head_dim rounded up to 64 or 128.  Tensor memory has 512 columns for two tiles: the scores S in fp32 take 128
+// each, the outputs O DP.  With DP = 64 the weights P have 64 columns of their own, so that the next scores are
+// computed while the softmax runs; with DP = 128 they lie over the scores that they come from, and a tile's P V and
+// next Q K^T are one chain.  (Three tiles of 96 keys with P over S, DP = 64: 262 us on an event of 300,000 hits where
+// two apart took 215.)
 template <int DP>
 struct AttendShape {
-  static constexpr bool kApart = DP == 64;         // P has columns of its own; otherwise it lies over S
-  // Apart, a tile's products wait for nothing of the other tile's: a warp to each.  Over S, a tile's P V and the next
-  // Q K^T are one chain, and two chains in turn keep the tensor cores busy while two side by side end together.
+  static constexpr bool kApart = DP == 64;
+  // Apart, a tile's products wait for nothing of the other tile's: a warp to each.  Two chains in turn keep the tensor
+  // cores busy, while two side by side end together, and both tiles wait.
   static constexpr int kMmaWarps = kApart ? 2 : 1;
   static constexpr int kQBufs = DP == 64 ? 2 : 1;
   static constexpr int kStages = DP == 64 ? 8 : 4; // of a block of keys or of values each
-  static constexpr int kTileBytes = kTileQ * DP * 2;
-  static constexpr int kS = 0, kP = kApart ? 256 : 0, kPStep = kApart ? 64 : 128, kO = kApart ? 384 : 256;
-  static constexpr int kSmem = kQBufs * 2 * kTileBytes + kStages * kTileBytes;
+  static constexpr int kQBytes = kTileQ * DP * 2, kKvBytes = kKeys * DP * 2;
+  static constexpr int kP = kApart ? 256 : 0, kPStep = kApart ? 64 : 128, kO = kApart ? 384 : 256;
+  static constexpr int kSmem = kQBufs * kMostTiles * kQBytes + kStages * kKvBytes;
 };
 // ------------------------------------------------------------------ PTX
 __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
@@ -127,15 +135,14 @@ __device__ __forceinline__ uint64_t sdesc_nmajor_sw128(uint32_t saddr, uint32_t 
 struct AttendTile { int row, n, head, sinks, lo, hi, whole_sinks, whole_lo, whole_hi, top, low; };
 struct AttendItem {
   Sequence sq;
-  AttendTile t[2];
+  AttendTile t[kMostTiles];
   int kv_head, sinks, lo, n;         // the item's blocks: [0, sinks), then n - sinks from lo on
   __device__ __forceinline__ int block(int i) const { return i < sinks ? i : lo + (i - sinks); }
 };
+// An item is up to `tiles` tiles of a sequence that read the same key head: its query heads side by side, 128 rows
+// after 128 rows.
 struct AttendGrid {
-  int pair_heads;                    // the two tiles: the same rows of two heads, or 256 rows of one
-  int single;                        // one tile to an item: few items, which then spread over more SMs
-  int rows;                          // queries of an item: 128 or 256
-  int heads;                         // items side by side: heads or pairs of heads
+  int tiles, group;                  // group: query heads to a key head
   int64_t items;
 };
 
@@ -150,46 +157,50 @@ __device__ __forceinline__ AttendTile attend_tile(const AttendParams& p, const S
   const Seen a = seen_keys(pos, sq.len, p.left, p.right, p.sinks);
   const Seen z = seen_keys(pos + t.n - 1, sq.len, p.left, p.right, p.sinks);
   if (z.hi <= 0) return t;
-  t.hi = (z.hi + kTileK - 1) / kTileK;
-  t.lo = min(a.lo, z.hi) / kTileK;
-  t.sinks = min((z.first + kTileK - 1) / kTileK, t.lo);
-  t.whole_hi = a.hi / kTileK;
-  t.whole_lo = (z.lo + kTileK - 1) / kTileK;
-  t.whole_sinks = p.sinks / kTileK;
+  t.hi = (z.hi + kKeys - 1) / kKeys;
+  t.lo = min(a.lo, z.hi) / kKeys;
+  t.sinks = min((z.first + kKeys - 1) / kKeys, t.lo);
+  t.whole_hi = a.hi / kKeys;
+  t.whole_lo = (z.lo + kKeys - 1) / kKeys;
+  t.whole_sinks = p.sinks / kKeys;
   // some row sees a key, so a negative pos + right is above -kTileQ
   t.top = p.right < 0 ? INT_MAX - kTileQ : (int)min((int64_t)INT_MAX - kTileQ, (int64_t)pos + p.right);
   t.low = p.left < 0 ? -kTileQ : (int)max((int64_t)-kTileQ, (int64_t)pos - p.left);
   return t;
 }
 
-// Item `at`: false when it has no rows.  A sequence's items start at slot q0 / rows + b, which leaves room for
-// ceil(nq / rows) of them and needs no sum over the sequences before it.
+// Item `at`: false when it has no rows.  Sequence b's items start at slot group (q0 / 128 + b) / tiles + b, which leaves
+// room for all of them and needs no sum over the sequences before it.  (Slots and tiles are below 2^31; the divisions
+// are in 32 bits, as 64 bits take thousands of cycles here.)
 __device__ __noinline__ bool attend_item(const AttendParams& p, const AttendGrid& g, int64_t at, AttendItem& it) {
-  const int slot = (int)(at / g.heads), h = (int)(at - (int64_t)slot * g.heads);
+  const uint32_t heads = (uint32_t)p.kv_heads, group = (uint32_t)g.group, tiles = (uint32_t)g.tiles;
+  const uint32_t slot = at >> 32 ? (uint32_t)(at / heads) : (uint32_t)at / heads;
+  it.kv_head = (int)(at - (int64_t)slot * heads);
+  auto start = [&](int b, int q0) { return group * (uint32_t)(q0 / kTileQ + b) / tiles + (uint32_t)b; };
   int a = 0, z = p.n_seqs;
 #pragma unroll 1
   while (z - a > 1) {
     const int mid = (int)(((int64_t)a + z) / 2);
-    if (min(max(p.q_start[mid], 0), p.n_q_rows) / g.rows + mid <= slot) a = mid; else z = mid;
+    if (start(mid, min(max(p.q_start[mid], 0), p.n_q_rows)) <= slot) a = mid; else z = mid;
   }
   bool bad;
   it.sq = sequence(p, a, &bad);
-  const int64_t row = (int64_t)(slot - (it.sq.q0 / g.rows + a)) * g.rows;
-  if (row < 0 || row >= it.sq.nq) return false;
-  const int head = g.pair_heads ? 2 * h : h;
-  it.kv_head = head / (p.heads / p.kv_heads);
-  it.t[0] = attend_tile(p, it.sq, (int)row, head);
-  it.t[1] = g.pair_heads ? attend_tile(p, it.sq, (int)row, head + 1)
-                         : attend_tile(p, it.sq, g.single ? it.sq.nq : (int)row + kTileQ, head);
+  const uint32_t from = start(a, it.sq.q0), all = group * (uint32_t)((it.sq.nq + kTileQ - 1) / kTileQ);
+  if (slot < from || (slot - from) * tiles >= all) return false;
+  const uint32_t first = (slot - from) * tiles;
   int lo = INT_MAX, hi = 0;
   it.sinks = 0;
-#pragma unroll
-  for (int t = 0; t < 2; ++t)
+#pragma unroll 1
+  for (uint32_t t = 0; t < kMostTiles; ++t) {
+    const uint32_t e = first + t, row = e / group;
+    const bool have = t < tiles && e < all;
+    it.t[t] = attend_tile(p, it.sq, have ? (int)row * kTileQ : it.sq.nq, it.kv_head * g.group + (int)(e - row * group));
     if (it.t[t].hi > 0) {
       lo = min(lo, it.t[t].lo);
       hi = max(hi, it.t[t].hi);
       it.sinks = max(it.sinks, it.t[t].sinks);
     }
+  }
   if (hi == 0) lo = 0;
   it.sinks = min(it.sinks, lo);
   it.lo = lo;
@@ -199,14 +210,17 @@ __device__ __noinline__ bool attend_item(const AttendParams& p, const AttendGrid
 
 // ------------------------------------------------------------------ kernel
 struct AttendBars {
-  uint64_t q_full[2], q_empty[2], kv_full[8], kv_empty[8], s_full[2], s_free[2], p_half[2], p_full[2], pv_done[2], drain[2];
+  uint64_t q_full[2], q_empty[2], kv_full[8], kv_empty[8], drain[kMostTiles];
+  uint64_t s_full[kMostTiles], s_free[kMostTiles], p_half[kMostTiles], p_full[kMostTiles], pv_done[kMostTiles];
   uint64_t item_full[kItemSlots], item_empty[kItemSlots];
   AttendItem item[kItemSlots];
   uint32_t tmem;
   int abort;
 };
 template <int DP>
-constexpr int attend_smem_bytes() { return AttendShape<DP>::kSmem + 8 * kStageBytes + (int)sizeof(AttendBars) + 1024; }
+constexpr int attend_smem_bytes() {
+  return AttendShape<DP>::kSmem + kSoftmaxWarps * kStageBytes + (int)sizeof(AttendBars) + 1024;
+}
 
 template <typename T, int DP>
 __global__ void __launch_bounds__(kAttendThreads, 1)
@@ -217,9 +231,9 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   uint8_t* q_buf = smem;
-  uint8_t* kv_buf = smem + S::kQBufs * 2 * S::kTileBytes;
+  uint8_t* kv_buf = smem + S::kQBufs * kMostTiles * S::kQBytes;
   uint8_t* stage = smem + S::kSmem;                // 32 rows of 32 columns of output to a softmax warp
-  AttendBars& b = *reinterpret_cast<AttendBars*>(stage + 8 * kStageBytes);
+  AttendBars& b = *reinterpret_cast<AttendBars*>(stage + kSoftmaxWarps * kStageBytes);
   const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
   volatile int* abort = &b.abort;
 
@@ -227,12 +241,13 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
     for (int i = 0; i < 2; ++i) {
       mbar_init(&b.q_full[i], 1);
       mbar_init(&b.q_empty[i], S::kMmaWarps);
+    }
+    for (int i = 0; i < kMostTiles; ++i) {
       mbar_init(&b.s_full[i], 1);
       mbar_init(&b.s_free[i], 4);
       mbar_init(&b.p_half[i], 4);
       mbar_init(&b.p_full[i], 4);
       mbar_init(&b.pv_done[i], 1);
-      mbar_init(&b.drain[i], 1);
     }
     for (int i = 0; i < 8; ++i) {
       mbar_init(&b.kv_full[i], 1);
@@ -240,8 +255,9 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
     }
     for (int i = 0; i < kItemSlots; ++i) {
       mbar_init(&b.item_full[i], 1);
-      mbar_init(&b.item_empty[i], 8 + S::kMmaWarps);
+      mbar_init(&b.item_empty[i], kSoftmaxWarps + S::kMmaWarps);
     }
+    for (int i = 0; i < kMostTiles; ++i) mbar_init(&b.drain[i], 1);
     b.abort = 0;
     fence_mbar_init();
   }
@@ -272,11 +288,11 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
       if (__any_sync(0xffffffffu, late || *abort)) return false;
     }
   };
-  if (warp >= 8) {
+  if (warp >= kSoftmaxWarps) {
     regs_down<kControlRegs>();
     if (warp == kCopyWarp) {
       // ---------------- the work, item by item; its queries, and its keys and values through the ring
-      const uint32_t bytes = (uint32_t)halves * kTileQ * 128;
+      const uint32_t q_bytes = (uint32_t)halves * kTileQ * 128, kv_bytes = (uint32_t)halves * kKeys * 128;
       uint32_t kv = 0, q = 0, items = 0;
       bool ok = true;
       for (int64_t at = blockIdx.x; ok; at += gridDim.x) {
@@ -298,29 +314,31 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         if (q >= S::kQBufs) ok = wait(&b.q_empty[qb], q / S::kQBufs - 1);
         if (!ok) break;
         if (lane == 0) {
-          const bool two = it.t[1].hi > 0, one = it.t[0].hi > 0;
-          mbar_arrive_expect_tx(&b.q_full[qb], bytes * ((one ? 1 : 0) + (two ? 1 : 0)));
+          uint32_t some = 0;
 #pragma unroll
-          for (int t = 0; t < 2; ++t)
-            if (t ? two : one)
+          for (int t = 0; t < kMostTiles; ++t) some += it.t[t].hi > 0 ? 1 : 0;
+          mbar_arrive_expect_tx(&b.q_full[qb], q_bytes * some);
+#pragma unroll
+          for (int t = 0; t < kMostTiles; ++t)
+            if (it.t[t].hi > 0)
 #pragma unroll 1
               for (int h = 0; h < halves; ++h)
-                tma_load_3d(q_buf + (qb * 2 + t) * S::kTileBytes + h * kTileQ * 128, &map_q, 64 * h, it.t[t].head,
+                tma_load_3d(q_buf + (qb * kMostTiles + t) * S::kQBytes + h * kTileQ * 128, &map_q, 64 * h, it.t[t].head,
                             it.sq.q0 + it.t[t].row, &b.q_full[qb]);
         }
         ++q;
 #pragma unroll 1
         for (int i = 0; i < it.n && ok; ++i) {
-          const int row = it.sq.k0 + it.block(i) * kTileK;
+          const int row = it.sq.k0 + it.block(i) * kKeys;
 #pragma unroll 1
           for (int kind = 0; kind < 2; ++kind, ++kv) {
             const uint32_t st = kv % S::kStages;
             if (kv >= S::kStages) ok = wait(&b.kv_empty[st], kv / S::kStages - 1);
             if (!ok) break;
             if (lane == 0) {
-              mbar_arrive_expect_tx(&b.kv_full[st], bytes);
+              mbar_arrive_expect_tx(&b.kv_full[st], kv_bytes);
               for (int h = 0; h < halves; ++h)
-                tma_load_3d(kv_buf + st * S::kTileBytes + h * kTileK * 128, kind ? &map_v : &map_k, 64 * h, it.kv_head,
+                tma_load_3d(kv_buf + st * S::kKvBytes + h * kKeys * 128, kind ? &map_v : &map_k, 64 * h, it.kv_head,
                             row, &b.kv_full[st]);
             }
           }
@@ -342,17 +360,17 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         if (bad) atomicOr(p.err, DEV_ERR_INDEX_RANGE);
       }
     } else if (warp < kMmaWarp + S::kMmaWarps) {
-      // ---------------- the products: of one tile, or of both in turn
-      constexpr int NT = 2 / S::kMmaWarps;
-      const int first = warp - kMmaWarp;
+      // ---------------- the products of tiles mine .. mine + NT - 1
+      constexpr int NT = kMostTiles / S::kMmaWarps;
+      const int mine = NT == 1 ? warp - kMmaWarp : 0;
       const int steps = (p.dim + 15) / 16;
-      constexpr uint32_t id_qk = idesc_attend<T>(kTileQ, kTileK, false);
+      constexpr uint32_t id_qk = idesc_attend<T>(kTileQ, kKeys, false);
+      const uint32_t id_pv = idesc_attend<T>(kTileQ, (uint32_t)steps * 16, true);
       // Descriptors and addresses are computed by the whole warp, outside the elected thread's branch, so that they
-      // stay in uniform registers: inside it an MMA takes four times as long to issue.
+      // stay in uniform registers: inside it an MMA takes several times as long to issue.
       const uint32_t q_base = (uint32_t)uniform((int)smem_u32(q_buf)), kv_base = (uint32_t)uniform((int)smem_u32(kv_buf));
       const uint64_t q_desc = sdesc_kmajor_sw128(q_base), k_desc = sdesc_kmajor_sw128(kv_base),
-                     v_desc = sdesc_nmajor_sw128(kv_base, kTileK * 128);
-      const uint32_t id_pv = idesc_attend<T>(kTileQ, (uint32_t)steps * 16, true);
+                     v_desc = sdesc_nmajor_sw128(kv_base, kKeys * 128);
       uint32_t kv = 0, q = 0, items = 0, qk_n[NT] = {}, pv_n[NT] = {};
       bool ok = true;
       while (ok) {
@@ -361,11 +379,11 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         if (!ok) break;
         AttendTile tile[NT];
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          const AttendTile& from = b.item[slot].t[first + j];
-          tile[j].sinks = uniform(from.sinks);
-          tile[j].lo = uniform(from.lo);
-          tile[j].hi = uniform(from.hi);
+        for (int t = 0; t < NT; ++t) {
+          const AttendTile& from = b.item[slot].t[mine + t];
+          tile[t].sinks = uniform(from.sinks);
+          tile[t].lo = uniform(from.lo);
+          tile[t].hi = uniform(from.hi);
         }
         const int n = uniform(b.item[slot].n), sinks = uniform(b.item[slot].sinks), lo = uniform(b.item[slot].lo),
                   len = uniform(b.item[slot].sq.len);
@@ -377,24 +395,23 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         const uint32_t qb = q % S::kQBufs;
         bool fresh[NT];
 #pragma unroll
-        for (int j = 0; j < NT; ++j) fresh[j] = true;
-        auto qk = [&](int j, uint32_t st) {          // S = Q K^T, once the last scores have been read
-          const int t = first + j;
-          if (S::kApart && qk_n[j] > 0) ok = wait(&b.s_free[t], qk_n[j] - 1);
+        for (int t = 0; t < NT; ++t) fresh[t] = true;
+        auto qk = [&](int t, uint32_t st) {          // S = Q K^T, once the last scores have been read
+          if (S::kApart && qk_n[t] > 0) ok = wait(&b.s_free[mine + t], qk_n[t] - 1);
           if (!ok) return;
           tc_fence_after();
-          const uint64_t qa = q_desc + ((qb * 2 + t) * S::kTileBytes >> 4), ka = k_desc + (st * S::kTileBytes >> 4);
+          const uint64_t qa = q_desc + ((qb * kMostTiles + mine + t) * S::kQBytes >> 4), ka = k_desc + (st * S::kKvBytes >> 4);
           if (elect_one()) {
 #pragma unroll
             for (int k = 0; k < DP / 16; ++k) {
               if (k >= steps) break;
-              const uint64_t off = ((k >> 2) * kTileQ * 128 + (k & 3) * 32) >> 4;
-              mma_bf16_ss(tmem + S::kS + 128 * t, qa + off, ka + off, id_qk, k > 0);
+              const uint64_t off = ((k >> 2) * 128 * 128 + (k & 3) * 32) >> 4;
+              mma_bf16_ss(tmem + kKeys * (mine + t), qa + off, ka + off, id_qk, k > 0);
             }
-            mma_commit(&b.s_full[t]);
+            mma_commit(&b.s_full[mine + t]);
           }
           __syncwarp();
-          ++qk_n[j];
+          ++qk_n[t];
         };
         ok = wait(&b.q_full[qb], q / S::kQBufs);
         for (int i = -1; i < n && ok; ++i) {
@@ -410,43 +427,41 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
             ok = wait(&b.kv_full[vs], vn / S::kStages);
             if (!ok) break;
             // Values of rows behind the sequence's last key: zeros, so that weights of zero leave no trace of them.
-            // (Where two warps do this, each does before its own products.)
-            const int have = len - kb * kTileK;
-            if (have < kTileK) {
+            // (Where several warps do this, each does before its own products.)
+            const int have = len - kb * kKeys;
+            if (have < kKeys) {
 #pragma unroll 1
-              for (int r = have * 8 + lane; r < kTileK * 8; r += 32)
+              for (int r = have * 8 + lane; r < kKeys * 8; r += 32)
                 for (int h = 0; h < halves; ++h)
-                  *reinterpret_cast<uint4*>(kv_buf + vs * S::kTileBytes + h * kTileK * 128 + r * 16) = make_uint4(0, 0, 0, 0);
+                  *reinterpret_cast<uint4*>(kv_buf + vs * S::kKvBytes + h * kKeys * 128 + r * 16) = make_uint4(0, 0, 0, 0);
               fence_async_shared();
               __syncwarp();
             }
           }
 #pragma unroll
-          for (int j = 0; j < NT; ++j) {
-            if (i >= 0 && tile_sees(tile[j], kb)) {  // O += P V, in halves of 64 keys
-              const int t = first + j;
-              const uint64_t va = v_desc + (vs * S::kTileBytes >> 4);
-              const uint32_t acc = fresh[j] ? 0u : 1u;
+          for (int t = 0; t < NT; ++t) {
+            if (i >= 0 && tile_sees(tile[t], kb)) {  // O += P V, the first 64 keys and the others
+              const uint64_t va = v_desc + (vs * S::kKvBytes >> 4);
+              const uint32_t acc = fresh[t] ? 0u : 1u;
 #pragma unroll
               for (int h = 0; h < 2; ++h) {
-                ok = ok && wait(h ? &b.p_full[t] : &b.p_half[t], pv_n[j]);
+                ok = ok && wait(h ? &b.p_full[mine + t] : &b.p_half[mine + t], pv_n[t]);
                 if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
 #pragma unroll
-                  for (int k = 4 * h; k < 4 * h + 4; ++k)
-                    mma_bf16_ts(tmem + S::kO + DP * t, tmem + S::kP + S::kPStep * t + 8 * k,
-                                va + (k * 2048 >> 4), id_pv, k > 0 ? 1u : acc);
-                  if (h) mma_commit(&b.pv_done[t]);
+                  for (int k = h ? 4 : 0; k < (h ? kKeys / 16 : 4); ++k)
+                    mma_bf16_ts(tmem + S::kO + DP * (mine + t), tmem + S::kP + S::kPStep * (mine + t) + 8 * k, va + (k * 2048 >> 4), id_pv,
+                                k > 0 ? 1u : acc);
+                  if (h) mma_commit(&b.pv_done[mine + t]);
                 }
                 __syncwarp();
               }
               if (!ok) break;
-              fresh[j] = false;
-              ++pv_n[j];
+              fresh[t] = false;
+              ++pv_n[t];
             }
-            if (!S::kApart && more && tile_sees(tile[j], next)) qk(j, ks);
-            if (!ok) break;
+            if (!S::kApart && more && tile_sees(tile[t], next)) qk(t, ks);
           }
           if (!ok) break;
           if (elect_one()) {
@@ -459,16 +474,17 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         kv += 2 * n;
         ++q;
       }
-      if (elect_one()) mma_commit(&b.drain[first]);
+      if (elect_one()) mma_commit(&b.drain[mine]);
       __syncwarp();
-      drain_wait(&b.drain[first], 0);
+      drain_wait(&b.drain[mine], 0);
     }
   } else {
     regs_up<kSoftmaxRegs>();
     // ---------------- softmax and output: a warpgroup to a tile, a row to a thread
     const int wg = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t ts = tmem + lanes + S::kS + 128 * wg, tp = tmem + lanes + S::kP + S::kPStep * wg,
+    constexpr int PARTS = kKeys / 32;
+    const uint32_t ts = tmem + lanes + kKeys * wg, tp = tmem + lanes + S::kP + S::kPStep * wg,
                    to = tmem + lanes + S::kO + DP * wg;
     const float scale = fabsf(p.scale_log2);
     const float slack = 8.f / scale;                 // scores may outgrow the running maximum by 2^8
@@ -498,9 +514,9 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
       auto read = [&](float* s) {                    // the block's scores
         tc_fence_after();
 #pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_ld_32x32(ts + 32 * c, s + 32 * c);
+        for (int c = 0; c < PARTS; ++c) tmem_ld_32x32(ts + 32 * c, s + 32 * c);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_wait_ld_32(s + 32 * c);
+        for (int c = 0; c < PARTS; ++c) tmem_wait_ld_32(s + 32 * c);
       };
       auto scores_read = [&] {
         if (!S::kApart) return;
@@ -508,7 +524,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive(&b.s_free[wg]);
       };
-      auto stored = [&](uint64_t* bar) {             // half of the weights are in place
+      auto stored = [&](uint64_t* bar) {             // the weights so far are in place
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
@@ -525,10 +541,10 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
           w[e] = pack2<T>(x.x, x.y);
         }
       };
-      // Quarter c of block kb: true when no row of the warp sees any of it; else what a row does not see becomes -inf.
+      // Part c (32 keys) of block kb: true when no row of the warp sees any of it; else what a row does not see becomes -inf.
       const int sink = min(p.sinks, len);
       auto hide = [&](int kb, int c, float* s) {
-        const int j = kb * kTileK + 32 * c;
+        const int j = kb * kKeys + 32 * c;
         const int first_top = min(len - 1, tile_top + w0), last_top = min(len - 1, tile_top + w1);
         if (w1 < w0 || j > last_top || (j + 31 < tile_low + w0 && j >= sink)) return true;
         if (j + 31 > first_top || (j < tile_low + w1 && j + 32 > sink)) {
@@ -547,14 +563,14 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
       constexpr bool LOOSE = std::is_same<T, __nv_bfloat16>::value;
       auto guess = [&](int kb, auto edge) {
         constexpr bool EDGE = decltype(edge)::value;   // a block that not every row sees whole (bf16)
-        float s[128];
+        float s[kKeys];
         read(s);
         if (LOOSE) scores_read();
         const float off = -m * scale;
         const float2 off2 = make_float2(off, off);
         float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-        uint32_t w[32];
-        auto quarter = [&](int c, uint32_t* w) {
+        uint32_t w[LOOSE ? 1 : 2][16];
+        auto part = [&](int c, uint32_t* w) {
           if (EDGE && hide(kb, c, s + 32 * c)) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) w[e] = 0u;
@@ -562,32 +578,30 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
             weigh(s + 32 * c, off2, sum, w);
           }
         };
-        if (!LOOSE) {
-          float mx[4] = {s[0], s[1], s[2], s[3]};
+        part(0, w[0]);
+        if constexpr (!LOOSE) {
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int c = 4; c < 124; c += 8)
+          for (int c = 0; c < kKeys; c += 8)
 #pragma unroll
             for (int x = 0; x < 4; ++x) mx[x] = max3(mx[x], s[c + x], s[c + 4 + x]);
-          const float high = max3(max3(mx[0], mx[1], mx[2]), max3(mx[3], s[124], s[125]), fmaxf(s[126], s[127]));
-          quarter(0, w);
-          quarter(1, w + 16);
+          const float high = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
+          part(1, w[1]);
           if (!warp_all(high <= m + slack)) return false;
           scores_read();
-        } else {
-          quarter(0, w);
         }
         // the last product with these weights' columns, and into these outputs, is over
         ok = wait(&b.pv_done[wg], n - 1);
         if (!ok) return true;
         tc_fence_after();
-        tmem_st_32x16(tp, w);
-        if (LOOSE) quarter(1, w + 16);
-        tmem_st_32x16(tp + 16, w + 16);
-        quarter(2, w);
-        stored(&b.p_half[wg]);
-        tmem_st_32x16(tp + 32, w);
-        quarter(3, w + 16);
-        tmem_st_32x16(tp + 48, w + 16);
+        tmem_st_32x16(tp, w[0]);
+#pragma unroll
+        for (int c = 1; c < PARTS; ++c) {
+          uint32_t* x = LOOSE ? w[0] : w[c & 1];
+          if (LOOSE || c > 1) part(c, x);
+          if (c == 2) stored(&b.p_half[wg]);
+          tmem_st_32x16(tp + 16 * c, x);
+        }
         const float all = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
         l += all;
         stored(&b.p_full[wg]);
@@ -596,20 +610,20 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
       };
       // Any block.
       auto block = [&](int kb, bool start) {
-        float s[128];
+        float s[kKeys];
         read(s);
         scores_read();
         if (p.scale_log2 < 0.f) {
 #pragma unroll
-          for (int c = 0; c < 128; ++c) s[c] = -s[c];
+          for (int c = 0; c < kKeys; ++c) s[c] = -s[c];
         }
-        uint32_t hidden = 0;                         // quarters of the block that no row of the warp sees
+        uint32_t hidden = 0;                         // parts of the block that no row of the warp sees
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
+        for (int c = 0; c < PARTS; ++c)
           if (hide(kb, c, s + 32 * c)) hidden |= 1u << c;
         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
+        for (int c = 0; c < PARTS; ++c)
           if (!(hidden >> c & 1u)) {
 #pragma unroll
             for (int e = 0; e < 32; e += 8)
@@ -634,7 +648,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         const float off = m == -INFINITY ? 0.f : -m * scale;
         float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < PARTS; ++c) {
           uint32_t w[16];
           if (hidden >> c & 1u) {
 #pragma unroll
@@ -716,7 +730,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
       for (int64_t at = blockIdx.x; at < g.items; at += gridDim.x) {
         AttendItem it;
         if (!attend_item(p, g, at, it)) continue;
-        const AttendTile t = wg ? it.t[1] : it.t[0];
+        const AttendTile t = it.t[wg];
         bool again = false;
         if (row < t.n) {
           const T* out = reinterpret_cast<const T*>(p.out.data + (int64_t)(it.sq.q0 + t.row + row) * p.out.row_bytes +

@@ -133,13 +133,13 @@ bool rotary_args_ok(const gnn_rotary* rot, int dtype, int head_dim, int64_t n_ro
   return count_ok(n_rows) && (uintptr_t)positions % 4 == 0;
 }
 
-// Boxes of 128 rows x 64 elements of one head, in the 128-byte swizzle; what lies outside reads as zeros.
-bool encode_map(const gnn_attention* a, CUtensorMap* map, const gnn_heads& h, int64_t rows, int dtype, int dim) {
+// Boxes of box_rows rows x 64 elements of one head, in the 128-byte swizzle; what lies outside reads as zeros.
+bool encode_map(const gnn_attention* a, CUtensorMap* map, const gnn_heads& h, int64_t rows, int dtype, int dim, int box_rows) {
   const cuuint64_t size[3] = {(cuuint64_t)dim, (cuuint64_t)h.n_heads, (cuuint64_t)std::max<int64_t>(rows, 1)};
   const cuuint64_t one = (cuuint64_t)(dim * 2 + 15) / 16 * 16;      // for a dimension of one, whose stride is not used
   const cuuint64_t stride[2] = {h.n_heads > 1 ? (cuuint64_t)h.head_stride * 2 : one,
                                 rows > 1 ? (cuuint64_t)h.row_stride * 2 : one};
-  const cuuint32_t box[3] = {64, 1, 128}, step[3] = {1, 1, 1};
+  const cuuint32_t box[3] = {64, 1, (cuuint32_t)box_rows}, step[3] = {1, 1, 1};
   return a->encode(map, dtype == GNN_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
                    h.data, size, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -157,19 +157,20 @@ cudaError_t launch_attend(unsigned grid, cudaStream_t st, const AttendParams& p,
 
 int run_tiles(gnn_attention* a, const gnn_attention_call* c, const gnn_heads* views, const AttendParams& p,
               cudaStream_t st) {
-  CUtensorMap maps[3];
-  if (!encode_map(a, &maps[0], views[0], c->n_q_rows, c->dtype, c->head_dim) ||
-      !encode_map(a, &maps[1], views[1], c->n_kv_rows, c->dtype, c->head_dim) ||
-      !encode_map(a, &maps[2], views[2], c->n_kv_rows, c->dtype, c->head_dim))
-    return GNN_ERR_INVALID_ARG;
   AttendGrid g = {};
-  // Two tiles share the keys that are loaded, but a tile alone in its block is faster: worth it while there are SMs
-  // for all of them (event of 2,000 hits, 32 tiles: 13.8 -> 11.7 us).
-  g.single = (c->n_q_rows / kTileQ + c->n_seqs) * p.heads <= a->n_sm;
-  g.pair_heads = !g.single && p.heads / p.kv_heads % 2 == 0;
-  g.rows = g.single || g.pair_heads ? kTileQ : 2 * kTileQ;
-  g.heads = g.pair_heads ? p.heads / 2 : p.heads;
-  g.items = (c->n_q_rows / g.rows + c->n_seqs) * g.heads;
+  g.group = p.heads / p.kv_heads;
+  // A block's tiles share the keys that are loaded, but fewer in a block are faster: as few as keep all SMs busy
+  // (event of 2,000 hits, 32 tiles, one or two to a block: 11.7 and 13.8 us).
+  const int64_t tiles = (c->n_q_rows / kTileQ + c->n_seqs) * p.heads;
+  g.tiles = (int)std::min<int64_t>(kMostTiles, std::max<int64_t>(1, (tiles + a->n_sm - 1) / a->n_sm));
+  const int64_t slots = (c->n_q_rows / kTileQ + c->n_seqs) * g.group / g.tiles + c->n_seqs;
+  if ((c->n_q_rows / kTileQ + c->n_seqs) * g.group + c->n_seqs >= (int64_t)1 << 31) return GNN_ERR_INVALID_ARG;
+  g.items = slots * p.kv_heads;
+  CUtensorMap maps[3];
+  if (!encode_map(a, &maps[0], views[0], c->n_q_rows, c->dtype, c->head_dim, kTileQ) ||
+      !encode_map(a, &maps[1], views[1], c->n_kv_rows, c->dtype, c->head_dim, kKeys) ||
+      !encode_map(a, &maps[2], views[2], c->n_kv_rows, c->dtype, c->head_dim, kKeys))
+    return GNN_ERR_INVALID_ARG;
   const unsigned grid = (unsigned)std::min<int64_t>(g.items, a->n_sm);
   cudaError_t err;
   if (c->dtype == GNN_DTYPE_BF16)
@@ -333,7 +334,7 @@ int gnn_attention_run(gnn_attention* att, const gnn_attention_call* c, gnn_strea
   for (const gnn_heads& v : views)
     if (!view_ok(&v, c->dtype) || (uintptr_t)v.data % 16 || v.row_stride % 8 || v.head_stride % 8)
       return GNN_ERR_INVALID_ARG;
-  if (c->n_seqs > 1 << 30) return GNN_ERR_INVALID_ARG;
+  if (c->n_seqs > 1 << 30 || c->q.n_heads > 4096) return GNN_ERR_INVALID_ARG;
   for (const gnn_heads& v : views)                 // one row or head for several is not a view that can be read here
     if ((v.n_heads > 1 && v.head_stride == 0) || v.row_stride == 0) return GNN_ERR_INVALID_ARG;
   if (c->k.n_heads != c->v.n_heads || c->q.n_heads != c->out.n_heads || c->q.n_heads % c->k.n_heads)

@@ -134,7 +134,7 @@ def rope(rot: Rotary, x, positions=None, out=None, stream=None):
     dtype, number, device, dim = _kind(x)
     n = x.shape[0]
     if out is None:
-        out = _torch.empty(x.shape, dtype=dtype, device=x.device)
+        out = _torch.empty_like(x)
     assert out.shape == x.shape
     pos, real = _positions(positions, n, device)
     if n == 0:
@@ -157,11 +157,11 @@ def qk_norm_rope(rot: Rotary, q, k, positions=None, v=None, q_gain=None, k_gain=
     assert rows is None or (k_out is not None and (v is None or v_out is not None)), "rows need k_out and v_out"
     assert v is not None or v_out is None, "v_out without v"
     if q_out is None:
-        q_out = _torch.empty(q.shape, dtype=dtype, device=q.device)
+        q_out = _torch.empty_like(q)
     if k_out is None:
-        k_out = _torch.empty(k_shape, dtype=dtype, device=q.device)
+        k_out = _torch.empty_like(k)
     if v is not None and v_out is None:
-        v_out = _torch.empty(k_shape, dtype=dtype, device=q.device)
+        v_out = _torch.empty_like(v)
     m = k_out.shape[0]
     assert q_out.shape == q.shape and (rows is not None or m == n), "outputs of other sizes"
     assert v is None or v_out.shape[0] == m, "k_out and v_out differ"
@@ -201,7 +201,7 @@ class WindowAttention:
         sinks: first keys that stay visible; max_q, max_kv: the most queries and keys of a sequence, when known."""
         dtype, number, device, dim = _kind(q)
         if out is None:
-            out = _torch.empty(q.shape, dtype=dtype, device=q.device)
+            out = _torch.empty_like(q)
         n, int32, rows = q_start.numel() - 1, _torch.int32, k.shape[0]
         assert n >= 0 and out.shape == q.shape and v.shape[0] == rows, "outputs, keys or values of other sizes"
         _CALL.pack_into(_AREA, 0, number, dim, *_heads(q, dtype, device, dim), *_heads(k, dtype, device, dim),
