@@ -38,6 +38,8 @@ class GnnAttentionCall(ctypes.Structure):
 
 
 _HEADS = struct.Struct("PqqiI")                              # GnnHeads
+_TWO, _SIX = struct.Struct("PqqiI" * 2), struct.Struct("PqqiI" * 6)
+_NONE = (0, 0, 0, 0, 0)
 _CALL = struct.Struct("ii" + "PqqiI" * 4 + "PPPqqiiiiiifi")   # GnnAttentionCall
 assert _HEADS.size == ctypes.sizeof(GnnHeads) and _CALL.size == ctypes.sizeof(GnnAttentionCall)
 _AREA = ctypes.create_string_buffer(max(6 * _HEADS.size, _CALL.size))
@@ -139,8 +141,7 @@ def rope(rot: Rotary, x, positions=None, out=None, stream=None):
     pos, real = _positions(positions, n, device)
     if n == 0:
         return out
-    _HEADS.pack_into(_AREA, 0, *_heads(x, dtype, device, dim))
-    _HEADS.pack_into(_AREA, _HEADS.size, *_heads(out, dtype, device, dim))
+    _TWO.pack_into(_AREA, 0, *_heads(x, dtype, device, dim), *_heads(out, dtype, device, dim))
     rc = _lib.gnn_rope(rot.address, number, dim, _AT[0], _AT[1], pos, real, n, _stream(stream, device))
     if rc != GNN_OK:
         raise GnnError(rc, "gnn_rope")
@@ -171,13 +172,17 @@ def qk_norm_rope(rot: Rotary, q, k, positions=None, v=None, q_gain=None, k_gain=
     if n == 0:
         return q_out, k_out, v_out
     assert m > 0, "k_out has no rows"
-    size = _HEADS.size
-    for i, x in enumerate((q, k, v, q_out, k_out, v_out)):
-        if x is not None:
-            _HEADS.pack_into(_AREA, i * size, *_heads(x, dtype, device, dim))
     a = _AT
-    rc = _lib.gnn_qk_norm_rope(rot.address, number, dim, eps, gq, gk, a[0], a[1], a[2] if v is not None else None, a[3], a[4],
-                               a[5] if v is not None else None, pos, real, at, m, n, _stream(stream, device))
+    if v is None:
+        _SIX.pack_into(_AREA, 0, *_heads(q, dtype, device, dim), *_heads(k, dtype, device, dim), *_NONE,
+                       *_heads(q_out, dtype, device, dim), *_heads(k_out, dtype, device, dim), *_NONE)
+    else:
+        _SIX.pack_into(_AREA, 0, *_heads(q, dtype, device, dim), *_heads(k, dtype, device, dim), *_heads(v, dtype, device, dim),
+                       *_heads(q_out, dtype, device, dim), *_heads(k_out, dtype, device, dim),
+                       *_heads(v_out, dtype, device, dim))
+    values, values_out = (None, None) if v is None else (a[2], a[5])
+    rc = _lib.gnn_qk_norm_rope(rot.address, number, dim, eps, gq, gk, a[0], a[1], values, a[3], a[4], values_out, pos, real, at,
+                               m, n, _stream(stream, device))
     if rc != GNN_OK:
         raise GnnError(rc, "gnn_qk_norm_rope")
     return q_out, k_out, v_out
