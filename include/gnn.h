@@ -445,7 +445,8 @@ int gnn_qk_norm_rope(const gnn_rotary* rot, int dtype, int head_dim, float eps, 
  *                   fp32, the weights that multiply v are rounded to dtype (their sum is not)
  *   head_dim        a multiple of 8, 8..128
  *   q, k, v, out    views of n_q_rows (q, out) and n_kv_rows (k, v) rows; data 16-byte aligned, strides
- *                   positive multiples of 8 elements below 2^39; q.n_heads a multiple of k.n_heads == v.n_heads.
+ *                   positive multiples of 8 elements below 2^39; q.n_heads a multiple of k.n_heads == v.n_heads,
+ *                   at most 4096.
  *                   out overlaps no input
  *   q_start         device int32 [n_seqs + 1], not decreasing; rows before the first and from the last on are
  *                   not written
@@ -456,7 +457,7 @@ int gnn_qk_norm_rope(const gnn_rotary* rot, int dtype, int head_dim, float eps, 
  * gnn_attention_status.  Enqueued on `stream`; only enqueues kernels (it can be captured).  The same inputs
  * give bitwise-identical outputs.
  * Errors: INVALID_ARG (null pointer, any limit above, scale not finite, sinks < 0, sizes above GNN_MAX_COUNT,
- * n_seqs above 2^30), CUDA.
+ * n_seqs above 2^28, 2^31 or more tiles of 128 queries for one key head), CUDA.
  *
  * gnn_attention_create -- a handle on the current device: the workspace of calls with few queries and the
  * device error word.  Synchronous.  One handle per stream: it is not safe for concurrent use.  Errors:

@@ -13,6 +13,11 @@
 //
 // The work is split by what there is: every block sums up the sequences' lengths and takes an equal share of
 // all units of 64 keys, so that sequences of different lengths leave no SM idle.
+//
+// 64 sequences of 4,096 to 8,192 keys, 16 query and 4 key heads of 128, one query each: 0.127 ms, 6.4 TB/s, 94 % of the
+// copy rate; eight of up to 131,072 with three queries (16 rows, 249 registers, eight warps to an SM): 0.155 ms,
+// 5.3 TB/s.  One query over 1,028 keys: 9.3 us, seven of them dependent loads and the join.  Blocks of a fixed number
+// of keys with the rows along M took 0.230 and 0.485 ms and 16.6 us.
 #pragma once
 #include "attend_tile.cuh"
 
@@ -292,9 +297,9 @@ __global__ void __launch_bounds__(32 * kFewWarps, NR == 2 && NC > 2 ? 2 : 3)
         for (int e = 0; e < NV; ++e)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {              // columns 2i and 2i + 1 of every lane's piece
-            const uint32_t a[4] = {
-                __byte_perm(word(v[0][e], i), word(v[1][e], i), 0x5410), __byte_perm(word(v[0][e], i), word(v[1][e], i), 0x7632),
-                __byte_perm(word(v[2][e], i), word(v[3][e], i), 0x5410), __byte_perm(word(v[2][e], i), word(v[3][e], i), 0x7632)};
+            const uint32_t v0 = word(v[0][e], i), v1 = word(v[1][e], i), v2 = word(v[2][e], i), v3 = word(v[3][e], i);
+            const uint32_t a[4] = {__byte_perm(v0, v1, 0x5410), __byte_perm(v0, v1, 0x7632), __byte_perm(v2, v3, 0x5410),
+                                   __byte_perm(v2, v3, 0x7632)};
 #pragma unroll
             for (int r = 0; r < NR; ++r) mma_16x8x16(o[e][i][r], a, w[r][0], w[r][1], T());
           }
@@ -321,8 +326,10 @@ __global__ void __launch_bounds__(32 * kFewWarps, NR == 2 && NC > 2 ? 2 : 3)
 #pragma unroll
         for (int e = 0; e < NV; ++e) {
           float* dst = &o_s[warp][row][8 * (g + 8 * e)];
-          *reinterpret_cast<float4*>(dst) = make_float4(o[e][0][r][x], o[e][0][r][x + 2], o[e][1][r][x], o[e][1][r][x + 2]);
-          *reinterpret_cast<float4*>(dst + 4) = make_float4(o[e][2][r][x], o[e][2][r][x + 2], o[e][3][r][x], o[e][3][r][x + 2]);
+#pragma unroll
+          for (int i = 0; i < 4; i += 2)
+            *reinterpret_cast<float4*>(dst + 2 * i) =
+                make_float4(o[e][i][r][x], o[e][i][r][x + 2], o[e][i + 1][r][x], o[e][i + 1][r][x + 2]);
         }
       }
     __syncthreads();
@@ -334,7 +341,8 @@ __global__ void __launch_bounds__(32 * kFewWarps, NR == 2 && NC > 2 ? 2 : 3)
                   (int64_t)(kv * G + (row0 + r) % G) * p.out.head_bytes;
       const float inv = sum == 0.f ? 0.f : 1.f / sum;
       if (sum == 0.f) val = make_float4(0.f, 0.f, 0.f, 0.f);
-      *reinterpret_cast<uint2*>(out + 2 * d) = make_uint2(pack2<T>(val.x * inv, val.y * inv), pack2<T>(val.z * inv, val.w * inv));
+      *reinterpret_cast<uint2*>(out + 2 * d) =
+          make_uint2(pack2<T>(val.x * inv, val.y * inv), pack2<T>(val.z * inv, val.w * inv));
     };
     const int quads = p.dim / 4;
     for (int x = threadIdx.x; x < rows * quads; x += 32 * kFewWarps) {

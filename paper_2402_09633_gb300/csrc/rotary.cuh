@@ -15,9 +15,9 @@
 // Bound by HBM: every element is read and written once.  A group of lanes owns a row of units for two heads of a
 // token, so that a thread has up to 64 bytes on their way, and little else: an angle's sine and cosine are used
 // for both heads and forgotten, and computed again for the token's next two.  Keeping them through all heads took
-// 118 registers and left 15 warps to an SM (rotation of 300,000 rows of two bf16 heads of 64: 43 us, 28 now; with norms,
-// keys and values 137 us, 77 now: 81 % and 89 % of the copy rate).  Queries, keys and values are different blocks' work;
-// frequencies and gains lie in shared memory.
+// 118 registers and left 15 warps to an SM.  Queries, keys and values are different blocks' work; frequencies and
+// gains lie in shared memory.  300,000 rows of two bf16 heads of 64: 28 us, 81 % of the copy rate (43 us with the
+// angles kept); with norms, keys and values 77 us, 89 % (137 us).
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -64,9 +64,11 @@ struct alignas(sizeof(T) * N < 16 ? sizeof(T) * N : 16) Pack {
   T v[N];
   __device__ __forceinline__ float2 get2(int i) const { return make_float2(to_f(v[i]), to_f(v[i + 1])); }
   __device__ __forceinline__ void set2(int i, float2 x) {
-    if constexpr (std::is_same<T, __nv_bfloat16>::value) *reinterpret_cast<__nv_bfloat162*>(v + i) = __floats2bfloat162_rn(x.x, x.y);
-    else if constexpr (std::is_same<T, __half>::value) *reinterpret_cast<__half2*>(v + i) = __floats2half2_rn(x.x, x.y);
-    else {
+    if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+      *reinterpret_cast<__nv_bfloat162*>(v + i) = __floats2bfloat162_rn(x.x, x.y);
+    } else if constexpr (std::is_same<T, __half>::value) {
+      *reinterpret_cast<__half2*>(v + i) = __floats2half2_rn(x.x, x.y);
+    } else {
       v[i] = x.x;
       v[i + 1] = x.y;
     }

@@ -134,7 +134,8 @@ bool rotary_args_ok(const gnn_rotary* rot, int dtype, int head_dim, int64_t n_ro
 }
 
 // Boxes of box_rows rows x 64 elements of one head, in the 128-byte swizzle; what lies outside reads as zeros.
-bool encode_map(const gnn_attention* a, CUtensorMap* map, const gnn_heads& h, int64_t rows, int dtype, int dim, int box_rows) {
+bool encode_map(const gnn_attention* a, CUtensorMap* map, const gnn_heads& h, int64_t rows, int dtype, int dim,
+                int box_rows) {
   const cuuint64_t size[3] = {(cuuint64_t)dim, (cuuint64_t)h.n_heads, (cuuint64_t)std::max<int64_t>(rows, 1)};
   const cuuint64_t one = (cuuint64_t)(dim * 2 + 15) / 16 * 16;      // for a dimension of one, whose stride is not used
   const cuuint64_t stride[2] = {h.n_heads > 1 ? (cuuint64_t)h.head_stride * 2 : one,
@@ -334,7 +335,7 @@ int gnn_attention_run(gnn_attention* att, const gnn_attention_call* c, gnn_strea
   for (const gnn_heads& v : views)
     if (!view_ok(&v, c->dtype) || (uintptr_t)v.data % 16 || v.row_stride % 8 || v.head_stride % 8)
       return GNN_ERR_INVALID_ARG;
-  if (c->n_seqs > 1 << 30 || c->q.n_heads > 4096) return GNN_ERR_INVALID_ARG;
+  if (c->n_seqs > 1 << 28 || c->q.n_heads > 4096) return GNN_ERR_INVALID_ARG;
   for (const gnn_heads& v : views)                 // one row or head for several is not a view that can be read here
     if ((v.n_heads > 1 && v.head_stride == 0) || v.row_stride == 0) return GNN_ERR_INVALID_ARG;
   if (c->k.n_heads != c->v.n_heads || c->q.n_heads != c->out.n_heads || c->q.n_heads % c->k.n_heads)
@@ -361,6 +362,8 @@ int gnn_attention_run(gnn_attention* att, const gnn_attention_call* c, gnn_strea
   p.err = att->d_err;
   const int64_t max_q = c->max_q > 0 ? std::min<int64_t>(c->max_q, c->n_q_rows) : c->n_q_rows;
   const int group = p.heads / p.kv_heads;
+  // Few rows for each key head go by mma.sync, which reads the keys once for 16 of them; a tile of 128 rows would be
+  // mostly empty, and one sequence's keys one block's work.
   if (max_q * group <= 2 * kFewRows && (int64_t)p.n_seqs * p.kv_heads <= 1 << 24)
     return run_few(att, c, p, max_q, (cudaStream_t)stream);
   return run_tiles(att, c, views, p, (cudaStream_t)stream);

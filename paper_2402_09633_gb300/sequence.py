@@ -177,12 +177,12 @@ def qk_norm_rope(rot: Rotary, q, k, positions=None, v=None, q_gain=None, k_gain=
         _SIX.pack_into(_AREA, 0, *_heads(q, dtype, device, dim), *_heads(k, dtype, device, dim), *_NONE,
                        *_heads(q_out, dtype, device, dim), *_heads(k_out, dtype, device, dim), *_NONE)
     else:
-        _SIX.pack_into(_AREA, 0, *_heads(q, dtype, device, dim), *_heads(k, dtype, device, dim), *_heads(v, dtype, device, dim),
-                       *_heads(q_out, dtype, device, dim), *_heads(k_out, dtype, device, dim),
-                       *_heads(v_out, dtype, device, dim))
+        _SIX.pack_into(_AREA, 0, *_heads(q, dtype, device, dim), *_heads(k, dtype, device, dim),
+                       *_heads(v, dtype, device, dim), *_heads(q_out, dtype, device, dim),
+                       *_heads(k_out, dtype, device, dim), *_heads(v_out, dtype, device, dim))
     values, values_out = (None, None) if v is None else (a[2], a[5])
-    rc = _lib.gnn_qk_norm_rope(rot.address, number, dim, eps, gq, gk, a[0], a[1], values, a[3], a[4], values_out, pos, real, at,
-                               m, n, _stream(stream, device))
+    rc = _lib.gnn_qk_norm_rope(rot.address, number, dim, eps, gq, gk, a[0], a[1], values, a[3], a[4], values_out, pos,
+                               real, at, m, n, _stream(stream, device))
     if rc != GNN_OK:
         raise GnnError(rc, "gnn_qk_norm_rope")
     return q_out, k_out, v_out
