@@ -5,8 +5,8 @@
 // stay on the old m, above 1 if need be.  Only blocks that some row of the tile sees are loaded; of those, parts that
 // no row of a warp sees cost no exponentials.
 //
-// What bounds it (event of 300,000 hits, two bf16 heads of 64, 512 neighbours to each side: 0.215 ms, 744 TFLOP/s of
-// visible products, tensor cores 35 % busy; causal 16,384, heads of 128, window 4,096: 0.187 ms, 1,320 TFLOP/s, 60 %):
+// What bounds it (event of 300,000 hits, two bf16 heads of 64, 512 neighbours to each side: 0.214 ms, 748 TFLOP/s of
+// visible products, tensor cores 35 % busy; causal 16,384, heads of 128, window 4,096: 0.183 ms, 1,350 TFLOP/s, 60 %):
 // a block's softmax is one chain of 1,300 cycles in a warp with 512 of them exponentials, two warps share a scheduler,
 // and tensor memory holds no third tile beside two.  Other splits lost: 16 rows to a warp in sixteen warps 0.36 ms,
 // two threads to a row 0.25, three tiles of 96 keys 0.26, one warp that issues whatever is ready 0.36 (its polls take
@@ -570,57 +570,85 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         }
         return false;
       };
-      // A block on the guess that its scores do not outgrow the running maximum (which they
-      // rarely do after the first block).  In bf16 nothing depends on the guess: weights above 1 lose no precision,
-      // their sum tells whether the next block has to look for the maximum, and only scores that outgrow it by 2^100
-      // in one block would overflow, in a row that is then not finite and done again.  In fp16, whose weights end at
-      // 2^16, the maximum is computed beside the weights: false, with nothing changed, when the guess was wrong.
+      // Blocks on the guess that their scores do not outgrow the running maximum (which they rarely do after the first).
+      // In bf16 nothing depends on the guess: weights above 1 lose no precision, their sum tells whether the next block
+      // has to look for the maximum, and only scores that outgrow it by 2^100 in one block would overflow, in a row
+      // that is then not finite and done again.  In fp16, whose weights end at 2^16, the maximum is computed beside
+      // the weights of a block that every row sees whole: false, with nothing changed, when the guess was wrong.
       constexpr bool LOOSE = std::is_same<T, __nv_bfloat16>::value;
-      auto guess = [&](int kb, auto edge) {
-        constexpr bool EDGE = decltype(edge)::value;   // a block that not every row sees whole (bf16)
-        float s[kKeys];
-        read(s);
-        if (LOOSE) scores_read();
+      auto loose = [&](int kb, auto edge) {
+        constexpr bool EDGE = decltype(edge)::value;   // a block that not every row sees whole
         const float off = -m * scale;
         const float2 off2 = make_float2(off, off);
         float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-        uint32_t w[LOOSE ? 1 : 2][16];
-        auto part = [&](int c, uint32_t* w) {
-          if (EDGE && hide(kb, c, s + 32 * c)) {
+        tc_fence_after();
+        // 64 keys at a time, or 32 where the first weights' product waits for them, in a loop: the code of all 128 in one
+        // piece misses the instruction caches.
+        constexpr int STEP = S::kApart ? 2 : 1;
+#pragma unroll 1
+        for (int c0 = 0; c0 < PARTS; c0 += STEP) {
+          float s[32 * STEP];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) w[e] = 0u;
-          } else {
-            weigh(s + 32 * c, off2, sum, w);
+          for (int c = 0; c < STEP; ++c) tmem_ld_32x32(ts + 32 * (c0 + c), s + 32 * c);
+#pragma unroll
+          for (int c = 0; c < STEP; ++c) tmem_wait_ld_32(s + 32 * c);
+          if (c0 + STEP == PARTS) scores_read();
+#pragma unroll
+          for (int c = 0; c < STEP; ++c) {
+            uint32_t w[16];
+            if (EDGE && hide(kb, c0 + c, s + 32 * c)) {
+#pragma unroll
+              for (int e = 0; e < 16; ++e) w[e] = 0u;
+            } else {
+              weigh(s + 32 * c, off2, sum, w);
+            }
+            if (c == 0 && c0 == 0) {
+              // the last product with these weights' columns, and into these outputs, is over
+              ok = wait(&b.pv_done[wg], n - 1);
+              if (!ok) return true;
+              tc_fence_after();
+            }
+            if (!S::kApart && c0 == 2) stored(&b.p_half[wg]);
+            tmem_st_32x16(tp + 16 * (c0 + c), w);
           }
-        };
-        part(0, w[0]);
-        if constexpr (!LOOSE) {
-          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-          for (int c = 0; c < kKeys; c += 8)
-#pragma unroll
-            for (int x = 0; x < 4; ++x) mx[x] = max3(mx[x], s[c + x], s[c + 4 + x]);
-          const float high = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
-          part(1, w[1]);
-          if (!warp_all(high <= m + slack)) return false;
-          scores_read();
+          if (S::kApart) stored(c0 ? &b.p_full[wg] : &b.p_half[wg]);
         }
-        // the last product with these weights' columns, and into these outputs, is over
+        const float all = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+        l += all;
+        if (!S::kApart) stored(&b.p_full[wg]);
+        plain = warp_all(all <= 256.f || row >= rows);
+        return true;
+      };
+      auto guess = [&]() {
+        float s[kKeys];
+        read(s);
+        const float off = -m * scale;
+        const float2 off2 = make_float2(off, off);
+        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        uint32_t w[2][16];
+        weigh(s, off2, sum, w[0]);
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int c = 0; c < kKeys; c += 8)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) mx[x] = max3(mx[x], s[c + x], s[c + 4 + x]);
+        const float high = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
+        weigh(s + 32, off2, sum, w[1]);
+        if (!warp_all(high <= m + slack)) return false;
+        scores_read();
         ok = wait(&b.pv_done[wg], n - 1);
         if (!ok) return true;
         tc_fence_after();
         tmem_st_32x16(tp, w[0]);
+        tmem_st_32x16(tp + 16, w[1]);
 #pragma unroll
-        for (int c = 1; c < PARTS; ++c) {
-          uint32_t* x = LOOSE ? w[0] : w[c & 1];
-          if (LOOSE || c > 1) part(c, x);
+        for (int c = 2; c < PARTS; ++c) {
+          weigh(s + 32 * c, off2, sum, w[c & 1]);
           if (c == 2) stored(&b.p_half[wg]);
-          tmem_st_32x16(tp + 16 * c, x);
+          tmem_st_32x16(tp + 16 * c, w[c & 1]);
         }
-        const float all = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-        l += all;
+        l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
         stored(&b.p_full[wg]);
-        if (LOOSE) plain = warp_all(all <= 256.f || row >= rows);
         return true;
       };
       // Any block.
@@ -685,7 +713,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         if (!ok) break;
         if (plain && p.scale_log2 >= 0.f) {
           const bool whole = kb < whole_hi && (kb >= whole_lo || kb < whole_sinks);
-          if (whole ? guess(kb, std::false_type()) : LOOSE && guess(kb, std::bool_constant<LOOSE>())) {
+          if (LOOSE ? (whole ? loose(kb, std::false_type()) : loose(kb, std::true_type())) : whole && guess()) {
             if (!ok) break;
             continue;
           }
