@@ -193,6 +193,34 @@ cudaError_t launch_few(unsigned grid, cudaStream_t st, const AttendParams& p, co
   }
 }
 
+// The most keys that queries of one sequence see.
+int64_t most_keys(const gnn_attention_call* c, const AttendParams& p, int64_t max_q) {
+  int64_t keys = c->kv_len ? c->n_kv_rows : max_q;
+  if (c->max_kv > 0) keys = std::min<int64_t>(keys, c->max_kv);
+  if (p.left >= 0 && p.right >= 0) keys = std::min<int64_t>(keys, (int64_t)p.sinks + p.left + p.right + max_q);
+  return keys;
+}
+
+// Whether the rows by mma.sync, which stream a sequence's keys once for every 16 of them and spread them over all SMs,
+// take less time than tiles of 128 queries, each of which has one block go through its keys.  Measured: a stream takes
+// 5.9 GB/ms behind 6 us (11 with 16 rows to a tile); a block of 128 keys takes a tile 0.83 us (heads up to 64) or 1.23
+// behind 6.5 us, two tiles in one block half as much again.  32 queries of four heads over one cache of 65,536 keys, two key heads of 128: 92 and 631 us; 64 caches of 8,192,
+// 16 queries: 373 and 194.
+bool few_is_faster(const gnn_attention* a, const gnn_attention_call* c, const AttendParams& p, int64_t max_q) {
+  const double group = p.heads / p.kv_heads, seqs = p.n_seqs, rows = max_q * group;
+  if (seqs * p.kv_heads > 1 << 24 || rows > 1 << 20) return false;
+  double keys = (double)most_keys(c, p, max_q);
+  if (c->kv_len && c->max_kv == 0) keys = std::min(keys, (double)c->n_kv_rows / seqs + 1);   // evenly shared, for want of better
+  const double streams = std::ceil(rows / (rows > 8 ? 16 : 8));
+  const double few = (rows > 8 ? 11 : 6) + streams * seqs * keys * p.kv_heads * p.dim * 4 / 5.9e6;
+  const double tiles = std::min((double)c->n_q_rows / kTileQ + seqs, seqs * std::ceil(max_q / (double)kTileQ)) * p.heads;
+  const double per = p.dim <= 64 ? 0.83 : 1.23;
+  // a causal tile of a long sequence sees half of it
+  const double blocks = std::ceil((p.left < 0 && p.right >= 0 && !c->kv_len ? keys / 2 : keys) / kKeys);
+  const double rounds = tiles <= a->n_sm ? 1 : 1.5 * std::ceil(tiles / 2 / a->n_sm);
+  return few <= 6.5 + rounds * blocks * per;
+}
+
 // Few queries to a sequence: one round of blocks, which share the keys out among them.
 int run_few(gnn_attention* a, const gnn_attention_call* c, const AttendParams& p, int64_t max_q, cudaStream_t st) {
   FewGrid f = {};
@@ -203,9 +231,7 @@ int run_few(gnn_attention* a, const gnn_attention_call* c, const AttendParams& p
   f.parts = a->d_parts;
   f.tickets = a->d_tickets;
   // no more blocks than there are units of keys, where the keys are known to be few
-  int64_t keys = c->kv_len ? c->n_kv_rows : max_q;
-  if (c->max_kv > 0) keys = std::min<int64_t>(keys, c->max_kv);
-  if (p.left >= 0 && p.right >= 0) keys = std::min<int64_t>(keys, (int64_t)p.sinks + p.left + p.right + max_q);
+  const int64_t keys = most_keys(c, p, max_q);
   const int64_t units = (int64_t)p.n_seqs * p.kv_heads * f.row_tiles * ((keys + kFewUnit) / kFewUnit);
   const unsigned grid = (unsigned)std::min<int64_t>(units, (int64_t)a->n_sm * (sixteen && p.dim > 64 ? 2 : 3));
   const cudaError_t err = c->dtype == GNN_DTYPE_BF16 ? launch_few<__nv_bfloat16>(grid, st, p, f, sixteen)
@@ -361,10 +387,7 @@ int gnn_attention_run(gnn_attention* att, const gnn_attention_call* c, gnn_strea
   p.scale_log2 = c->scale == 0.f ? 1e-30f : (float)((double)c->scale * 1.4426950408889634);
   p.err = att->d_err;
   const int64_t max_q = c->max_q > 0 ? std::min<int64_t>(c->max_q, c->n_q_rows) : c->n_q_rows;
-  const int group = p.heads / p.kv_heads;
-  // Few rows for each key head go by mma.sync, which reads the keys once for 16 of them; a tile of 128 rows would be
-  // mostly empty, and one sequence's keys one block's work.
-  if (max_q * group <= 2 * kFewRows && (int64_t)p.n_seqs * p.kv_heads <= 1 << 24)
+  if (few_is_faster(att, c, p, max_q))
     return run_few(att, c, p, max_q, (cudaStream_t)stream);
   return run_tiles(att, c, views, p, (cudaStream_t)stream);
 }

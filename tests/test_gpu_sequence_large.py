@@ -65,3 +65,16 @@ def test_a_row_that_is_not_finite_costs_only_itself():
     k2[333:833] = math.inf
     got = _attend(q, k2, v2, _starts(lengths), None, None, 100, 100, 4)
     assert torch.equal(got[:333], clean[:333]) and torch.equal(got[833:], clean[833:])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("H,K,nq", [(4, 1, 4), (2, 2, 3), (16, 2, 5)])
+def test_new_queries_that_see_different_keys(dtype, H, K, nq):
+    """Several new queries of a sequence: a key that one of them sees may hold anything for the others."""
+    n = 777
+    q, k, v = (_rand(r, h, 64, dtype=dtype, seed=h + r) for r, h in ((nq, H), (n, K), (n, K)))
+    v[n - 1, 0, 5] = math.nan                                # the last query's own key
+    v[n - 2, 0] = math.inf                                   # seen by the last two
+    k[n - nq - 50] = math.nan                                # at the left edge of the first
+    _attend(q, k, v, [0, nq], [0], [n], 50, 0, 0, max_q=nq, max_kv=n)
+    _attend(q, k, v, [0, nq], [0], [n], 50, 0, 3, max_q=nq, max_kv=n)
