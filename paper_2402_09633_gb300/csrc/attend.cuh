@@ -15,6 +15,7 @@ struct AttendParams {
   const int* kv_start;               // [n_seqs], or null: q_start
   const int* kv_len;                 // [n_seqs], or null: as many as queries
   int n_q_rows, n_kv_rows, n_seqs;
+  int max_q;                         // queries of a sequence, at most
   int heads, kv_heads, dim;
   int left, right, sinks;
   float scale_log2;                  // scale * log2(e)

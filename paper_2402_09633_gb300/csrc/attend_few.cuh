@@ -30,7 +30,6 @@ constexpr int kFewPadded = 8;        // shares up to which blocks have parts of 
 
 struct FewGrid {
   int group;                         // query heads to a key head
-  int max_q;                         // queries of a sequence, at most
   int row_tiles;
   float* parts;                      // [block][2]: a tile's outputs [rows][dim], maxima [rows] and sums [rows]
   int* tickets;                      // [block], zero between calls: of the tile that starts in the block and goes on
@@ -122,7 +121,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, NR == 2 && NC > 2 ? 2 : 3)
       if (b < p.n_seqs) {
         bool bad;
         const Sequence sq = sequence(p, b, &bad);
-        if ((bad || sq.nq > f.max_q) && blockIdx.x == 0) atomicOr(p.err, DEV_ERR_INDEX_RANGE);
+        if ((bad || sq.nq > p.max_q) && blockIdx.x == 0) atomicOr(p.err, DEV_ERR_INDEX_RANGE);
         if (b < 32 * kFewWarps) seq_s[b] = sq;
         u = few_units(p, sq);
       }
@@ -155,9 +154,9 @@ __global__ void __launch_bounds__(32 * kFewWarps, NR == 2 && NC > 2 ? 2 : 3)
   auto process = [&](int b, int kr, int v0, int v1, int units, int64_t u0) {
     bool bad = false;
     const Sequence sq = balanced && b < 32 * kFewWarps ? seq_s[b] : sequence(p, b, &bad);
-    if (!balanced && (bad || sq.nq > f.max_q) && threadIdx.x == 0) atomicOr(p.err, DEV_ERR_INDEX_RANGE);
+    if (!balanced && (bad || sq.nq > p.max_q) && threadIdx.x == 0) atomicOr(p.err, DEV_ERR_INDEX_RANGE);
     const int rt = kr % f.row_tiles, kv = kr / f.row_tiles, row0 = rt * ROWS;
-    const int rows = min(min(sq.nq, f.max_q) * G - row0, ROWS);
+    const int rows = min(min(sq.nq, p.max_q) * G - row0, ROWS);
     if (rows <= 0) return;
     const FewKeys keys = few_keys(p, sq);
     const int pos0 = sq.len - sq.nq, pos_first = pos0 + row0 / G, pos_last = pos0 + (row0 + rows - 1) / G;

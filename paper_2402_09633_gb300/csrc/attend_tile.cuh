@@ -366,12 +366,12 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
 #pragma unroll 1
       for (uint32_t i = 0; i < S::kQBufs; ++i)
         if (q > i) drain_wait(&b.q_full[i], (q - 1 - i) / S::kQBufs & 1);
-      // offsets that point outside the views
+      // offsets that point outside the views, and more queries than were announced
 #pragma unroll 1
       for (int64_t s = (int64_t)blockIdx.x * 32 + lane; s < p.n_seqs; s += (int64_t)gridDim.x * 32) {
         bool bad;
-        sequence(p, (int)s, &bad);
-        if (bad) atomicOr(p.err, DEV_ERR_INDEX_RANGE);
+        const Sequence sq = sequence(p, (int)s, &bad);
+        if (bad || sq.nq > p.max_q) atomicOr(p.err, DEV_ERR_INDEX_RANGE);
       }
     } else if (warp < kMmaWarp + S::kMmaWarps) {
       // ---------------- the products of tiles mine .. mine + NT - 1

@@ -225,7 +225,6 @@ bool few_is_faster(const gnn_attention* a, const gnn_attention_call* c, const At
 int run_few(gnn_attention* a, const gnn_attention_call* c, const AttendParams& p, int64_t max_q, cudaStream_t st) {
   FewGrid f = {};
   f.group = p.heads / p.kv_heads;
-  f.max_q = (int)max_q;
   const bool sixteen = max_q * f.group > 8;
   f.row_tiles = (int)((max_q * f.group + (sixteen ? 15 : 7)) / (sixteen ? 16 : 8));
   f.parts = a->d_parts;
@@ -377,6 +376,7 @@ int gnn_attention_run(gnn_attention* att, const gnn_attention_call* c, gnn_strea
   p.n_q_rows = (int)c->n_q_rows;
   p.n_kv_rows = (int)c->n_kv_rows;
   p.n_seqs = c->n_seqs;
+  p.max_q = (int)(c->max_q > 0 ? std::min<int64_t>(c->max_q, c->n_q_rows) : c->n_q_rows);
   p.heads = c->q.n_heads;
   p.kv_heads = c->k.n_heads;
   p.dim = c->head_dim;
@@ -386,9 +386,7 @@ int gnn_attention_run(gnn_attention* att, const gnn_attention_call* c, gnn_strea
   // a scale of zero as one too small to be seen, so that -inf, a score that is not seen, stays -inf
   p.scale_log2 = c->scale == 0.f ? 1e-30f : (float)((double)c->scale * 1.4426950408889634);
   p.err = att->d_err;
-  const int64_t max_q = c->max_q > 0 ? std::min<int64_t>(c->max_q, c->n_q_rows) : c->n_q_rows;
-  if (few_is_faster(att, c, p, max_q))
-    return run_few(att, c, p, max_q, (cudaStream_t)stream);
+  if (few_is_faster(att, c, p, p.max_q)) return run_few(att, c, p, p.max_q, (cudaStream_t)stream);
   return run_tiles(att, c, views, p, (cudaStream_t)stream);
 }
 

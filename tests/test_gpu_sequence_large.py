@@ -78,3 +78,14 @@ def test_new_queries_that_see_different_keys(dtype, H, K, nq):
     k[n - nq - 50] = math.nan                                # at the left edge of the first
     _attend(q, k, v, [0, nq], [0], [n], 50, 0, 0, max_q=nq, max_kv=n)
     _attend(q, k, v, [0, nq], [0], [n], 50, 0, 3, max_q=nq, max_kv=n)
+
+
+@pytest.mark.parametrize("rows,most", [(300, 100), (2, 1)])
+def test_more_queries_than_announced_are_reported(rows, most):
+    from paper_2402_09633_gb300 import WindowAttention
+    x = torch.zeros(rows, 1, 64, dtype=BF16, device="cuda")
+    att, starts = WindowAttention(), torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    att(x, x, x, starts, left=10, right=0, max_q=most)
+    assert att.status() == -5
+    att(x, x, x, starts, left=10, right=0, max_q=rows)
+    assert att.status() == 0
