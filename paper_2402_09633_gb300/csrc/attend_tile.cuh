@@ -5,9 +5,9 @@
 // stay on the old m, above 1 if need be.  Only blocks that some row of the tile sees are loaded; of those, parts that
 // no row of a warp sees cost no exponentials.
 //
-// What bounds it (event of 300,000 hits, two bf16 heads of 64, 512 neighbours to each side: 0.214 ms, 748 TFLOP/s of
-// visible products, tensor cores 35 % busy; causal 16,384, heads of 128, window 4,096: 0.183 ms, 1,350 TFLOP/s, 60 %):
-// a block's softmax is one chain of 1,300 cycles in a warp with 512 of them exponentials, two warps share a scheduler,
+// What bounds it (event of 300,000 hits, two bf16 heads of 64, 512 neighbours to each side: 0.200 ms, 800 TFLOP/s of
+// visible products, tensor cores 35 % busy; causal 16,384, heads of 128, window 4,096: 0.181 ms, 1,364 TFLOP/s, 60 %):
+// a block's softmax is one chain of 1,200 cycles in a warp with 512 of them exponentials, two warps share a scheduler,
 // and tensor memory holds no third tile beside two.  Other splits lost: 16 rows to a warp in sixteen warps 0.36 ms,
 // two threads to a row 0.25, three tiles of 96 keys 0.26, one warp that issues whatever is ready 0.36 (its polls take
 // issue slots).
@@ -581,41 +581,61 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         const float off = -m * scale;
         const float2 off2 = make_float2(off, off);
         float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-        tc_fence_after();
-        // 64 keys at a time, or 32 where the first weights' product waits for them, in a loop: the code of all 128 in one
-        // piece misses the instruction caches.
-        constexpr int STEP = S::kApart ? 2 : 1;
-#pragma unroll 1
-        for (int c0 = 0; c0 < PARTS; c0 += STEP) {
-          float s[32 * STEP];
+        if constexpr (!EDGE && S::kApart) {
+          // All scores first, so that the next product over them runs beside the weights (213 -> 205 us).
+          float s[kKeys];
+          read(s);
+          scores_read();
+          uint32_t w[2][16];
 #pragma unroll
-          for (int c = 0; c < STEP; ++c) tmem_ld_32x32(ts + 32 * (c0 + c), s + 32 * c);
-#pragma unroll
-          for (int c = 0; c < STEP; ++c) tmem_wait_ld_32(s + 32 * c);
-          if (c0 + STEP == PARTS) scores_read();
-#pragma unroll
-          for (int c = 0; c < STEP; ++c) {
-            uint32_t w[16];
-            if (EDGE && hide(kb, c0 + c, s + 32 * c)) {
-#pragma unroll
-              for (int e = 0; e < 16; ++e) w[e] = 0u;
-            } else {
-              weigh(s + 32 * c, off2, sum, w);
-            }
-            if (c == 0 && c0 == 0) {
-              // the last product with these weights' columns, and into these outputs, is over
+          for (int c = 0; c < PARTS; ++c) {
+            weigh(s + 32 * c, off2, sum, w[c & 1]);
+            if (c == 0) {
               ok = wait(&b.pv_done[wg], n - 1);
               if (!ok) return true;
               tc_fence_after();
             }
-            if (!S::kApart && c0 == 2) stored(&b.p_half[wg]);
-            tmem_st_32x16(tp + 16 * (c0 + c), w);
+            if (c == 2) stored(&b.p_half[wg]);
+            tmem_st_32x16(tp + 16 * c, w[c & 1]);
           }
-          if (S::kApart) stored(c0 ? &b.p_full[wg] : &b.p_half[wg]);
+          stored(&b.p_full[wg]);
+        } else {
+          tc_fence_after();
+          // 64 keys at a time, or 32 where the first weights' product waits for them, in a loop: with the code of all 128
+          // in one piece for these blocks too, the kernel misses the instruction caches.
+          constexpr int STEP = S::kApart ? 2 : 1;
+#pragma unroll 1
+          for (int c0 = 0; c0 < PARTS; c0 += STEP) {
+            float s[32 * STEP];
+#pragma unroll
+            for (int c = 0; c < STEP; ++c) tmem_ld_32x32(ts + 32 * (c0 + c), s + 32 * c);
+#pragma unroll
+            for (int c = 0; c < STEP; ++c) tmem_wait_ld_32(s + 32 * c);
+            if (c0 + STEP == PARTS) scores_read();
+#pragma unroll
+            for (int c = 0; c < STEP; ++c) {
+              uint32_t w[16];
+              if (EDGE && hide(kb, c0 + c, s + 32 * c)) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) w[e] = 0u;
+              } else {
+                weigh(s + 32 * c, off2, sum, w);
+              }
+              if (c == 0 && c0 == 0) {
+                // the last product with these weights' columns, and into these outputs, is over
+                ok = wait(&b.pv_done[wg], n - 1);
+                if (!ok) return true;
+                tc_fence_after();
+              }
+              if (!S::kApart && c0 == 2) stored(&b.p_half[wg]);
+              tmem_st_32x16(tp + 16 * (c0 + c), w);
+            }
+            if (S::kApart) stored(c0 ? &b.p_full[wg] : &b.p_half[wg]);
+          }
+          if (!S::kApart) stored(&b.p_full[wg]);
         }
         const float all = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
         l += all;
-        if (!S::kApart) stored(&b.p_full[wg]);
         plain = warp_all(all <= 256.f || row >= rows);
         return true;
       };
@@ -653,13 +673,15 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
       };
       // Any block.
       auto block = [&](int kb, bool start) {
+        if (p.scale_log2 < 0.f) {                    // rare, and so in little code
+          tc_fence_after();
+#pragma unroll 1
+          for (int c = 0; c < kKeys; c += 8) tmem_scale_32x8(ts + c, -1.f);
+          tmem_st_wait();
+        }
         float s[kKeys];
         read(s);
         scores_read();
-        if (p.scale_log2 < 0.f) {
-#pragma unroll
-          for (int c = 0; c < kKeys; ++c) s[c] = -s[c];
-        }
         uint32_t hidden = 0;                         // parts of the block that no row of the warp sees
 #pragma unroll
         for (int c = 0; c < PARTS; ++c)
@@ -732,7 +754,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
       const float r = none ? 0.f : 1.f / l;
       float2 odd = make_float2(0.f, 0.f);            // not finite once a value is not
       uint8_t* mine = stage + warp * kStageBytes;
-#pragma unroll 1
+#pragma unroll S::kApart ? 2 : 1                      // 204 -> 201 us; four in one piece cost as much as they save
       for (int c = 0; c < DP; c += 32) {
         // A thread has a row, and rows lie apart: written from here, every store would touch 32 lines.  Through shared
         // memory, 16 bytes at a place that the row turns by its number, four threads write 64 bytes of a row.
