@@ -5,8 +5,8 @@
 // stay on the old m, above 1 if need be.  Only blocks that some row of the tile sees are loaded; of those, parts that
 // no row of a warp sees cost no exponentials.
 //
-// What bounds it (event of 300,000 hits, two bf16 heads of 64, 512 neighbours to each side: 0.200 ms, 800 TFLOP/s of
-// visible products, tensor cores 35 % busy; causal 16,384, heads of 128, window 4,096: 0.181 ms, 1,364 TFLOP/s, 60 %):
+// What bounds it (event of 300,000 hits, two bf16 heads of 64, 512 neighbours to each side: 0.199 ms, 800 TFLOP/s of
+// visible products, tensor cores 36 % busy; causal 16,384, heads of 128, window 4,096: 0.181 ms, 1,364 TFLOP/s, 62 %):
 // a block's softmax is one chain of 1,200 cycles in a warp with 512 of them exponentials, two warps share a scheduler,
 // and tensor memory holds no third tile beside two.  Other splits lost: 16 rows to a warp in sixteen warps 0.36 ms,
 // two threads to a row 0.25, three tiles of 96 keys 0.26, one warp that issues whatever is ready 0.36 (its polls take
