@@ -571,10 +571,11 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         return false;
       };
       // Blocks on the guess that their scores do not outgrow the running maximum (which they rarely do after the first).
-      // In bf16 nothing depends on the guess: weights above 1 lose no precision, their sum tells whether the next block
-      // has to look for the maximum, and only scores that outgrow it by 2^100 in one block would overflow, in a row
-      // that is then not finite and done again.  In fp16, whose weights end at 2^16, the maximum is computed beside
-      // the weights of a block that every row sees whole: false, with nothing changed, when the guess was wrong.
+      // In bf16 nothing depends on the guess: weights above 1 lose no precision, and their sum tells whether the next
+      // block has to look for the maximum, and how far that was left behind.  Scores that outgrow it by 2^128 in one block
+      // overflow the weights, their sum or the outputs: such a row is left not finite and done again.  In fp16, whose
+      // weights end at 2^16, the maximum is computed beside the weights of a block that every row sees whole: false,
+      // with nothing changed, when the guess was wrong.
       constexpr bool LOOSE = std::is_same<T, __nv_bfloat16>::value;
       auto loose = [&](int kb, auto edge) {
         constexpr bool EDGE = decltype(edge)::value;   // a block that not every row sees whole
@@ -729,6 +730,22 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         plain = warp_all(m > -INFINITY);
         return true;
       };
+      // After weights on a maximum left far behind: it catches up by the powers of two in their sum, which comes down by as
+      // many, and the outputs with it.  Otherwise the step from the old maximum to a new one could be past 2^-126,
+      // which is zero, and drop sums that count.
+      auto catch_up = [&] {
+        if (!wait(&b.pv_done[wg], n - 1)) return false;
+        tc_fence_after();
+        const bool late = l > 65536.f;
+        const float mn = late ? m + (float)min((__float_as_int(l) >> 23) - 127, 120) / scale : m;
+        const float shrink = late ? exp2_approx((m - mn) * scale) : 1.f;
+        m = mn;
+        l *= shrink;
+#pragma unroll 1
+        for (int c = 0; c < DP; c += 8) tmem_scale_32x8(to + c, shrink);
+        tmem_st_wait();
+        return true;
+      };
       for (int i = 0; i < blocks; ++i, ++n) {
         const int kb = i < sinks ? i : lo + (i - sinks);
         ok = wait(&b.s_full[wg], n);
@@ -739,6 +756,10 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
             if (!ok) break;
             continue;
           }
+        }
+        if (LOOSE && __any_sync(0xffffffffu, l > 65536.f)) {
+          ok = catch_up();
+          if (!ok) break;
         }
         ok = block(kb, i == 0);
         if (!ok) break;
@@ -751,7 +772,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         tc_fence_after();
       }
       const bool none = blocks == 0 || l == 0.f;
-      const float r = none ? 0.f : 1.f / l;
+      const float r = none ? 0.f : LOOSE && !(l < INFINITY) ? NAN : 1.f / l;   // a sum that overflowed: done again
       float2 odd = make_float2(0.f, 0.f);            // not finite once a value is not
       uint8_t* mine = stage + warp * kStageBytes;
 #pragma unroll S::kApart ? 2 : 1                      // 204 -> 201 us; four in one piece cost as much as they save
