@@ -171,11 +171,19 @@ __global__ void __launch_bounds__(kRotThreads, V >= 8 ? 4 : 5) rotary_kernel(con
       for (int u = 0; u < UPL; ++u) {
         const int unit = sub + u * p.group;
         if (unit >= p.units) continue;
-        const bool turned = unit * V < pairs;
+        if (unit * V >= pairs) {                   // past the rotation: each element by itself, whatever lies beside it
+          if constexpr (NORM) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+              for (int e = 0; e < V; ++e) {
+                xu[b][u].v[e] = from_f<T>(to_f(xu[b][u].v[e]) * (r[b] * gain_s[e][unit]));
+                xw[b][u].v[e] = from_f<T>(to_f(xw[b][u].v[e]) * (r[b] * gain_s[V + e][unit]));
+              }
+          }
+          continue;
+        }
         auto angle = [&](int e, float& c, float& s) {
-          c = 1.f;
-          s = 0.f;
-          if (!turned) return;
           const uint64_t f = freq_s[e][unit];
           const float turns = p.pos_float ? turns_real(__int_as_float(pos), __uint_as_float((uint32_t)(f >> 32)),
                                                        __uint_as_float((uint32_t)f))
