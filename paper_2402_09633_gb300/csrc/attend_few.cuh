@@ -464,9 +464,9 @@ __global__ void __launch_bounds__(32 * kFewWarps, NR == 2 && NC > 2 ? 2 : 3)
         store(r, 4 * (place - r * quads), sum_s[r], val);
       }
     }
-    // Rows of several queries see different keys, and a weight of zero times a value that is not finite is NaN: such
-    // rows are done again, key by visible key.
-    if (pos_last > pos_first) {
+    // A sequence's queries see different keys, all of which a tile goes through (one of a single query too), and a weight of
+    // zero times a value that is not finite is NaN: such rows are done again, key by visible key.
+    if (sq.nq > 1) {
       __syncthreads();
       for (int r = warp; r < rows; r += kFewWarps) {
         const int i = (row0 + r) / G, head = kv * G + (row0 + r) % G;
