@@ -37,20 +37,18 @@ class GnnAttentionCall(ctypes.Structure):
                 ("right", _i32), ("sinks", _i32), ("scale", _f32), ("reserved", _i32)]
 
 
-_HEADS = struct.Struct("PqqiI")                              # GnnHeads
-_TWO, _SIX = struct.Struct("PqqiI" * 2), struct.Struct("PqqiI" * 6)
-_NONE = (0, 0, 0, 0, 0)
-_CALL = struct.Struct("ii" + "PqqiI" * 4 + "PPPqqiiiiiifi")   # GnnAttentionCall
-assert _HEADS.size == ctypes.sizeof(GnnHeads) and _CALL.size == ctypes.sizeof(GnnAttentionCall)
-_AREA = ctypes.create_string_buffer(max(6 * _HEADS.size, _CALL.size))
-_AT = [ctypes.addressof(_AREA) + i * _HEADS.size for i in range(6)]
+# The structures are packed into bytes that belong to one call: threads may call at once, each on its own stream.
+_HEADS = struct.Struct("PqqiI").pack                         # GnnHeads
+_CALL = struct.Struct("ii" + "PqqiI" * 4 + "PPPqqiiiiiifi").pack   # GnnAttentionCall
+assert struct.calcsize("PqqiI") == ctypes.sizeof(GnnHeads)
+assert struct.calcsize("ii" + "PqqiI" * 4 + "PPPqqiiiiiifi") == ctypes.sizeof(GnnAttentionCall)
 _lib = _torch = _raw_stream = None
 DTYPES = {}
 
 
 def _library():
-    """The library, loaded once more so that its calls keep the interpreter lock: they only enqueue work, and the one
-    area that their arguments are packed in is then not written by two threads."""
+    """The library, loaded once more so that its calls keep the interpreter lock: they only enqueue work, and giving the
+    lock up and taking it again would cost more than they do."""
     global _lib, _torch, _raw_stream
     if _lib is None:
         import torch
@@ -81,12 +79,17 @@ def _stream(stream, device):
     return _raw_stream(device) if stream is None else stream.cuda_stream
 
 
-def _heads(x, dtype, device, dim):
+def _fields(x, dtype, device, dim):
     """A view's fields; x: cuda tensor [rows, heads, dim], last stride 1, of the given type, device and head size."""
     shape, stride = x.shape, x.stride()
     assert len(shape) == 3 and (stride[2] == 1 or shape[2] == 1), "a tensor [rows, heads, dim], last stride 1"
     assert x.dtype == dtype and x.get_device() == device and shape[2] == dim, "types, devices or head sizes differ"
     return x.data_ptr(), stride[0], stride[1], shape[1], 0
+
+
+def _heads(x, dtype, device, dim):
+    """A view as a gnn_heads, whose address a call is given."""
+    return _HEADS(*_fields(x, dtype, device, dim))
 
 
 def _kind(x):
@@ -141,8 +144,8 @@ def rope(rot: Rotary, x, positions=None, out=None, stream=None):
     pos, real = _positions(positions, n, device)
     if n == 0:
         return out
-    _TWO.pack_into(_AREA, 0, *_heads(x, dtype, device, dim), *_heads(out, dtype, device, dim))
-    rc = _lib.gnn_rope(rot.address, number, dim, _AT[0], _AT[1], pos, real, n, _stream(stream, device))
+    rc = _lib.gnn_rope(rot.address, number, dim, _heads(x, dtype, device, dim), _heads(out, dtype, device, dim), pos, real,
+                       n, _stream(stream, device))
     if rc != GNN_OK:
         raise GnnError(rc, "gnn_rope")
     return out
@@ -172,17 +175,10 @@ def qk_norm_rope(rot: Rotary, q, k, positions=None, v=None, q_gain=None, k_gain=
     if n == 0:
         return q_out, k_out, v_out
     assert m > 0, "k_out has no rows"
-    a = _AT
-    if v is None:
-        _SIX.pack_into(_AREA, 0, *_heads(q, dtype, device, dim), *_heads(k, dtype, device, dim), *_NONE,
-                       *_heads(q_out, dtype, device, dim), *_heads(k_out, dtype, device, dim), *_NONE)
-    else:
-        _SIX.pack_into(_AREA, 0, *_heads(q, dtype, device, dim), *_heads(k, dtype, device, dim),
-                       *_heads(v, dtype, device, dim), *_heads(q_out, dtype, device, dim),
-                       *_heads(k_out, dtype, device, dim), *_heads(v_out, dtype, device, dim))
-    values, values_out = (None, None) if v is None else (a[2], a[5])
-    rc = _lib.gnn_qk_norm_rope(rot.address, number, dim, eps, gq, gk, a[0], a[1], values, a[3], a[4], values_out, pos,
-                               real, at, m, n, _stream(stream, device))
+    values, values_out = (None, None) if v is None else (_heads(v, dtype, device, dim), _heads(v_out, dtype, device, dim))
+    rc = _lib.gnn_qk_norm_rope(rot.address, number, dim, eps, gq, gk, _heads(q, dtype, device, dim),
+                               _heads(k, dtype, device, dim), values, _heads(q_out, dtype, device, dim),
+                               _heads(k_out, dtype, device, dim), values_out, pos, real, at, m, n, _stream(stream, device))
     if rc != GNN_OK:
         raise GnnError(rc, "gnn_qk_norm_rope")
     return q_out, k_out, v_out
@@ -209,12 +205,12 @@ class WindowAttention:
             out = _torch.empty_like(q)
         n, int32, rows = q_start.numel() - 1, _torch.int32, k.shape[0]
         assert n >= 0 and out.shape == q.shape and v.shape[0] == rows, "outputs, keys or values of other sizes"
-        _CALL.pack_into(_AREA, 0, number, dim, *_heads(q, dtype, device, dim), *_heads(k, dtype, device, dim),
-                        *_heads(v, dtype, device, dim), *_heads(out, dtype, device, dim),
-                        _vector(q_start, n + 1, int32, device), _vector(kv_start, n, int32, device) or 0,
-                        _vector(kv_len, n, int32, device) or 0, q.shape[0], rows, n, max_q, max_kv, left, right, sinks,
-                        1.0 / math.sqrt(dim) if scale is None else scale, 0)
-        rc = _lib.gnn_attention_run(self.handle, _AT[0], _stream(stream, device))
+        call = _CALL(number, dim, *_fields(q, dtype, device, dim), *_fields(k, dtype, device, dim),
+                     *_fields(v, dtype, device, dim), *_fields(out, dtype, device, dim),
+                     _vector(q_start, n + 1, int32, device), _vector(kv_start, n, int32, device) or 0,
+                     _vector(kv_len, n, int32, device) or 0, q.shape[0], rows, n, max_q, max_kv, left, right, sinks,
+                     1.0 / math.sqrt(dim) if scale is None else scale, 0)
+        rc = _lib.gnn_attention_run(self.handle, call, _stream(stream, device))
         if rc != GNN_OK:
             raise GnnError(rc, "gnn_attention_run")
         return out
