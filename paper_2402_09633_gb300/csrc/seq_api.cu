@@ -336,6 +336,8 @@ int gnn_attention_create(gnn_attention** out) {
   if (err == cudaSuccess) err = dev_alloc((void**)&a->d_parts, blocks * 2 * kFewRows * (128 + 2) * 4);
   if (err == cudaSuccess) err = dev_alloc((void**)&a->d_tickets, blocks * 4);
   if (err == cudaSuccess) err = cudaMemset(a->d_tickets, 0, blocks * 4);
+  // the zeros are in place before any stream's first call: streams need not wait for the one they are written in
+  if (err == cudaSuccess) err = cudaStreamSynchronize(cudaStreamLegacy);
   if (err != cudaSuccess) {
     free_attention(a);
     return cuda_fail(err);
@@ -392,11 +394,13 @@ int gnn_attention_run(gnn_attention* att, const gnn_attention_call* c, gnn_strea
 
 int gnn_attention_status(gnn_attention* att, gnn_stream_t stream) {
   if (!att) return GNN_ERR_INVALID_ARG;
-  cudaError_t err = cudaStreamSynchronize((cudaStream_t)stream);
-  if (err != cudaSuccess) return cuda_fail(err);
+  // In the caller's stream, so that the word is read behind its calls so far and cleared before the next.
+  const cudaStream_t st = (cudaStream_t)stream;
   uint32_t word = 0;
-  err = cudaMemcpy(&word, att->d_err, 4, cudaMemcpyDeviceToHost);
-  if (err == cudaSuccess) err = cudaMemset(att->d_err, 0, 4);
+  cudaError_t err = cudaMemcpyAsync(&word, att->d_err, 4, cudaMemcpyDeviceToHost, st);
+  if (err == cudaSuccess) err = cudaMemsetAsync(att->d_err, 0, 4, st);
+  const cudaError_t done = cudaStreamSynchronize(st);          // whatever failed: the copy writes to this frame
+  if (err == cudaSuccess) err = done;
   if (err != cudaSuccess) return cuda_fail(err);
   if (word & DEV_ERR_TIMEOUT) return GNN_ERR_DEVICE_TIMEOUT;
   if (word & DEV_ERR_INDEX_RANGE) return GNN_ERR_INDEX_RANGE;

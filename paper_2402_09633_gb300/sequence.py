@@ -59,12 +59,12 @@ def _library():
         lib.gnn_rope.argtypes = [_vp, i, i, _vp, _vp, _vp, i, _i64, _vp]
         lib.gnn_qk_norm_rope.argtypes = [_vp, i, i, _f32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, i, _vp, _i64, _i64,
                                          _vp]
-        lib.gnn_attention_create.argtypes = [ctypes.POINTER(_vp)]
         lib.gnn_attention_run.argtypes = [_vp, _vp, _vp]
-        for f in (lib.gnn_rotary_init, lib.gnn_rope, lib.gnn_qk_norm_rope, lib.gnn_attention_create,
-                  lib.gnn_attention_run):
+        for f in (lib.gnn_rotary_init, lib.gnn_rope, lib.gnn_qk_norm_rope, lib.gnn_attention_run):
             f.restype = i
         waits = binding.load_library()                       # these wait for the device, without the lock
+        waits.gnn_attention_create.argtypes = [ctypes.POINTER(_vp)]
+        waits.gnn_attention_create.restype = i
         waits.gnn_attention_status.argtypes = [_vp, _vp]
         waits.gnn_attention_status.restype = i
         waits.gnn_attention_destroy.argtypes = [_vp]
@@ -188,8 +188,9 @@ class WindowAttention:
     """One handle of gnn_attention_create on the current device (a stream's own; see include/gnn.h)."""
 
     def __init__(self):
+        _library()
         h = _vp()
-        rc = _library().gnn_attention_create(ctypes.byref(h))
+        rc = binding.load_library().gnn_attention_create(ctypes.byref(h))
         if rc != GNN_OK:
             raise GnnError(rc, "gnn_attention_create")
         self.handle = h
