@@ -347,7 +347,7 @@ int gnn_csr_build_noalloc(const int32_t* edge_index, int64_t n_nodes, int64_t n_
  * positions, and a hit attends to a window of the order and to a few first tokens that stay
  * visible.  The calls below are those three steps, for a batch of whole events at once and for new
  * hits over a cache of earlier ones.  (Library operators: the paper has no counterpart.)  They need
- * no gnn_ctx.
+ * no gnn_ctx.  Arrays and streams are those of the current device.
  *
  * gnn_heads -- a view of a device array [rows, n_heads, head_dim] of one of the types below: element
  * (r, h, d) at data + r * row_stride + h * head_stride + d, strides in elements, so that slices of a
@@ -457,7 +457,8 @@ int gnn_qk_norm_rope(const gnn_rotary* rot, int dtype, int head_dim, float eps, 
  * gnn_attention_status.  Enqueued on `stream`; only enqueues kernels (it can be captured).  The same inputs
  * give bitwise-identical outputs.
  * Errors: INVALID_ARG (null pointer, any limit above, scale not finite, sinks < 0, sizes above GNN_MAX_COUNT,
- * n_seqs above 2^28, 2^31 or more tiles of 128 queries for one key head), CUDA.
+ * n_seqs above 2^28, 2^31 or more tiles of 128 queries for one key head, a handle of another device than the current
+ * one), CUDA.
  *
  * gnn_attention_create -- a handle on the current device: the workspace of calls with few queries and the
  * device error word.  Synchronous.  One handle per stream: it is not safe for concurrent use.  Errors:

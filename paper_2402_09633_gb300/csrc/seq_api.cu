@@ -388,6 +388,10 @@ int gnn_attention_run(gnn_attention* att, const gnn_attention_call* c, gnn_strea
   // a scale of zero as one too small to be seen, so that -inf, a score that is not seen, stays -inf
   p.scale_log2 = c->scale == 0.f ? 1e-30f : (float)((double)c->scale * 1.4426950408889634);
   p.err = att->d_err;
+  int device = 0;                                  // the handle's memory and SMs are its device's
+  const cudaError_t err = cudaGetDevice(&device);
+  if (err != cudaSuccess) return cuda_fail(err);
+  if (device != att->device) return GNN_ERR_INVALID_ARG;
   if (few_is_faster(att, c, p, p.max_q)) return run_few(att, c, p, p.max_q, (cudaStream_t)stream);
   return run_tiles(att, c, views, p, (cudaStream_t)stream);
 }

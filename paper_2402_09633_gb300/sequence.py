@@ -1,8 +1,8 @@
 """Hits read as a sequence: rotary positions, norms of queries and keys with the rotation, and attention with a
 sliding window (ctypes binding of the same calls in include/gnn.h; argument marshalling only).
 
-All tensors are views [rows, heads, head_dim] on the GPU whose last stride is 1, so slices of a packed projection
-are taken as they are."""
+All tensors are views [rows, heads, head_dim] on the current device whose last stride is 1, so slices of a packed
+projection are taken as they are."""
 from __future__ import annotations
 
 import ctypes
@@ -42,14 +42,14 @@ _HEADS = struct.Struct("PqqiI").pack                         # GnnHeads
 _CALL = struct.Struct("ii" + "PqqiI" * 4 + "PPPqqiiiiiifi").pack   # GnnAttentionCall
 assert struct.calcsize("PqqiI") == ctypes.sizeof(GnnHeads)
 assert struct.calcsize("ii" + "PqqiI" * 4 + "PPPqqiiiiiifi") == ctypes.sizeof(GnnAttentionCall)
-_lib = _torch = _raw_stream = None
+_lib = _torch = _raw_stream = _current_device = None
 DTYPES = {}
 
 
 def _library():
     """The library, loaded once more so that its calls keep the interpreter lock: they only enqueue work, and giving the
     lock up and taking it again would cost more than they do."""
-    global _lib, _torch, _raw_stream
+    global _lib, _torch, _raw_stream, _current_device
     if _lib is None:
         import torch
         binding.load_library()
@@ -70,7 +70,7 @@ def _library():
         waits.gnn_attention_destroy.argtypes = [_vp]
         waits.gnn_attention_destroy.restype = None
         DTYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
-        _raw_stream = torch._C._cuda_getCurrentRawStream
+        _raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
         _lib, _torch = lib, torch
     return _lib
 
@@ -96,6 +96,7 @@ def _kind(x):
     """(type, its number, device, head size) of a cuda tensor."""
     device, dtype = x.get_device(), x.dtype
     assert device >= 0, "a cuda tensor"
+    assert device == _current_device(), "the tensors' device is not the current one, where calls launch"
     assert dtype in DTYPES, f"type {dtype} is not taken"
     return dtype, DTYPES[dtype], device, x.shape[2]
 
@@ -193,7 +194,7 @@ class WindowAttention:
         rc = binding.load_library().gnn_attention_create(ctypes.byref(h))
         if rc != GNN_OK:
             raise GnnError(rc, "gnn_attention_create")
-        self.handle = h
+        self.handle, self.device = h, _current_device()
 
     def __call__(self, q, k, v, q_start, left: int = -1, right: int = -1, sinks: int = 0, scale=None, kv_start=None,
                  kv_len=None, max_q: int = 0, max_kv: int = 0, out=None, stream=None):
@@ -202,6 +203,7 @@ class WindowAttention:
         are the rows of its queries.  left, right: keys visible before and after a query's own position (-1: all),
         sinks: first keys that stay visible; max_q, max_kv: the most queries and keys of a sequence, when known."""
         dtype, number, device, dim = _kind(q)
+        assert device == self.device, "the handle belongs to another device"
         if out is None:
             out = _torch.empty_like(q)
         n, int32, rows = q_start.numel() - 1, _torch.int32, k.shape[0]

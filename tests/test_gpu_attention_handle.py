@@ -44,3 +44,20 @@ def test_status_leaves_nothing_for_later():
             assert att.status() == 0
     assert not main.query()                                  # none of it waited for the other stream's work
     torch.cuda.synchronize()
+
+
+def test_a_handle_of_another_device_is_refused():
+    """By the library, before it looks at anything else of the handle: zeros behind the number of a second device."""
+    import ctypes
+    from paper_2402_09633_gb300 import WindowAttention
+    from paper_2402_09633_gb300.binding import GnnError
+    x = torch.zeros(20, 1, 64, dtype=torch.bfloat16, device="cuda")
+    starts = torch.tensor([0, 20], dtype=torch.int32, device="cuda")
+    att = WindowAttention()
+    own, att.handle = att.handle, ctypes.cast((ctypes.c_int * 64)(1), ctypes.c_void_p)
+    with pytest.raises(GnnError) as e:
+        att(x, x, x, starts)
+    assert e.value.code == -1
+    att.handle = own
+    att(x, x, x, starts)
+    assert att.status() == 0

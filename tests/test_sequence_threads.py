@@ -48,6 +48,7 @@ int gnn_attention_run(gnn_attention* a, const gnn_attention_call* c, gnn_stream_
 
 class Tensor:
     """What the binding asks of a cuda tensor, without memory behind it."""
+    device = 0
 
     def __init__(self, address, dtype, *shape):
         self.address, self.dtype, self.shape = address, dtype, shape
@@ -56,7 +57,7 @@ class Tensor:
         return (64 * self.shape[0], 64, 1)
 
     def get_device(self):
-        return 0
+        return self.device
 
     def data_ptr(self):
         return self.address
@@ -89,6 +90,8 @@ def patched(stand_in, monkeypatch):
     monkeypatch.setattr(Q, "_lib", None)
     monkeypatch.setattr(binding, "LIB_PATH", stand_in)
     monkeypatch.setattr(binding, "_lib", ctypes.CDLL(stand_in))
+    Q._library()
+    monkeypatch.setattr(Q, "_current_device", lambda: Tensor.device)
     interval = sys.getswitchinterval()
     sys.setswitchinterval(1e-6)
     yield
@@ -114,7 +117,6 @@ def _calls(kind, n, attend):
 
 @pytest.mark.parametrize("kinds", [("rope",), ("norm",), ("attend",), ("rope", "norm", "attend")])
 def test_each_call_gets_its_own_arguments(patched, kinds):
-    Q._library()
     wrong, done = [], []
 
     def work(n):
