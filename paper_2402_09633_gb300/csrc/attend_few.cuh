@@ -74,6 +74,71 @@ __device__ __forceinline__ int few_units(const AttendParams& p, const Sequence& 
   return sq.nq == 0 ? 0 : max(1, (int)(((int64_t)few_keys(p, sq).n + kFewUnit - 1) / kFewUnit));
 }
 
+// Units before each sequence (pre[0 .. n_seqs]), the first sequences (seq_s), and a block's share of all units.  A
+// block whose share is small would spend it on waiting if it had parts of two tiles: there each tile starts with a block
+// of its own.  128 sequences' units fit 32 bits, as each has below 2^25 - 127; those of all need not, as sequences may
+// read the same keys.
+template <int NR>
+__device__ __forceinline__ int64_t few_share(const AttendParams& p, int KR, int64_t* pre, uint32_t* scan_s, Sequence* seq_s) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  auto block_scan = [&](uint32_t x, uint32_t* sum) {   // the sum up to this thread's, and that of all
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+      const uint32_t y = __shfl_up_sync(0xffffffffu, x, d);
+      if (lane >= d) x += y;
+    }
+    __syncthreads();
+    if (lane == 31) scan_s[warp] = x;
+    __syncthreads();
+    *sum = 0;
+#pragma unroll
+    for (int w = 0; w < kFewWarps; ++w) {
+      if (w < warp) x += scan_s[w];
+      *sum += scan_s[w];
+    }
+    return x;
+  };
+  // More parts make a tile's own time shorter and its join longer (0.7 us a unit, up to 0.35 us a part of 16 rows): no
+  // more than balances the two.  (One sequence of 8,192 keys, four queries, 16 rows: 41 -> 22 us.)
+  auto even = [&](int64_t sum) {
+    const int64_t least = (int64_t)sqrtf(0.12f * NR * (float)sum / (float)p.n_seqs);
+    return max(max((int64_t)1, least), (sum * KR + gridDim.x - 1) / gridDim.x);
+  };
+  int64_t share = 1, before = 0;
+  for (int b0 = 0; b0 < p.n_seqs; b0 += 32 * kFewWarps) {
+    const int b = b0 + threadIdx.x;
+    uint32_t u = 0, sum;
+    if (b < p.n_seqs) {
+      bool bad;
+      const Sequence sq = sequence(p, b, &bad);
+      if ((bad || sq.nq > p.max_q) && blockIdx.x == 0) atomicOr(p.err, DEV_ERR_INDEX_RANGE);
+      if (b < 32 * kFewWarps) seq_s[b] = sq;
+      u = few_units(p, sq);
+    }
+    uint32_t upto = block_scan(u, &sum);
+    if (p.n_seqs <= 32 * kFewWarps) {
+      share = even(sum);
+      if (share <= kFewPadded) {
+        for (uint32_t s = (uint32_t)share; s <= 2 * kFewPadded; ++s) {
+          uint32_t padded;
+          const uint32_t x = block_scan((u + s - 1) / s * s, &padded);
+          if ((int64_t)padded * KR > (int64_t)s * gridDim.x) continue;
+          upto = x;
+          u = (u + s - 1) / s * s;
+          sum = padded;
+          share = s;
+          break;
+        }
+      }
+    }
+    if (b < p.n_seqs) pre[b] = before + upto - u;
+    before += sum;
+  }
+  if (threadIdx.x == 0) pre[p.n_seqs] = before;
+  __syncthreads();
+  return p.n_seqs > 32 * kFewWarps ? even(before) : share;
+}
+
 // NC: 16-byte pieces of a key that a lane takes, a quarter of those of head_dim up to 32 NC.  NR: rows of a tile / 8.
 template <typename T, int NC, int NR>
 __global__ void __launch_bounds__(32 * kFewWarps, NR == 2 && NC > 2 ? 2 : 3)
@@ -81,7 +146,8 @@ __global__ void __launch_bounds__(32 * kFewWarps, NR == 2 && NC > 2 ? 2 : 3)
   constexpr int NV = (NC + 1) / 2, DS = NV * 64 + 4, ROWS = 8 * NR;   // pieces of a value to a lane; a row in shared memory
   __shared__ __align__(16) float o_s[kFewWarps][ROWS][DS];
   __shared__ float m_s[kFewWarps][ROWS], l_s[kFewWarps][ROWS], sum_s[ROWS];
-  __shared__ int pre[kFewSeqs + 1], scan_s[kFewWarps];
+  __shared__ int64_t pre[kFewSeqs + 1];
+  __shared__ uint32_t scan_s[kFewWarps];
   __shared__ int last_s;
   __shared__ Sequence seq_s[32 * kFewWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -90,65 +156,7 @@ __global__ void __launch_bounds__(32 * kFewWarps, NR == 2 && NC > 2 ? 2 : 3)
   const bool balanced = p.n_seqs <= kFewSeqs;
   pdl_wait();
 
-  // Units before each sequence, and a block's share of all of them.  A block whose share is small would spend it
-  // on waiting if it had parts of two tiles: there each tile starts with a block of its own.
-  int share = 1;
-  if (balanced) {
-    auto block_scan = [&](int x, int* sum) {         // the sum up to this thread's, and that of all
-#pragma unroll
-      for (int d = 1; d < 32; d *= 2) {
-        const int y = __shfl_up_sync(0xffffffffu, x, d);
-        if (lane >= d) x += y;
-      }
-      __syncthreads();
-      if (lane == 31) scan_s[warp] = x;
-      __syncthreads();
-      *sum = 0;
-#pragma unroll
-      for (int w = 0; w < kFewWarps; ++w) {
-        if (w < warp) x += scan_s[w];
-        *sum += scan_s[w];
-      }
-      return x;
-    };
-    // More parts make a tile's own time shorter and its join longer (0.7 us a unit, up to 0.35 us a part of 16 rows): no
-    // more than balances the two.  (One sequence of 8,192 keys, four queries, 16 rows: 41 -> 22 us.)
-    auto least = [&](int sum) { return (int)sqrtf(0.12f * NR * (float)sum / (float)p.n_seqs); };
-    int before = 0;
-    for (int b0 = 0; b0 < p.n_seqs; b0 += 32 * kFewWarps) {
-      const int b = b0 + threadIdx.x;
-      int u = 0, sum;
-      if (b < p.n_seqs) {
-        bool bad;
-        const Sequence sq = sequence(p, b, &bad);
-        if ((bad || sq.nq > p.max_q) && blockIdx.x == 0) atomicOr(p.err, DEV_ERR_INDEX_RANGE);
-        if (b < 32 * kFewWarps) seq_s[b] = sq;
-        u = few_units(p, sq);
-      }
-      int upto = block_scan(u, &sum);
-      if (p.n_seqs <= 32 * kFewWarps) {
-        share = max(max(1, least(sum)), (int)(((int64_t)sum * KR + gridDim.x - 1) / gridDim.x));
-        if (share <= kFewPadded) {
-          for (int s = share; s <= 2 * kFewPadded; ++s) {
-            int padded;
-            const int x = block_scan((u + s - 1) / s * s, &padded);
-            if ((int64_t)padded * KR > (int64_t)s * gridDim.x) continue;
-            upto = x;
-            u = (u + s - 1) / s * s;
-            sum = padded;
-            share = s;
-            break;
-          }
-        }
-      }
-      if (b < p.n_seqs) pre[b] = before + upto - u;
-      before += sum;
-    }
-    if (threadIdx.x == 0) pre[p.n_seqs] = before;
-    __syncthreads();
-    if (p.n_seqs > 32 * kFewWarps)
-      share = max(max(1, least(before)), (int)(((int64_t)before * KR + gridDim.x - 1) / gridDim.x));
-  }
+  const int64_t share = balanced ? few_share<NR>(p, KR, pre, scan_s, seq_s) : 1;
 
   // Units [v0, v1) of the `units` of row tile kr of sequence b; u0: the tile's first unit among all.
   auto process = [&](int b, int kr, int v0, int v1, int units, int64_t u0) {
@@ -488,16 +496,16 @@ __global__ void __launch_bounds__(32 * kFewWarps, NR == 2 && NC > 2 ? 2 : 3)
   };
 
   if (balanced) {
-    const int64_t end = min(((int64_t)blockIdx.x + 1) * share, (int64_t)pre[p.n_seqs] * KR);
+    const int64_t end = min(((int64_t)blockIdx.x + 1) * share, pre[p.n_seqs] * KR);
     for (int64_t u = (int64_t)blockIdx.x * share; u < end;) {
-      const int x = (int)(u / KR);
+      const int64_t x = u / KR;
       int a = 0, z = p.n_seqs;                       // the last sequence that starts at or before x has units
       while (z - a > 1) {
         const int mid = (a + z) / 2;
         if (pre[mid] <= x) a = mid; else z = mid;
       }
-      const int units = pre[a + 1] - pre[a];
-      const int64_t r = u - (int64_t)pre[a] * KR;
+      const int units = (int)(pre[a + 1] - pre[a]);
+      const int64_t r = u - pre[a] * KR;
       const int kr = (int)(r / units), v0 = (int)(r - (int64_t)kr * units), v1 = (int)min((int64_t)units, v0 + (end - u));
       // where tiles are padded to whole shares, `units` counts the padding too
       const int real = share <= 2 * kFewPadded && p.n_seqs <= 32 * kFewWarps ? few_units(p, seq_s[a]) : units;
