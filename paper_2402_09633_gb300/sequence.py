@@ -79,6 +79,14 @@ def _stream(stream, device):
     return _raw_stream(device) if stream is None else stream.cuda_stream
 
 
+def _empty_like(x, stream):
+    """Like x, in memory of the call's stream: what another stream's held before may still be in use there."""
+    if stream is None:
+        return _torch.empty_like(x)
+    with _torch.cuda.stream(stream):
+        return _torch.empty_like(x)
+
+
 def _fields(x, dtype, device, dim):
     """A view's fields; x: cuda tensor [rows, heads, dim], last stride 1, of the given type, device and head size."""
     shape, stride = x.shape, x.stride()
@@ -140,7 +148,7 @@ def rope(rot: Rotary, x, positions=None, out=None, stream=None):
     dtype, number, device, dim = _kind(x)
     n = x.shape[0]
     if out is None:
-        out = _torch.empty_like(x)
+        out = _empty_like(x, stream)
     assert out.shape == x.shape
     pos, real = _positions(positions, n, device)
     if n == 0:
@@ -162,11 +170,11 @@ def qk_norm_rope(rot: Rotary, q, k, positions=None, v=None, q_gain=None, k_gain=
     assert rows is None or (k_out is not None and (v is None or v_out is not None)), "rows need k_out and v_out"
     assert v is not None or v_out is None, "v_out without v"
     if q_out is None:
-        q_out = _torch.empty_like(q)
+        q_out = _empty_like(q, stream)
     if k_out is None:
-        k_out = _torch.empty_like(k)
+        k_out = _empty_like(k, stream)
     if v is not None and v_out is None:
-        v_out = _torch.empty_like(v)
+        v_out = _empty_like(v, stream)
     m = k_out.shape[0]
     assert q_out.shape == q.shape and (rows is not None or m == n), "outputs of other sizes"
     assert v is None or v_out.shape[0] == m, "k_out and v_out differ"
@@ -205,7 +213,7 @@ class WindowAttention:
         dtype, number, device, dim = _kind(q)
         assert device == self.device, "the handle belongs to another device"
         if out is None:
-            out = _torch.empty_like(q)
+            out = _empty_like(q, stream)
         n, int32, rows = q_start.numel() - 1, _torch.int32, k.shape[0]
         assert n >= 0 and out.shape == q.shape and v.shape[0] == rows, "outputs, keys or values of other sizes"
         call = _CALL(number, dim, *_fields(q, dtype, device, dim), *_fields(k, dtype, device, dim),
