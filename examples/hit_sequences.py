@@ -3,8 +3,8 @@
     python examples/hit_sequences.py [hits per event] [events]
 
 The encoder puts the hits of every event of a batch in order of azimuth, normalises and rotates queries and keys
-(qk_norm_rope) and lets every hit attend to a window of that order and to a few global tokens at the start of its
-event (WindowAttention).  The decoder keeps keys and values of each track's hits in a cache: each step puts the new
+(qk_norm_rope) and lets every hit attend to a window of that order and to a few first tokens of its event, which stay
+visible to all (WindowAttention; those tokens themselves see the window of their own places).  The decoder keeps keys and values of each track's hits in a cache: each step puts the new
 hits' in their rows (the same call), attends with one query to a track, and drops the oldest hits by renumbering the
 rest (rope, on the cached keys).  Weights are random: this shows how the calls fit together, not a trained model."""
 import math
@@ -79,7 +79,7 @@ class TrackCache:
 
 
 def event_batch(hits, events, net):
-    """Embeddings [rows, hidden] of the hits of some events, each in order of azimuth behind its global tokens, the
+    """Embeddings [rows, hidden] of the hits of some events, each in order of azimuth behind its first tokens, the
     events' first rows and every row's position."""
     rows, starts = [], [0]
     for e in range(events):

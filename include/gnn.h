@@ -440,7 +440,8 @@ int gnn_qk_norm_rope(const gnn_rotary* rot, int dtype, int head_dim, float eps, 
  * out = sum over the visible j of softmax_j(scale * q . k_j) v_j, head by head; query head h reads key head
  * h / (q.n_heads / k.n_heads).  A query that sees no key, or whose visible scores are all -inf, gets zeros.
  * Keys that a query does not see take no part in its result, whatever they hold (NaN and infinities too),
- * nor do rows outside the sequence.
+ * nor do rows outside the sequence.  A row that comes out not finite is computed again, key by key, which is slow: a NaN
+ * that every query of a large event sees costs hundreds of times the call's time.
  *   dtype           GNN_DTYPE_BF16 or GNN_DTYPE_FP16, of q, k, v and out; scores, sums and outputs are held in
  *                   fp32, the weights that multiply v are rounded to dtype (their sum is not)
  *   head_dim        a multiple of 8, 8..128

@@ -15,8 +15,8 @@
 // all units of 64 keys, so that sequences of different lengths leave no SM idle.
 //
 // 64 sequences of 4,096 to 8,192 keys, 16 query and 4 key heads of 128, one query each: 0.127 ms, 6.4 TB/s, 94 % of the
-// copy rate; eight of up to 131,072 with three queries (16 rows, 249 registers, eight warps to an SM): 0.155 ms,
-// 5.3 TB/s.  One query over 1,028 keys: 9.3 us, seven of them dependent loads and the join.  Blocks of a fixed number
+// copy rate; eight of up to 131,072 with three queries (16 rows, 250 registers, eight warps to an SM): 0.155 ms,
+// 5.3 TB/s.  One query over 1,028 keys: 9.7 us, seven of them dependent loads and the join.  Blocks of a fixed number
 // of keys with the rows along M took 0.230 and 0.485 ms and 16.6 us.
 #pragma once
 #include "attend_tile.cuh"

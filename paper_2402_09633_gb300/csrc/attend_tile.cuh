@@ -5,8 +5,8 @@
 // stay on the old m, above 1 if need be.  Only blocks that some row of the tile sees are loaded; of those, parts that
 // no row of a warp sees cost no exponentials.
 //
-// What bounds it (event of 300,000 hits, two bf16 heads of 64, 512 neighbours to each side: 0.199 ms, 800 TFLOP/s of
-// visible products, tensor cores 36 % busy; causal 16,384, heads of 128, window 4,096: 0.181 ms, 1,364 TFLOP/s, 62 %):
+// What bounds it (event of 300,000 hits, two bf16 heads of 64, 512 neighbours to each side: 0.200 ms, 800 TFLOP/s of
+// visible products, tensor cores 36 % busy; causal 16,384, heads of 128, window 4,096: 0.186 ms, 1,330 TFLOP/s, 62 %):
 // a block's softmax is one chain of 1,200 cycles in a warp with 512 of them exponentials, two warps share a scheduler,
 // and tensor memory holds no third tile beside two.  Other splits lost: 16 rows to a warp in sixteen warps 0.36 ms,
 // two threads to a row 0.25, three tiles of 96 keys 0.26, one warp that issues whatever is ready 0.36 (its polls take
@@ -809,7 +809,8 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
       dirty = dirty || (row < rows && !(fabsf(odd.x + odd.y) < INFINITY));
     }
     // A weight of zero times a value that is not finite is NaN: rows that hold one are done again, key by visible
-    // key.  After everything else, so that nothing waits for it.
+    // key, also where the result cannot be finite.  After everything else, so that nothing waits for it.  (Event of 300,000
+    // hits: one NaN that 1,025 rows see takes it from 0.2 to 6.7 ms, one in a first token, which all rows see, to 100 ms.)
     if (ok && __any_sync(0xffffffffu, dirty)) {
       float* qs = reinterpret_cast<float*>(stage + warp * kStageBytes);
       __syncwarp();

@@ -16,8 +16,8 @@
 // token, so that a thread has up to 64 bytes on their way, and little else: an angle's sine and cosine are used
 // for both heads and forgotten, and computed again for the token's next two.  Keeping them through all heads took
 // 118 registers and left 15 warps to an SM.  Queries, keys and values are different blocks' work; frequencies and
-// gains lie in shared memory.  300,000 rows of two bf16 heads of 64: 28 us, 81 % of the copy rate (43 us with the
-// angles kept); with norms, keys and values 77 us, 89 % (137 us).
+// gains lie in shared memory.  300,000 rows of two bf16 heads of 64: 27 us, 84 % of the copy rate (43 us with the
+// angles kept); with norms, keys and values 74 us, 92 % (137 us).  In fp32 51 us, 89 %, and 144 us, 94 %.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
