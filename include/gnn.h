@@ -438,7 +438,9 @@ int gnn_qk_norm_rope(const gnn_rotary* rot, int dtype, int head_dim, float eps, 
  * position p = kv_len[b] - nq + i and sees key j when
  *   j <= p + right  and  (j >= p - left  or  j < sinks);      left, right < 0: no bound.
  * out = sum over the visible j of softmax_j(scale * q . k_j) v_j, head by head; query head h reads key head
- * h / (q.n_heads / k.n_heads).  A query that sees no key, or whose visible scores are all -inf, gets zeros.
+ * h / (q.n_heads / k.n_heads).  A query that sees no key, or whose visible scores are all -inf, gets zeros.  A scale of 0
+ * is taken as one too small to change a weight (a q . k_j of -inf weighs nothing then too).  An infinite value that a query
+ * sees makes its result infinite or, where the value's weight rounds to zero, NaN.
  * Keys that a query does not see take no part in its result, whatever they hold (NaN and infinities too),
  * nor do rows outside the sequence.  A row that comes out not finite is computed again, key by key, which is slow: a NaN
  * that every query of a large event sees costs hundreds of times the call's time.
