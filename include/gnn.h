@@ -490,6 +490,175 @@ int gnn_attention_run(gnn_attention* att, const gnn_attention_call* call, gnn_st
 int gnn_attention_status(gnn_attention* att, gnn_stream_t stream);
 void gnn_attention_destroy(gnn_attention* att);
 
+/*
+ * Several hypotheses of a sequence.  A decoder that extends tracks hit by hit keeps a few hypotheses (beams) of each
+ * event.  Their keys and values lie in pages, the event's own tokens once for all of them; the calls below append new
+ * rows, attend over the event's rows and each hypothesis' own, choose the best continuations and move the states
+ * to them.  (Library operators: the paper has no counterpart.)
+ *
+ * gnn_pages -- a cache in pages: position j of sequence b lies in row table[b * table_stride + j / page_size] * page_size
+ * + j % page_size of k and v, views of n_pages * page_size rows.
+ *   dtype, head_dim  of k and v
+ *   page_size     a power of two, 16..1024
+ *   table         device int32, n_seqs rows of table_width entries; entries that no position below kv_len uses are not
+ *                 read.  Sequences may have pages in common
+ *   kv_len        device int32 [n_seqs]: each sequence's positions, those of new rows among them
+ *   status        device uint32, zero before the first call: where calls report what they find
+ * Entries outside [0, n_pages), lengths outside the table's and offsets outside the views that a call is given are
+ * reported as INDEX_RANGE; no such row is read or written, and the results of the sequences that they belong to are
+ * undefined.  A cache is these arrays and nothing else: there is no handle, and calls on several streams may use one at once.
+ *
+ * gnn_paged_status -- read a status word behind the work of `stream` so far, clear it, and return what it said: GNN_OK,
+ * GNN_ERR_INDEX_RANGE, GNN_ERR_DEVICE_TIMEOUT or GNN_ERR_CUDA.  Waits for `stream`.  Errors: INVALID_ARG (NULL, misaligned).
+ */
+typedef struct gnn_pages {
+  gnn_heads k, v;
+  int64_t n_pages;
+  int32_t dtype, head_dim, page_size, table_width;
+  const int32_t* table;
+  int64_t table_stride;
+  const int32_t* kv_len;
+  int32_t n_seqs;
+  int32_t reserved;            /* 0 */
+  uint32_t* status;
+} gnn_pages;
+
+int gnn_paged_status(uint32_t* status, gnn_stream_t stream);
+
+/*
+ * gnn_paged_append -- new rows of keys and values into their pages.  Rows q_start[b] .. q_start[b + 1] - 1 are the last
+ * positions of sequence b, of kv_len[b] with them: each key is rotated (and normalised first, with eps > 0, as by
+ * gnn_qk_norm_rope) and written to its place, values are copied, and so are queries, when given, to q_out.  One launch.
+ *   rot              table of the rotation
+ *   q, q_out         views of n_rows rows, or data NULL in both: no queries.  q_out may be q (same strides)
+ *   k, v             views of n_rows rows with the cache's heads, which overlap no page
+ *   q_gain, k_gain   device float32 [head_dim], or NULL: 1; only with eps > 0
+ *   eps              0: no norms
+ *   positions        device, of the rotation, int32 [n_rows] or, with positions_float != 0, float32 [n_rows]; NULL: those in
+ *                    the sequences
+ *   q_start          device int32 [n_seqs + 1], not decreasing; rows before the first and from the last on are skipped
+ * A row whose position is below zero (a sequence with fewer positions than rows) is not written.  No place may be that of
+ * two rows.  Types, head_dim and limits as for gnn_rope.  Enqueued on `stream`; n_rows == 0 or n_seqs == 0 is a no-op.
+ * Errors: INVALID_ARG, CUDA.
+ */
+typedef struct gnn_append_call {
+  gnn_heads q, k, v, q_out;
+  const float* q_gain;
+  const float* k_gain;
+  const void* positions;
+  const int32_t* q_start;
+  int64_t n_rows;
+  float eps;
+  int32_t positions_float;
+} gnn_append_call;
+
+int gnn_paged_append(const gnn_pages* pages, const gnn_rotary* rot, const gnn_append_call* call, gnn_stream_t stream);
+
+/*
+ * gnn_paged_attend -- attention of new queries over a cache in pages.  Query i of the nq rows of sequence b stands at
+ * position p = kv_len[b] - nq + i and sees its keys j <= p:
+ *   out = sum over j of softmax_j(scale * q . k_j) v_j, head by head; query head h reads key head h / (q.n_heads /
+ * k.n_heads).  A query that sees no key, or whose scores are all -inf, gets zeros.
+ * Sequences group_start[g] .. group_start[g + 1] - 1 share their first shared_len[g] positions: those are read once for all
+ * of them, through the pages of the first.  (The others' entries for them are not read.)  Sequences of no group share nothing.
+ * What a query does not see takes no part in its result, whatever it holds.  An infinite or NaN value that a query sees
+ * makes its result infinite or NaN.  A scale of 0 is taken as one too small to change a weight.
+ *   pages            GNN_DTYPE_BF16 or GNN_DTYPE_FP16; head_dim a multiple of 8, 8..128; k, v: data 16-byte aligned,
+ *                    strides positive multiples of 8 elements
+ *   q, out           views of n_q_rows rows, in the same way; q.n_heads a multiple of the cache's heads, at most
+ *                    4096, and at most 128 query heads to a key head.  out overlaps no input
+ *   q_start          device int32 [n_seqs + 1], not decreasing; rows before the first and from the last on are not written
+ *   group_start      device int32 [n_groups + 1], not decreasing, and shared_len, device int32 [n_groups]; both NULL with
+ *                    n_groups 0.  n_groups <= n_seqs
+ *   max_q            the most queries of a sequence; 0: not known.  A sequence with more is INDEX_RANGE, its rows undefined
+ *   workspace        device, 16-byte aligned, of at least the bytes that gnn_paged_workspace says for the same call; written
+ *                    before it is read, so its contents need not be anything.  Calls that may overlap have one each
+ * A sequence some of whose queries stand below its group's shared_len is computed row by row, which is slow.  Scores, sums and
+ * outputs are held in fp32, the weights that multiply v are rounded to dtype (their sum is not).  Enqueued on
+ * `stream`; only enqueues kernels (it can be captured).  The same inputs give bitwise-identical outputs.
+ * Errors: INVALID_ARG (any limit above, a workspace that is too small), CUDA.
+ */
+typedef struct gnn_paged_call {
+  gnn_heads q, out;
+  const int32_t* q_start;
+  const int32_t* group_start;
+  const int32_t* shared_len;
+  int64_t n_q_rows;
+  int32_t n_groups, max_q;
+  float scale;
+  int32_t reserved;            /* 0 */
+  void* workspace;
+  uint64_t workspace_bytes;
+} gnn_paged_call;
+
+int gnn_paged_workspace(const gnn_pages* pages, const gnn_paged_call* call, uint64_t* bytes);
+int gnn_paged_attend(const gnn_pages* pages, const gnn_paged_call* call, gnn_stream_t stream);
+
+/*
+ * gnn_beam_select -- the best continuations of each group of `beams` hypotheses.  Hypothesis b (row b of logits, scores)
+ * goes on with token t at
+ *   value(b, t) = scores[b] + logits[b, t] - log(sum over t of exp(logits[b, t]))
+ * and the `best` largest values of a group's hypotheses and tokens come out in order, ties to the lowest
+ * (hypothesis, token): out_scores (value), out_parents (hypothesis, 0 .. beams - 1 within the group), out_tokens, each
+ * [n_groups * best].  A hypothesis that has ended (ended[b] != 0) has one continuation: token end_token at scores[b]; its
+ * logits are not read.  A value of -inf is no continuation; a row whose logits hold NaN or +inf, or whose score is
+ * NaN, has none.  Where there are fewer than `best`, the rest is -inf, parent 0, token -1.
+ * Values are held and compared to about 1e-7 (their order within a row is that of the logits, exactly).
+ *   dtype, logits    of any gnn_dtype, device [n_groups * beams, vocab], row_stride elements apart, aligned to elements
+ *   scores           device float32 [n_groups * beams];  ended  device uint8 [n_groups * beams], or NULL
+ *   beams, best      1..64;  vocab 1..GNN_MAX_COUNT
+ *   workspace        as for gnn_paged_attend, of the bytes that gnn_beam_workspace says
+ * The same inputs give bitwise-identical outputs.  Enqueued on `stream`; n_groups == 0 is a no-op.
+ * Errors: INVALID_ARG (n_groups * beams above GNN_MAX_COUNT too), CUDA.
+ */
+typedef struct gnn_beam_call {
+  const void* logits;
+  int64_t row_stride, n_groups;
+  const float* scores;
+  const uint8_t* ended;
+  int32_t dtype, beams, vocab, best, end_token;
+  int32_t reserved;            /* 0 */
+  float* out_scores;
+  int32_t* out_parents;
+  int32_t* out_tokens;
+  void* workspace;
+  uint64_t workspace_bytes;
+} gnn_beam_call;
+
+int gnn_beam_workspace(const gnn_beam_call* call, uint64_t* bytes);
+int gnn_beam_select(const gnn_beam_call* call, gnn_stream_t stream);
+
+/*
+ * gnn_beam_reorder -- states of hypotheses moved to those that continue them: in every group of `beams` slots, slot i of
+ * each of n_states arrays gets what slot parents[i] of it held.
+ *   parents          device int32 [n_groups * beams], 0 .. beams - 1 within the group; a slot whose parent is
+ *                    outside that keeps its own
+ *   states           host array; data has n_groups * beams rows of row_bytes bytes, `stride` bytes apart (stride >=
+ *                    row_bytes); out: the same out_stride bytes apart, or data itself (same strides): in place.  Arrays
+ *                    do not overlap otherwise
+ *   beams            1..64
+ * Enqueued on `stream`; no workspace.  Errors: INVALID_ARG, CUDA.
+ *
+ * gnn_paged_reorder -- the same for caches in pages, whose sequences are the hypotheses: n_caches caches (of a model's
+ * layers) that share one table and kv_len, n_seqs = n_groups * beams.  In place: a slot's entries for its parent's full
+ * pages become the parent's (such pages are shared from then on: append writes none of them), and the rows of the
+ * page that the parent has begun are copied into the slot's own page of the same number.  So every slot has, from its first page
+ * that is not full on, pages of its own.  kv_len is not written: the slots of a group have the same (a group whose
+ * slots have not is INDEX_RANGE, in the first cache's status, and is left as it is, and so is one where such a slot's own
+ * page is outside the pages).
+ * Types: any gnn_dtype.
+ */
+typedef struct gnn_beam_state {
+  void* data;
+  void* out;
+  int64_t stride, out_stride, row_bytes;
+} gnn_beam_state;
+
+int gnn_beam_reorder(const int32_t* parents, int64_t n_groups, int32_t beams, const gnn_beam_state* states, int32_t n_states,
+                     gnn_stream_t stream);
+int gnn_paged_reorder(const gnn_pages* caches, int32_t n_caches, const int32_t* parents, int64_t n_groups, int32_t beams,
+                      gnn_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,298 @@
+// Entry points for several hypotheses of a sequence: caches in pages, the choice of continuations, and moving states
+// (include/gnn.h).
+#include <cuda_runtime.h>
+#include <algorithm>
+#include <cmath>
+
+#include "../../include/gnn.h"
+#include "beam.cuh"
+#include "host.cuh"
+#include "paged.cuh"
+#include "sequence_host.cuh"
+
+using namespace gnn;
+
+namespace {
+
+constexpr int kPageLeast = 16, kPageMost = 1024;
+
+bool pages_ok(const gnn_pages* c) {
+  if (!c || c->reserved != 0 || c->dtype < GNN_DTYPE_FP32 || c->dtype > GNN_DTYPE_FP16) return false;
+  if (c->page_size < kPageLeast || c->page_size > kPageMost || (c->page_size & (c->page_size - 1))) return false;
+  if (c->n_pages < 1 || !count_ok(c->n_pages) || !count_ok(c->n_pages * c->page_size)) return false;
+  if (c->n_seqs < 0 || c->n_seqs > 1 << 28 || c->table_width < 1 || !count_ok(c->table_width)) return false;
+  if (c->table_stride < 0 || c->table_stride >= (int64_t)1 << 39) return false;
+  if (c->n_seqs > 0 && (!c->table || !c->kv_len || (uintptr_t)c->table % 4 || (uintptr_t)c->kv_len % 4)) return false;
+  if (c->head_dim < 1 || c->head_dim > 2 * kRotMaxPairs) return false;
+  return c->status && (uintptr_t)c->status % 4 == 0 && view_ok(&c->k, c->dtype) && view_ok(&c->v, c->dtype) &&
+         c->k.n_heads == c->v.n_heads;
+}
+
+int log2_of(int n) {
+  int s = 0;
+  while (1 << s < n) ++s;
+  return s;
+}
+
+// A view that the attention reads in pieces of 16 bytes.
+bool wide_ok(const gnn_heads& v, int dtype) {
+  return view_ok(&v, dtype) && (uintptr_t)v.data % 16 == 0 && v.row_stride > 0 && v.row_stride % 8 == 0 && v.head_stride % 8 == 0 &&
+         (v.n_heads == 1 || v.head_stride > 0);
+}
+
+bool attend_ok(const gnn_pages* c, const gnn_paged_call* a) {
+  if (!pages_ok(c) || !a || a->reserved != 0 || c->dtype == GNN_DTYPE_FP32) return false;
+  if (c->head_dim < 8 || c->head_dim > 128 || c->head_dim % 8 != 0 || !std::isfinite(a->scale)) return false;
+  if (!count_ok(a->n_q_rows) || a->max_q < 0 || a->n_groups < 0 || a->n_groups > c->n_seqs) return false;
+  if ((a->n_groups > 0) != (a->group_start != nullptr) || (a->group_start != nullptr) != (a->shared_len != nullptr)) return false;
+  if ((uintptr_t)a->group_start % 4 || (uintptr_t)a->shared_len % 4) return false;
+  if (!wide_ok(c->k, c->dtype) || !wide_ok(c->v, c->dtype)) return false;
+  if (a->n_q_rows == 0 || c->n_seqs == 0) return true;
+  if (!a->q_start || (uintptr_t)a->q_start % 4 || !wide_ok(a->q, c->dtype) || !wide_ok(a->out, c->dtype)) return false;
+  if (a->q.n_heads != a->out.n_heads || a->q.n_heads > 4096 || a->q.n_heads % c->k.n_heads) return false;
+  return a->q.n_heads / c->k.n_heads <= 128;
+}
+
+bool beam_ok(const gnn_beam_call* c) {
+  if (!c || c->reserved != 0 || c->dtype < GNN_DTYPE_FP32 || c->dtype > GNN_DTYPE_FP16) return false;
+  if (c->beams < 1 || c->beams > kBeamMost || c->best < 1 || c->best > kBeamMost || c->vocab < 1 || !count_ok(c->vocab))
+    return false;
+  return count_ok(c->n_groups) && count_ok(c->n_groups * c->beams) && c->row_stride >= 0 && c->row_stride < (int64_t)1 << 39;
+}
+
+// Strips of a row: enough blocks for every SM, of at least two chunks each.
+int beam_strips(const gnn_beam_call* c, int n_sm) {
+  const int64_t rows = c->n_groups * c->beams, chunk = kStripThreads * 32 / elem_bytes(c->dtype);
+  const int64_t want = (4 * (int64_t)n_sm + rows - 1) / rows, most = (c->vocab + 2 * chunk - 1) / (2 * chunk);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), kStripsMost));
+}
+
+constexpr int kMostSms = 160;        // that strips are counted for where no device need be asked
+
+uint64_t beam_bytes(const gnn_beam_call* c) {
+  const uint64_t strips = (uint64_t)c->n_groups * c->beams * beam_strips(c, kMostSms);
+  return strips * (sizeof(BeamSum) + 8 * (uint64_t)c->best);
+}
+
+int width_of(uintptr_t bits) { return bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 1; }
+
+// Launches over `what` states or pools of columns of at most `columns` each.
+int run_moves(MoveParams& p, int what, int64_t columns, cudaStream_t st) {
+  const int sms = device_sms();
+  if (!sms) return cuda_fail(cudaGetLastError());
+  // segments for a few rounds of all SMs, at least a block's columns each
+  const int64_t want = (16 * (int64_t)sms + p.groups * what - 1) / (p.groups * what);
+  p.segments = (int)std::max<int64_t>(1, std::min<int64_t>(want, (columns + kMoveThreads - 1) / kMoveThreads));
+  if (p.groups * what * p.segments >= (int64_t)1 << 31) return GNN_ERR_INVALID_ARG;
+  const size_t smem = (size_t)p.beams * kMoveThreads * 16;
+  cudaError_t err = cudaFuncSetAttribute(beam_move_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBeamMost * kMoveThreads * 16);
+  if (err == cudaSuccess)
+    err = launch_pdl(beam_move_kernel, (unsigned)(p.groups * what * p.segments), kMoveThreads, smem, st, p);
+  return err == cudaSuccess ? GNN_OK : cuda_fail(err);
+}
+
+}  // namespace
+
+extern "C" {
+
+int gnn_paged_status(uint32_t* status, gnn_stream_t stream) {
+  if (!status || (uintptr_t)status % 4) return GNN_ERR_INVALID_ARG;
+  const cudaStream_t st = (cudaStream_t)stream;
+  uint32_t word = 0;
+  cudaError_t err = cudaMemcpyAsync(&word, status, 4, cudaMemcpyDeviceToHost, st);
+  if (err == cudaSuccess) err = cudaMemsetAsync(status, 0, 4, st);
+  const cudaError_t done = cudaStreamSynchronize(st);          // whatever failed: the copy writes to this frame
+  if (err == cudaSuccess) err = done;
+  if (err != cudaSuccess) return cuda_fail(err);
+  if (word & DEV_ERR_TIMEOUT) return GNN_ERR_DEVICE_TIMEOUT;
+  if (word & DEV_ERR_INDEX_RANGE) return GNN_ERR_INDEX_RANGE;
+  return GNN_OK;
+}
+
+int gnn_paged_append(const gnn_pages* c, const gnn_rotary* rot, const gnn_append_call* a, gnn_stream_t stream) {
+  if (!a || !pages_ok(c) || !rotary_args_ok(rot, c->dtype, c->head_dim, a->n_rows, a->positions)) return GNN_ERR_INVALID_ARG;
+  if (!std::isfinite(a->eps) || a->eps < 0.f || (uintptr_t)a->q_gain % 4 || (uintptr_t)a->k_gain % 4 || (uintptr_t)a->q_start % 4)
+    return GNN_ERR_INVALID_ARG;
+  if (a->eps == 0.f && (a->q_gain || a->k_gain)) return GNN_ERR_INVALID_ARG;
+  if (a->n_rows == 0 || c->n_seqs == 0) return GNN_OK;
+  if (!a->q_start || (a->q.data != nullptr) != (a->q_out.data != nullptr)) return GNN_ERR_INVALID_ARG;
+  const gnn_heads* in[3] = {&a->q, &a->k, &a->v};
+  const gnn_heads* out[3] = {&a->q_out, &c->k, &c->v};
+  RotaryParams p = {};
+  for (int i = a->q.data ? 0 : 1; i < 3; ++i) {
+    if (!view_ok(in[i], c->dtype) || !view_ok(out[i], c->dtype) || in[i]->n_heads != out[i]->n_heads) return GNN_ERR_INVALID_ARG;
+    p.in[i] = view(*in[i], c->dtype);
+    p.out[i] = view(*out[i], c->dtype);
+    p.heads[i] = in[i]->n_heads;
+  }
+  p.gain[0] = a->q_gain;
+  p.gain[1] = a->k_gain;
+  p.eps = a->eps;
+  p.pages = {a->q_start, c->kv_len, c->table, c->table_stride, c->n_pages, c->n_seqs, c->table_width, log2_of(c->page_size), c->status};
+  return run_rotary<true>(rot, c->dtype, c->head_dim, p, a->eps > 0.f, a->positions, a->positions_float, a->n_rows,
+                          (cudaStream_t)stream);
+}
+
+int gnn_paged_workspace(const gnn_pages* c, const gnn_paged_call* a, uint64_t* bytes) {
+  if (!bytes || !attend_ok(c, a)) return GNN_ERR_INVALID_ARG;
+  *bytes = 0;
+  return GNN_OK;
+}
+
+int gnn_paged_attend(const gnn_pages* c, const gnn_paged_call* a, gnn_stream_t stream) {
+  if (!attend_ok(c, a)) return GNN_ERR_INVALID_ARG;
+  if (a->n_q_rows == 0 || c->n_seqs == 0) return GNN_OK;
+  PagedParams p = {};
+  p.q = view(a->q, c->dtype);
+  p.k = view(c->k, c->dtype);
+  p.v = view(c->v, c->dtype);
+  p.out = view(a->out, c->dtype);
+  p.q_start = a->q_start;
+  p.kv_len = c->kv_len;
+  p.table = c->table;
+  p.group_start = a->group_start;
+  p.shared_len = a->shared_len;
+  p.table_stride = c->table_stride;
+  p.n_pages = c->n_pages;
+  p.n_q_rows = (int)a->n_q_rows;
+  p.n_seqs = c->n_seqs;
+  p.n_groups = a->n_groups;
+  p.width = c->table_width;
+  p.shift = log2_of(c->page_size);
+  p.max_q = (int)(a->max_q > 0 ? std::min<int64_t>(a->max_q, a->n_q_rows) : a->n_q_rows);
+  p.heads = a->q.n_heads;
+  p.kv_heads = c->k.n_heads;
+  p.dim = c->head_dim;
+  // a scale of zero as one too small to be seen, so that -inf, a score that is not seen, stays -inf
+  p.scale_log2 = a->scale == 0.f ? 1e-30f : (float)((double)a->scale * 1.4426950408889634);
+  p.err = c->status;
+  const int64_t blocks = ((int64_t)p.n_q_rows * p.heads + kPagedRowWarps - 1) / kPagedRowWarps;
+  const unsigned grid = (unsigned)std::min<int64_t>(blocks, 16 * (int64_t)device_sms());
+  const cudaError_t err = c->dtype == GNN_DTYPE_BF16
+                              ? launch_pdl(paged_rows_kernel<__nv_bfloat16>, grid, 32 * kPagedRowWarps, 0, (cudaStream_t)stream, p)
+                              : launch_pdl(paged_rows_kernel<__half>, grid, 32 * kPagedRowWarps, 0, (cudaStream_t)stream, p);
+  return err == cudaSuccess ? GNN_OK : cuda_fail(err);
+}
+
+int gnn_beam_workspace(const gnn_beam_call* c, uint64_t* bytes) {
+  if (!bytes || !beam_ok(c)) return GNN_ERR_INVALID_ARG;
+  *bytes = c->n_groups == 0 ? 0 : beam_bytes(c);
+  return GNN_OK;
+}
+
+int gnn_beam_select(const gnn_beam_call* c, gnn_stream_t stream) {
+  if (!beam_ok(c)) return GNN_ERR_INVALID_ARG;
+  if (c->n_groups == 0) return GNN_OK;
+  if (!c->logits || !c->scores || !c->out_scores || !c->out_parents || !c->out_tokens || !c->workspace) return GNN_ERR_INVALID_ARG;
+  if ((uintptr_t)c->logits % elem_bytes(c->dtype) || (uintptr_t)c->scores % 4 || (uintptr_t)c->out_scores % 4 ||
+      (uintptr_t)c->out_parents % 4 || (uintptr_t)c->out_tokens % 4 || (uintptr_t)c->workspace % 16 ||
+      c->workspace_bytes < beam_bytes(c))
+    return GNN_ERR_INVALID_ARG;
+  BeamParams p = {};
+  p.x = c->logits;
+  p.stride = c->row_stride;
+  p.score = c->scores;
+  p.ended = c->ended;
+  p.end = c->end_token;
+  p.beams = c->beams;
+  p.vocab = c->vocab;
+  p.best = c->best;
+  p.strips = beam_strips(c, kMostSms);
+  p.rows = c->n_groups * c->beams;
+  if (p.rows * p.strips >= (int64_t)1 << 31) p.strips = 1;
+  p.sums = static_cast<BeamSum*>(c->workspace);
+  p.lists = reinterpret_cast<uint64_t*>(p.sums + p.rows * p.strips);
+  p.out_score = c->out_scores;
+  p.out_parent = c->out_parents;
+  p.out_token = c->out_tokens;
+  const cudaStream_t st = (cudaStream_t)stream;
+  const unsigned grid = (unsigned)(p.rows * p.strips);
+  cudaError_t err = c->dtype == GNN_DTYPE_FP32   ? launch_pdl(beam_strip_kernel<float>, grid, kStripThreads, 0, st, p)
+                    : c->dtype == GNN_DTYPE_BF16 ? launch_pdl(beam_strip_kernel<__nv_bfloat16>, grid, kStripThreads, 0, st, p)
+                                                 : launch_pdl(beam_strip_kernel<__half>, grid, kStripThreads, 0, st, p);
+  if (err == cudaSuccess) err = launch_pdl(beam_join_kernel, (unsigned)c->n_groups, 32 * kJoinWarps, 0, st, p);
+  return err == cudaSuccess ? GNN_OK : cuda_fail(err);
+}
+
+int gnn_beam_reorder(const int32_t* parents, int64_t n_groups, int32_t beams, const gnn_beam_state* states, int32_t n_states,
+                     gnn_stream_t stream) {
+  if (beams < 1 || beams > kBeamMost || !count_ok(n_groups) || !count_ok(n_groups * beams) || n_states < 0 || (n_states > 0 && !states) ||
+      (uintptr_t)parents % 4)
+    return GNN_ERR_INVALID_ARG;
+  for (int i = 0; i < n_states; ++i) {
+    const gnn_beam_state& s = states[i];
+    const int64_t most = (int64_t)1 << 39;
+    if (s.row_bytes < 0 || s.stride < s.row_bytes || s.out_stride < s.row_bytes || s.stride >= most || s.out_stride >= most ||
+        (s.out == s.data && s.out_stride != s.stride))
+      return GNN_ERR_INVALID_ARG;
+    if (n_groups > 0 && s.row_bytes > 0 && (!s.data || !s.out)) return GNN_ERR_INVALID_ARG;
+  }
+  if (n_groups == 0) return GNN_OK;
+  if (!parents) return GNN_ERR_INVALID_ARG;
+  MoveParams p = {};
+  p.parent = parents;
+  p.groups = n_groups;
+  p.beams = beams;
+  int64_t columns = 0;
+  for (int i = 0; i < n_states; ++i) {
+    const gnn_beam_state& s = states[i];
+    if (s.row_bytes > 0) {
+      const int w = width_of((uintptr_t)s.data | (uintptr_t)s.out | (uintptr_t)s.stride | (uintptr_t)s.out_stride | (uintptr_t)s.row_bytes);
+      p.state[p.states++] = {static_cast<char*>(s.data), static_cast<char*>(s.out), s.stride, s.out_stride, s.row_bytes, w};
+      columns = std::max(columns, s.row_bytes / w);
+    }
+    if (p.states == 0 || (p.states < kMoveStates && i + 1 < n_states)) continue;
+    const int rc = run_moves(p, p.states, columns, (cudaStream_t)stream);
+    if (rc != GNN_OK) return rc;
+    p.states = 0;
+    columns = 0;
+  }
+  return GNN_OK;
+}
+
+int gnn_paged_reorder(const gnn_pages* caches, int32_t n_caches, const int32_t* parents, int64_t n_groups,
+                      int32_t beams, gnn_stream_t stream) {
+  if (n_caches < 1 || !caches || beams < 1 || beams > kBeamMost || !count_ok(n_groups) || !count_ok(n_groups * beams) ||
+      (uintptr_t)parents % 4)
+    return GNN_ERR_INVALID_ARG;
+  const gnn_pages& c = caches[0];
+  for (int i = 0; i < n_caches; ++i) {
+    const gnn_pages& x = caches[i];
+    if (!pages_ok(&x) || x.n_seqs != n_groups * beams || x.table != c.table || x.kv_len != c.kv_len || x.page_size != c.page_size ||
+        x.table_stride != c.table_stride || x.table_width != c.table_width || x.n_pages != c.n_pages)
+      return GNN_ERR_INVALID_ARG;
+  }
+  if (n_groups == 0) return GNN_OK;
+  if (!parents) return GNN_ERR_INVALID_ARG;
+  MoveParams p = {};
+  p.parent = parents;
+  p.groups = n_groups;
+  p.beams = beams;
+  p.table = const_cast<int*>(c.table);
+  p.kv_len = c.kv_len;
+  p.table_stride = c.table_stride;
+  p.n_pages = c.n_pages;
+  p.table_width = c.table_width;
+  p.shift = log2_of(c.page_size);
+  p.err = c.status;
+  for (int i = 0; i < 2 * n_caches;) {
+    int64_t columns = 1;
+    p.pools = 0;
+    for (; i < 2 * n_caches && p.pools < kMoveStates; ++i) {
+      const gnn_pages& x = caches[i / 2];
+      const HeadsView v = view(i % 2 ? x.v : x.k, x.dtype);
+      const int bytes = x.head_dim * elem_bytes(x.dtype);
+      const int w = width_of((uintptr_t)v.data | (uintptr_t)v.row_bytes | (uintptr_t)v.head_bytes | (uintptr_t)bytes);
+      if (p.pools > 0 && bytes != p.dim_bytes) break;
+      p.dim_bytes = bytes;
+      p.pool[p.pools++] = {v.data, v.row_bytes, v.head_bytes, x.k.n_heads, w};
+      columns = std::max<int64_t>(columns, (int64_t)x.page_size * x.k.n_heads * (bytes / w));
+    }
+    // the table last: the launches before only read it
+    const int err = run_moves(p, p.pools + (i == 2 * n_caches ? 1 : 0), columns, (cudaStream_t)stream);
+    if (err != GNN_OK) return err;
+  }
+  return GNN_OK;
+}
+
+}  // extern "C"

@@ -34,6 +34,46 @@ struct HeadsView {                   // [rows, heads, D], elements of a head con
   int64_t row_bytes, head_bytes;
 };
 
+// Where rows of sequences lie in pages: position p of sequence b is row table[b][p / page] * page + p % page.
+struct PagedRows {
+  const int* q_start;                // [n_seqs + 1]: a sequence's new rows
+  const int* kv_len;                 // [n_seqs]: its positions, the new rows' among them
+  const int* table;
+  int64_t table_stride, n_pages;
+  int n_seqs, width, shift;          // entries of a sequence's row of the table; pages have 2^shift rows
+  uint32_t* err;
+};
+
+// The sequence that row t belongs to, the last that starts at or before it; -1 when there is none.  Looks first where
+// sequences of one length would have it.
+__device__ __forceinline__ int sequence_of(const int* start, int n_seqs, int64_t rows, int t) {
+  int a = (int)((int64_t)t * n_seqs / rows), z = n_seqs;
+  a = min(a, n_seqs - 1);
+  if (t >= start[a] && t < start[a + 1]) return a;
+  a = 0;
+#pragma unroll 1
+  while (z - a > 1) {
+    const int mid = (int)(((int64_t)a + z) / 2);
+    if (start[mid] <= t) a = mid; else z = mid;
+  }
+  return t >= start[a] && t < start[a + 1] ? a : -1;
+}
+
+struct PagedPlace { int seq, pos; int64_t row; };      // seq -1: of no sequence; row -1: nowhere
+__device__ __forceinline__ PagedPlace paged_place(const PagedRows& g, int64_t rows, int t) {
+  PagedPlace at = {sequence_of(g.q_start, g.n_seqs, rows, t), 0, -1};
+  if (at.seq < 0) return at;
+  const int end = g.q_start[at.seq + 1];
+  if (end > rows) atomicOr(g.err, DEV_ERR_INDEX_RANGE);
+  at.pos = (int)((int64_t)g.kv_len[at.seq] - min((int64_t)end, rows) + t);
+  if (at.pos < 0) return at;                           // a sequence shorter than its rows: what has no position
+  const int entry = at.pos >> g.shift;
+  const int page = entry < g.width ? g.table[(int64_t)at.seq * g.table_stride + entry] : -1;
+  if (page >= 0 && page < g.n_pages) at.row = ((int64_t)page << g.shift) + (at.pos & ((1 << g.shift) - 1));
+  else atomicOr(g.err, DEV_ERR_INDEX_RANGE);
+  return at;
+}
+
 struct RotaryParams {
   HeadsView in[3], out[3];           // queries, keys (rotated, normed), values (copied)
   int heads[3];
@@ -47,6 +87,7 @@ struct RotaryParams {
   const float* gain[2];              // of queries and of keys, or null
   uint64_t fixed[kRotMaxPairs];      // turns a position, in 2^-64 turns (modulo a turn)
   float hi[kRotMaxPairs], lo[kRotMaxPairs];   // the same as a sum of floats
+  PagedRows pages;                   // where keys and values go, and the positions, of the paged form
 };
 
 template <typename T> __device__ __forceinline__ float to_f(T x);
@@ -84,9 +125,12 @@ __device__ __forceinline__ float turns_whole(int x, uint64_t fixed) {
   return (float)(int)((fixed * (uint64_t)(int64_t)x + 0x80000000u) >> 32) * 0x1p-32f;
 }
 
+// PAGED: rows are those of sequences, and keys and values go to their places in pages; without positions of their own
+// the rows' are those in their sequences.
+//
 // V pairs to a unit.  V == 1 takes any even R and any alignment that elements have; larger V need R and D to
 // be multiples of 2V and addresses and strides of V elements.
-template <typename T, int V, bool INTER, bool NORM>
+template <typename T, int V, bool INTER, bool NORM, bool PAGED = false>
 __global__ void __launch_bounds__(kRotThreads, V >= 8 ? 4 : 5) rotary_kernel(const __grid_constant__ RotaryParams p) {
   constexpr int UPL = V >= 4 ? 1 : 4 / V;          // units a lane may own: D <= 256
   constexpr int MOST = 2 * kRotMaxPairs / (2 * V); // units of a row
@@ -134,10 +178,20 @@ __global__ void __launch_bounds__(kRotThreads, V >= 8 ? 4 : 5) rotary_kernel(con
           xw[b][u] = *reinterpret_cast<const Pack<T, V>*>(head + (half ? i + pairs : 2 * i + V) * sizeof(T));
         }
       }
-    const int64_t row = part == 0 || !p.rows ? t : p.rows[t];
-    const bool store = task < tasks && (part == 0 || !p.rows || (row >= 0 && row < p.out_rows));
+    int64_t row;
+    bool store;
+    int own_pos = (int)t;
+    if constexpr (PAGED) {
+      const PagedPlace place = paged_place(p.pages, p.tokens, (int)t);
+      row = part == 0 ? t : place.row;
+      store = task < tasks && place.seq >= 0 && row >= 0;
+      own_pos = place.pos;
+    } else {
+      row = part == 0 || !p.rows ? t : p.rows[t];
+      store = task < tasks && (part == 0 || !p.rows || (row >= 0 && row < p.out_rows));
+    }
     if (!copy) {
-      const int pos = !p.pos ? (int)t : static_cast<const int*>(p.pos)[t];     // or a float's bits
+      const int pos = !p.pos ? own_pos : static_cast<const int*>(p.pos)[t];     // or a float's bits
       float r[2] = {1.f, 1.f};
       if (NORM) {
 #pragma unroll

@@ -13,6 +13,7 @@
 #include "attend_tile.cuh"
 #include "host.cuh"
 #include "rotary.cuh"
+#include "sequence_host.cuh"
 
 using namespace gnn;
 
@@ -34,104 +35,7 @@ void free_attention(gnn_attention* a) {
   delete a;
 }
 
-constexpr int32_t kRotaryMagic = 0x54524E47;       // "GNRT"
 constexpr double kTwoPi = 6.283185307179586476925286766559;
-
-int elem_bytes(int dtype) { return dtype == GNN_DTYPE_FP32 ? 4 : 2; }
-
-// A view whose elements are aligned, with strides that may be used; the furthest element stays within 2^62 bytes.
-bool view_ok(const gnn_heads* h, int dtype) {
-  if (!h || !h->data || h->n_heads < 1 || h->n_heads > (1 << 20) || h->reserved != 0) return false;
-  if ((uintptr_t)h->data % elem_bytes(dtype) != 0) return false;
-  return h->row_stride >= 0 && h->head_stride >= 0 && h->row_stride < (int64_t)1 << 39 &&
-         h->head_stride < (int64_t)1 << 39;
-}
-
-HeadsView view(const gnn_heads& h, int dtype) {
-  const int64_t e = elem_bytes(dtype);
-  return {static_cast<char*>(h.data), h.row_stride * e, h.head_stride * e};
-}
-
-bool lies_on(const HeadsView& v, int64_t bytes) {
-  return (uintptr_t)v.data % bytes == 0 && v.row_bytes % bytes == 0 && v.head_bytes % bytes == 0;
-}
-
-template <typename T, int V>
-cudaError_t launch_rotary(const RotaryParams& p, bool inter, bool norm, unsigned grid, cudaStream_t st) {
-  if (norm)
-    return inter ? launch_pdl(rotary_kernel<T, V, true, true>, grid, kRotThreads, 0, st, p)
-                 : launch_pdl(rotary_kernel<T, V, false, true>, grid, kRotThreads, 0, st, p);
-  return inter ? launch_pdl(rotary_kernel<T, V, true, false>, grid, kRotThreads, 0, st, p)
-               : launch_pdl(rotary_kernel<T, V, false, false>, grid, kRotThreads, 0, st, p);
-}
-
-int device_sms() {
-  int dev = 0, n = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return 0;
-  if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-  return n;
-}
-
-// Fills the shared fields and launches; p.in, p.out, p.heads, p.gain, p.rows and p.eps are set.
-int run_rotary(const gnn_rotary* rot, int dtype, int head_dim, RotaryParams& p, bool norm, const void* positions,
-               int positions_float, int64_t n_rows, cudaStream_t st) {
-  p.dim = head_dim;
-  p.rot = rot->rot_dim;
-  p.tokens = n_rows;
-  p.pos = positions;
-  p.pos_float = positions && positions_float;
-  p.amplitude = rot->amplitude;
-  std::memcpy(p.fixed, rot->turn_fixed, sizeof p.fixed);
-  std::memcpy(p.hi, rot->turn_hi, sizeof p.hi);
-  std::memcpy(p.lo, rot->turn_lo, sizeof p.lo);
-  const bool inter = rot->layout == GNN_ROTARY_INTERLEAVED;
-  const int e = elem_bytes(dtype);
-  // the most pairs to a unit (8 in 16-bit types, 4, 2 or 1) that head_dim, rot_dim and how the views lie allow
-  int V = dtype == GNN_DTYPE_FP32 ? 4 : 8;
-  for (; V > 1; V /= 2) {
-    bool ok = head_dim % (2 * V) == 0 && p.rot % (2 * V) == 0;
-    for (int i = 0; i < 3; ++i)
-      if (p.heads[i]) ok = ok && lies_on(p.in[i], V * e) && lies_on(p.out[i], V * e);
-    if (ok) break;
-  }
-  p.units = head_dim / (2 * V);
-  p.group = 1;
-  while (p.group < p.units && p.group < 32) p.group *= 2;
-  const int sms = device_sms();
-  if (!sms) return cuda_fail(cudaGetLastError());
-  // Blocks for one round of all tasks (two heads of a token), six to an SM at most, shared out by heads.
-  const int heads = p.heads[0] + p.heads[1] + p.heads[2], per_block = kRotThreads / p.group;
-  unsigned grid = 0;
-  for (int i = 0; i < 3; ++i) {
-    p.block0[i] = grid;
-    if (!p.heads[i]) continue;
-    const int64_t blocks = (n_rows * ((p.heads[i] + 1) / 2) + per_block - 1) / per_block;
-    grid += (unsigned)std::min<int64_t>(blocks, std::max<int64_t>(1, (int64_t)sms * 6 * p.heads[i] / heads));
-  }
-  p.block0[3] = grid;
-  cudaError_t err;
-  if (dtype == GNN_DTYPE_FP32)
-    err = V == 4   ? launch_rotary<float, 4>(p, inter, norm, grid, st)
-          : V == 2 ? launch_rotary<float, 2>(p, inter, norm, grid, st)
-                   : launch_rotary<float, 1>(p, inter, norm, grid, st);
-  else if (dtype == GNN_DTYPE_BF16)
-    err = V == 8   ? launch_rotary<__nv_bfloat16, 8>(p, inter, norm, grid, st)
-          : V == 4 ? launch_rotary<__nv_bfloat16, 4>(p, inter, norm, grid, st)
-          : V == 2 ? launch_rotary<__nv_bfloat16, 2>(p, inter, norm, grid, st)
-                   : launch_rotary<__nv_bfloat16, 1>(p, inter, norm, grid, st);
-  else
-    err = V == 8   ? launch_rotary<__half, 8>(p, inter, norm, grid, st)
-          : V == 4 ? launch_rotary<__half, 4>(p, inter, norm, grid, st)
-          : V == 2 ? launch_rotary<__half, 2>(p, inter, norm, grid, st)
-                   : launch_rotary<__half, 1>(p, inter, norm, grid, st);
-  return err == cudaSuccess ? GNN_OK : cuda_fail(err);
-}
-
-bool rotary_args_ok(const gnn_rotary* rot, int dtype, int head_dim, int64_t n_rows, const void* positions) {
-  if (!rot || rot->magic != kRotaryMagic || dtype < GNN_DTYPE_FP32 || dtype > GNN_DTYPE_FP16) return false;
-  if (head_dim < rot->rot_dim || head_dim > 2 * kRotMaxPairs || head_dim % 2 != 0) return false;
-  return count_ok(n_rows) && (uintptr_t)positions % 4 == 0;
-}
 
 // Boxes of box_rows rows x 64 elements of one head, in the 128-byte swizzle; what lies outside reads as zeros.
 bool encode_map(const gnn_attention* a, CUtensorMap* map, const gnn_heads& h, int64_t rows, int dtype, int dim,
@@ -287,7 +191,7 @@ int gnn_rope(const gnn_rotary* rot, int dtype, int head_dim, const gnn_heads* x,
   p.in[0] = view(*x, dtype);
   p.out[0] = view(*y, dtype);
   p.heads[0] = x->n_heads;
-  return run_rotary(rot, dtype, head_dim, p, false, positions, positions_float, n_rows, (cudaStream_t)stream);
+  return run_rotary<false>(rot, dtype, head_dim, p, false, positions, positions_float, n_rows, (cudaStream_t)stream);
 }
 
 int gnn_qk_norm_rope(const gnn_rotary* rot, int dtype, int head_dim, float eps, const float* q_gain,
@@ -316,7 +220,7 @@ int gnn_qk_norm_rope(const gnn_rotary* rot, int dtype, int head_dim, float eps, 
   p.rows = rows;
   p.out_rows = out_rows;
   p.eps = eps;
-  return run_rotary(rot, dtype, head_dim, p, true, positions, positions_float, n_rows, (cudaStream_t)stream);
+  return run_rotary<false>(rot, dtype, head_dim, p, true, positions, positions_float, n_rows, (cudaStream_t)stream);
 }
 
 int gnn_attention_create(gnn_attention** out) {
