@@ -566,13 +566,16 @@ int gnn_paged_append(const gnn_pages* pages, const gnn_rotary* rot, const gnn_ap
  *   pages            GNN_DTYPE_BF16 or GNN_DTYPE_FP16; head_dim a multiple of 8, 8..128; k, v: data 16-byte aligned,
  *                    strides positive multiples of 8 elements
  *   q, out           views of n_q_rows rows, in the same way; q.n_heads a multiple of the cache's heads, at most
- *                    4096, and at most 128 query heads to a key head.  out overlaps no input
+ *                    4096, at most 128 query heads to a key head, and fewer than 2^32 query rows times heads.  out overlaps no
+ *                    input
  *   q_start          device int32 [n_seqs + 1], not decreasing; rows before the first and from the last on are not written
  *   group_start      device int32 [n_groups + 1], not decreasing, and shared_len, device int32 [n_groups]; both NULL with
  *                    n_groups 0.  n_groups <= n_seqs
  *   max_q            the most queries of a sequence; 0: not known.  A sequence with more is INDEX_RANGE, its rows undefined
- *   workspace        device, 16-byte aligned, of at least the bytes that gnn_paged_workspace says for the same call; written
- *                    before it is read, so its contents need not be anything.  Calls that may overlap have one each
+ *   workspace        device, 32-byte aligned, of at least the bytes that gnn_paged_workspace says for the same call; written
+ *                    before it is read, so its contents need not be anything.  Calls that may overlap have one each.
+ *                    About 8 head_dim bytes for each query row and head, and more for groups and short rows: the call is
+ *                    for few new rows at a time, not for whole prompts
  * A sequence some of whose queries stand below its group's shared_len is computed row by row, which is slow.  Scores, sums and
  * outputs are held in fp32, the weights that multiply v are rounded to dtype (their sum is not).  Enqueued on
  * `stream`; only enqueues kernels (it can be captured).  The same inputs give bitwise-identical outputs.

@@ -14,7 +14,7 @@ LIB = os.path.join(HERE, "libgnn_gb300.so")
 SOURCES = [os.path.join(HERE, "csrc", f) for f in ("gnn_api.cu", "seq_api.cu", "paged_api.cu")]
 DEPS = SOURCES + [os.path.join(HERE, "csrc", f) for f in ("ptx.cuh", "csr.cuh", "mlp_tiles.cuh", "components.cuh", "compact.cuh", "frnn.cuh",
                                                             "host.cuh", "rotary.cuh", "attend.cuh", "attend_tile.cuh",
-                                                            "attend_few.cuh", "attend_ptx.cuh", "sequence_host.cuh", "paged.cuh", "beam.cuh")] + \
+                                                            "attend_few.cuh", "attend_ptx.cuh", "sequence_host.cuh", "paged.cuh", "paged_tile.cuh", "beam.cuh")] + \
     [os.path.join(ROOT, "include", "gnn.h")]
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 FLAGS = ["-gencode", "arch=compute_103a,code=sm_103a", "-O3", "-lineinfo", "-std=c++17",

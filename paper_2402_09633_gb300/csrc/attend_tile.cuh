@@ -92,7 +92,7 @@ __device__ __forceinline__ AttendTile attend_tile(const AttendParams& p, const S
 // Item `at`: false when it has no rows.  Sequence b's items start at slot group (q0 / 128 + b) / tiles + b, which leaves
 // room for all of them and needs no sum over the sequences before it.  (Slots and tiles are below 2^31; the divisions
 // are in 32 bits, as 64 bits take thousands of cycles here.)
-__device__ __noinline__ bool attend_item(const AttendParams& p, const AttendGrid& g, int64_t at, AttendItem& it) {
+static __device__ __noinline__ bool attend_item(const AttendParams& p, const AttendGrid& g, int64_t at, AttendItem& it) {
   const uint32_t heads = (uint32_t)p.kv_heads, group = (uint32_t)g.group, tiles = (uint32_t)g.tiles;
   const uint32_t slot = at >> 32 ? (uint32_t)(at / heads) : (uint32_t)at / heads;
   it.kv_head = (int)(at - (int64_t)slot * heads);

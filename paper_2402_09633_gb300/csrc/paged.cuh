@@ -116,28 +116,4 @@ __device__ __noinline__ void paged_attend_row(const PagedParams& p, const PagedS
     if (lane + 32 * d < p.dim) out[lane + 32 * d] = from_f<T>(l == 0.f ? 0.f : o[d] / l);
 }
 
-constexpr int kPagedRowWarps = 4;
-
-// Every row by paged_attend_row.
-template <typename T>
-__global__ void __launch_bounds__(32 * kPagedRowWarps) paged_rows_kernel(const __grid_constant__ PagedParams p) {
-  __shared__ float q_s[kPagedRowWarps][128];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  pdl_wait();
-  for (int64_t at = (int64_t)blockIdx.x * kPagedRowWarps + warp; at < (int64_t)p.n_q_rows * p.heads;
-       at += (int64_t)gridDim.x * kPagedRowWarps) {
-    const int row = (int)(at / p.heads), head = (int)(at - (int64_t)row * p.heads);
-    const int b = sequence_of(p.q_start, p.n_seqs, p.n_q_rows, row);
-    if (b < 0) continue;
-    bool bad = false;
-    const PagedSequence sq = paged_sequence(p, b, &bad);
-    if ((bad || sq.nq > p.max_q) && lane == 0) atomicOr(p.err, DEV_ERR_INDEX_RANGE);
-    const T* src = reinterpret_cast<const T*>(p.q.data + (int64_t)row * p.q.row_bytes + (int64_t)head * p.q.head_bytes);
-    __syncwarp();
-    for (int d = lane; d < p.dim; d += 32) q_s[warp][d] = to_f(src[d]);
-    __syncwarp();
-    paged_attend_row<T>(p, sq, b, row - sq.q0, head, q_s[warp]);
-  }
-}
-
 }  // namespace gnn

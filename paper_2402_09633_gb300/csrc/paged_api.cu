@@ -1,5 +1,6 @@
 // Entry points for several hypotheses of a sequence: caches in pages, the choice of continuations, and moving states
 // (include/gnn.h).
+#include <cudaTypedefs.h>
 #include <cuda_runtime.h>
 #include <algorithm>
 #include <cmath>
@@ -8,6 +9,7 @@
 #include "beam.cuh"
 #include "host.cuh"
 #include "paged.cuh"
+#include "paged_tile.cuh"
 #include "sequence_host.cuh"
 
 using namespace gnn;
@@ -51,6 +53,77 @@ bool attend_ok(const gnn_pages* c, const gnn_paged_call* a) {
   if (!a->q_start || (uintptr_t)a->q_start % 4 || !wide_ok(a->q, c->dtype) || !wide_ok(a->out, c->dtype)) return false;
   if (a->q.n_heads != a->out.n_heads || a->q.n_heads > 4096 || a->q.n_heads % c->k.n_heads) return false;
   return a->q.n_heads / c->k.n_heads <= 128;
+}
+
+// How a call is cut into tiles, and where its parts lie in the workspace; the bytes that takes.
+struct PagedPlan { PagedGrid g; uint64_t bytes; unsigned blocks; };
+PagedPlan paged_plan(const gnn_pages* c, const gnn_paged_call* a, int n_sm) {
+  PagedPlan r = {};
+  PagedGrid& g = r.g;
+  const int64_t n = a->n_q_rows, max_q = a->max_q > 0 ? std::min<int64_t>(a->max_q, n) : n;
+  r.blocks = (unsigned)n_sm;
+  g.group = a->q.n_heads / c->k.n_heads;
+  g.tile_q = kTileQ / g.group;
+  g.box_a = (int)std::min<int64_t>(g.tile_q, n);
+  g.box_b = (int)std::min<int64_t>(g.tile_q, max_q);
+  g.box = std::min(c->page_size, kKeys);
+  g.rows_a = g.box_a * g.group;
+  g.rows_b = g.box_b * g.group;
+  const int64_t n_a = a->n_groups > 0 ? (n / (2 * g.tile_q) + a->n_groups) * c->k.n_heads : 0;
+  const int64_t n_b = (n / g.tile_q + c->n_seqs) * c->k.n_heads;
+  g.n_a = n_a;
+  const int64_t sums_a = n_a > 0 ? 2 * (n_a + r.blocks) * g.rows_a : 0, sums_b = 2 * (n_b + r.blocks) * g.rows_b;
+  char* at = static_cast<char*>(a->workspace);
+  auto take = [&](int64_t bytes) {
+    char* here = at;
+    const int64_t whole = (bytes + 31) / 32 * 32;
+    at = reinterpret_cast<char*>((uintptr_t)at + whole);
+    r.bytes += whole;
+    return here;
+  };
+  g.out_a = reinterpret_cast<float*>(take(sums_a * c->head_dim * 4));
+  g.out_b = reinterpret_cast<float*>(take(sums_b * c->head_dim * 4));
+  g.sum_a = reinterpret_cast<float2*>(take(sums_a * 8));
+  g.sum_b = reinterpret_cast<float2*>(take(sums_b * 8));
+  g.first_a = reinterpret_cast<int2*>(take(n_a * 8));
+  g.first_b = reinterpret_cast<int2*>(take(n_b * 8));
+  return r;
+}
+
+PFN_cuTensorMapEncodeTiled_v12000 map_encoder() {
+  static const PFN_cuTensorMapEncodeTiled_v12000 found = [] {
+    PFN_cuTensorMapEncodeTiled_v12000 f = nullptr;
+    cudaDriverEntryPointQueryResult r;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", (void**)&f, 12000, cudaEnableDefault, &r) != cudaSuccess ||
+        r != cudaDriverEntryPointSuccess)
+      f = nullptr;
+    return f;
+  }();
+  return found;
+}
+
+// Boxes of box_rows rows x box_heads heads x 64 elements, in the 128-byte swizzle; what lies outside reads as zeros.
+bool paged_map(CUtensorMap* map, const gnn_heads& h, int64_t rows, int dtype, int dim, int box_heads, int box_rows) {
+  const cuuint64_t size[3] = {(cuuint64_t)dim, (cuuint64_t)h.n_heads, (cuuint64_t)rows};
+  const cuuint64_t one = (cuuint64_t)(dim * 2 + 15) / 16 * 16;      // for a dimension of one, whose stride is not used
+  const cuuint64_t stride[2] = {h.n_heads > 1 ? (cuuint64_t)h.head_stride * 2 : one, rows > 1 ? (cuuint64_t)h.row_stride * 2 : one};
+  const cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_rows}, step[3] = {1, 1, 1};
+  return map_encoder()(map, dtype == GNN_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, h.data,
+                       size, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                       CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, int DP>
+cudaError_t launch_paged(const PagedParams& p, const PagedPlan& plan, const CUtensorMap* maps, cudaStream_t st) {
+  cudaError_t err = cudaFuncSetAttribute(paged_tile_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, paged_smem_bytes<DP>());
+  if (err == cudaSuccess)
+    err = launch_pdl(paged_tile_kernel<T, DP>, plan.blocks, kAttendThreads, paged_smem_bytes<DP>(), st, p, plan.g, maps[0], maps[1],
+                     maps[2], maps[3]);
+  const int64_t rows = (int64_t)p.n_q_rows * p.heads;
+  if (err == cudaSuccess)
+    err = launch_pdl(paged_join_kernel<T>, (unsigned)((rows + kPagedJoinWarps - 1) / kPagedJoinWarps), 32 * kPagedJoinWarps, 0, st, p,
+                     plan.g, (int)plan.blocks);
+  return err;
 }
 
 bool beam_ok(const gnn_beam_call* c) {
@@ -136,12 +209,22 @@ int gnn_paged_append(const gnn_pages* c, const gnn_rotary* rot, const gnn_append
 int gnn_paged_workspace(const gnn_pages* c, const gnn_paged_call* a, uint64_t* bytes) {
   if (!bytes || !attend_ok(c, a)) return GNN_ERR_INVALID_ARG;
   *bytes = 0;
+  if (a->n_q_rows == 0 || c->n_seqs == 0) return GNN_OK;
+  const int sms = device_sms();
+  if (!sms) return cuda_fail(cudaGetLastError());
+  *bytes = paged_plan(c, a, sms).bytes;
   return GNN_OK;
 }
 
 int gnn_paged_attend(const gnn_pages* c, const gnn_paged_call* a, gnn_stream_t stream) {
   if (!attend_ok(c, a)) return GNN_ERR_INVALID_ARG;
   if (a->n_q_rows == 0 || c->n_seqs == 0) return GNN_OK;
+  if (!a->workspace || (uintptr_t)a->workspace % 32 || a->n_q_rows * a->q.n_heads >= (int64_t)1 << 32) return GNN_ERR_INVALID_ARG;
+  const int sms = device_sms();
+  if (!sms) return cuda_fail(cudaGetLastError());
+  if (!map_encoder()) return GNN_ERR_CUDA;
+  const PagedPlan plan = paged_plan(c, a, sms);
+  if (a->workspace_bytes < plan.bytes) return GNN_ERR_INVALID_ARG;
   PagedParams p = {};
   p.q = view(a->q, c->dtype);
   p.k = view(c->k, c->dtype);
@@ -166,11 +249,16 @@ int gnn_paged_attend(const gnn_pages* c, const gnn_paged_call* a, gnn_stream_t s
   // a scale of zero as one too small to be seen, so that -inf, a score that is not seen, stays -inf
   p.scale_log2 = a->scale == 0.f ? 1e-30f : (float)((double)a->scale * 1.4426950408889634);
   p.err = c->status;
-  const int64_t blocks = ((int64_t)p.n_q_rows * p.heads + kPagedRowWarps - 1) / kPagedRowWarps;
-  const unsigned grid = (unsigned)std::min<int64_t>(blocks, 16 * (int64_t)device_sms());
+  CUtensorMap maps[4];
+  const int64_t rows = c->n_pages * c->page_size;
+  if (!paged_map(&maps[0], a->q, a->n_q_rows, c->dtype, p.dim, plan.g.group, plan.g.box_a) ||
+      !paged_map(&maps[1], a->q, a->n_q_rows, c->dtype, p.dim, plan.g.group, plan.g.box_b) ||
+      !paged_map(&maps[2], c->k, rows, c->dtype, p.dim, 1, plan.g.box) || !paged_map(&maps[3], c->v, rows, c->dtype, p.dim, 1, plan.g.box))
+    return GNN_ERR_INVALID_ARG;
+  const cudaStream_t st = (cudaStream_t)stream;
   const cudaError_t err = c->dtype == GNN_DTYPE_BF16
-                              ? launch_pdl(paged_rows_kernel<__nv_bfloat16>, grid, 32 * kPagedRowWarps, 0, (cudaStream_t)stream, p)
-                              : launch_pdl(paged_rows_kernel<__half>, grid, 32 * kPagedRowWarps, 0, (cudaStream_t)stream, p);
+                              ? p.dim <= 64 ? launch_paged<__nv_bfloat16, 64>(p, plan, maps, st) : launch_paged<__nv_bfloat16, 128>(p, plan, maps, st)
+                              : p.dim <= 64 ? launch_paged<__half, 64>(p, plan, maps, st) : launch_paged<__half, 128>(p, plan, maps, st);
   return err == cudaSuccess ? GNN_OK : cuda_fail(err);
 }
 
