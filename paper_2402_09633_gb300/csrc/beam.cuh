@@ -3,10 +3,10 @@
 // value(b, t) = score[b] + x[b, t] - log sum_t exp(x[b, t]) for the hypotheses b of a group and all t; the `best` largest
 // of a group in order, ties to the lowest b * vocab + t.  A hypothesis that has ended has one continuation, its score.
 //
-// Within a row the order is that of x, so one pass over the logits finds a row's candidates beside its sum: a block
-// has a strip of a row, keeps a running maximum and sum to a thread, and a list of the elements above the strip's best-th
-// so far.  A second kernel joins the strips row by row, then the rows by value in 64 bits, so that rounding
-// neither makes nor breaks ties.  Bound by HBM: logits are read once.
+// Within a row the order is that of x, so one pass over the logits finds a row's candidates beside its sum: a warp has a
+// stretch of a row, a running maximum and sum to a lane, and a list of the elements above the stretch's best-th so far, with
+// no barrier between warps until the end.  A second kernel joins the lists row by row, then the rows by value in 64 bits,
+// so that rounding neither makes nor breaks ties.  Bound by HBM: logits are read once.
 #pragma once
 #include "attend_ptx.cuh"
 #include "rotary.cuh"
@@ -16,6 +16,7 @@ namespace gnn {
 constexpr int kBeamMost = 64;        // hypotheses of a group, and continuations that are kept
 constexpr int kStripThreads = 256;
 constexpr int kStripsMost = 32;      // strips of a row: one to a lane of the warp that joins them
+constexpr int kWarpBuffer = 128;     // keys that a warp collects before it keeps the best
 
 struct alignas(16) BeamSum { double s; float r; };    // the sum of 2^(x log2 e - r) over a strip
 struct BeamParams {
@@ -58,143 +59,231 @@ __device__ __forceinline__ uint4 load_skewed(const void* at, int bytes) {
                     __funnelshift_r(w[3], w[4], bits));
 }
 
+// How many keys of a list in falling order, `n` of them, are above k.
+__device__ __forceinline__ int above(const uint64_t* list, int n, uint64_t k) {
+  int a = 0, z = n;
+  while (a < z) {
+    const int mid = (a + z) / 2;
+    if (list[mid] > k) a = mid + 1; else z = mid;
+  }
+  return a;
+}
+
+// A warp's best keys so far.
+struct WarpList {
+  uint64_t* buf;                     // [kWarpBuffer], the warp's own
+  int have;
+  float tau;                         // later elements count only above it
+};
+
+// Leaves the best keys in order, and the threshold at the last of them.  Keys differ: a key's place is how many are larger.
+template <int SLOTS>
+__device__ __forceinline__ void warp_rank(WarpList& l, int best) {
+  const int lane = threadIdx.x & 31;
+  uint64_t k[SLOTS];
+  int rank[SLOTS];
+#pragma unroll
+  for (int i = 0; i < SLOTS; ++i) {
+    k[i] = lane + 32 * i < l.have ? l.buf[lane + 32 * i] : 0;
+    rank[i] = 0;
+  }
+#pragma unroll 4
+  for (int j = 0; j < l.have; ++j) {
+    const uint64_t y = l.buf[j];
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) rank[i] += y > k[i];
+  }
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < SLOTS; ++i)
+    if (lane + 32 * i < l.have && rank[i] < best) l.buf[rank[i]] = k[i];
+}
+__device__ __noinline__ void warp_prune(WarpList& l, int best) {
+  __syncwarp();
+  if (l.have <= 32) warp_rank<1>(l, best); else warp_rank<kWarpBuffer / 32>(l, best);
+  __syncwarp();
+  l.have = min(l.have, best);
+  if (l.have == best) l.tau = unordered((uint32_t)(l.buf[best - 1] >> 32));
+}
+
+// 2^n for a whole number that is not positive, exactly; zero where that is below what floats hold.
+__device__ __forceinline__ float power2(float n) { return n < -126.f ? 0.f : __int_as_float(((int)n + 127) << 23); }
+
+constexpr int kStripPieces = 4;      // of 16 bytes, that a lane takes at a time
+constexpr int kStripStages = 3;
+constexpr int kStripStage = (32 * kStripPieces + 1) * 16;       // and the one that rows which start between two reach into
+constexpr int kStripSmem = kStripThreads / 32 * kStripStages * kStripStage;
+
 template <typename T>
-__global__ void __launch_bounds__(kStripThreads) beam_strip_kernel(const __grid_constant__ BeamParams p) {
-  constexpr int VEC = 16 / sizeof(T), N = 2 * VEC;   // elements of 16 bytes; of a thread at a time
-  constexpr int CHUNK = kStripThreads * N, CAP = CHUNK + 256;
-  // log2 e in two pieces, and sums relative to 2^r with r as it is rounded: the logarithm of a row's sum is to be good
-  // to 10^-8 or so, as rows' values are compared with each other
+__global__ void __launch_bounds__(kStripThreads, 3) beam_strip_kernel(const __grid_constant__ BeamParams p) {
+  constexpr int VEC = 16 / sizeof(T), P = kStripPieces, N = P * VEC, WARPS = kStripThreads / 32;     // elements of a piece, of a lane at a time
+  // log2 e in two pieces: the logarithm of a row's sum is to be good to 10^-8 or so, as rows' values are compared with each
+  // other.  Sums are relative to 2^r with a whole number r, so that joining them rounds nothing.
   constexpr float kHi = 1.44269504f, kLo = (float)(1.4426950408889634 - (double)1.44269504f);
-  __shared__ uint64_t buf[CAP], pick_s[kBeamMost], top_s[kBeamMost];
-  __shared__ int count_s;
-  __shared__ float high_s[kStripThreads / 32];
-  __shared__ double sum_s[kStripThreads / 32];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int64_t row = blockIdx.x / p.strips;
-  const int strip = (int)(blockIdx.x - row * p.strips);
-  if (tid == 0) count_s = 0;
+  extern __shared__ __align__(16) uint8_t strip_smem[];
+  __shared__ uint64_t buf_s[WARPS][kWarpBuffer];
+  __shared__ float high_s[WARPS];
+  __shared__ double sum_s[WARPS];
+  __shared__ int have_s[WARPS], count_s[WARPS];
+  __shared__ unsigned tau_s;                         // the highest of the warps' thresholds, as it is ordered
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, best = p.best;
+  const int row = p.strips == 1 ? (int)blockIdx.x : (int)(blockIdx.x / (unsigned)p.strips);
+  const int strip = (int)blockIdx.x - row * p.strips;
+  if (tid == 0) tau_s = 0;
+  __syncthreads();
   pdl_wait();
   pdl_trigger();
   if (p.ended && p.ended[row]) return;
   const T* x = static_cast<const T*>(p.x) + row * p.stride;
-  // Pieces of 16 bytes, by the elements' numbers: rows that hold the same have the same sum to the last bit, wherever in
-  // memory they start, so that values which are equal compare so.
-  const int skew = (int)((uintptr_t)x / sizeof(T) % VEC);
-  const int64_t pieces = ((int64_t)p.vocab + VEC - 1) / VEC;
-  const int64_t per = (pieces + p.strips - 1) / p.strips;
-  const int64_t p0 = min(pieces, strip * per), p1 = min(pieces, p0 + per);
-  __syncthreads();
-
-  float m = -INFINITY, r = 0.f, s = 0.f, tau = -INFINITY;
-  int have = 0;                                      // keys in buf, as every thread knows it
-  // Leaves the best keys of buf in order in its first places, and the threshold at the last of them.
-  auto prune = [&] {
-    int n = have;
-    uint64_t least = 0;
-    if (n > kStripThreads) {                         // the largest key that `best` of them reach, bit by bit
-#pragma unroll 1
-      for (int bit = 63; bit >= 0; --bit) {
-        const uint64_t t = least | 1ull << bit;
-        int c = 0;
-        for (int i = tid; i < n; i += kStripThreads) c += buf[i] >= t;
-        c = __reduce_add_sync(0xffffffffu, c);
-        if (tid == 0) count_s = 0;
-        __syncthreads();
-        if (lane == 0) atomicAdd(&count_s, c);
-        __syncthreads();
-        if (count_s >= p.best) least = t;
-        __syncthreads();
+  // Pieces by the elements' numbers: rows that hold the same have the same sum to the last bit, wherever in memory they start, so
+  // that values which are equal compare so.  Those below `whole`, and not the first of a row that starts between two, come through
+  // shared memory, kStripStages rounds ahead of their use; the others element by element.
+  const int skew = (int)((uintptr_t)x / sizeof(T) % VEC), bytes = skew * (int)sizeof(T), vocab = p.vocab;
+  const int pieces = (vocab + VEC - 1) / VEC, whole = skew == 0 ? vocab / VEC : (vocab + skew) / VEC - 1;
+  const int per = (pieces + p.strips * WARPS - 1) / (p.strips * WARPS), p0 = min(pieces, (strip * WARPS + warp) * per),
+            p1 = min(pieces, p0 + per);
+  const uint4* wide = reinterpret_cast<const uint4*>(x - skew);
+  uint8_t* ring = strip_smem + warp * kStripStages * kStripStage;
+  // 16 bytes that lie in the row whole: pieces of memory first .. last - 1
+  const int first = skew ? 1 : 0, last = (int)(((int64_t)vocab + skew) / VEC);
+  auto fetch = [&](int c0, int stage) {              // pieces of memory c0 .. c0 + 32 P
+    uint8_t* to = ring + stage * kStripStage;
+    if (c0 < p1) {
+#pragma unroll
+      for (int h = 0; h <= P; ++h) {
+        const int i = h * 32 + lane, at = c0 + i;
+        if (i <= 32 * P && at >= first && at < last && at <= p1)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to + i * 16)), "l"(wide + at) : "memory");
       }
     }
-    const uint64_t* from = buf;
-    if (n > kStripThreads) {
-      if (tid == 0) count_s = 0;
-      __syncthreads();
-      for (int i = tid; i < n; i += kStripThreads)
-        if (buf[i] >= least) pick_s[atomicAdd(&count_s, 1)] = buf[i];
-      __syncthreads();
-      from = pick_s;
-      n = p.best;
-    }
-    if (tid < n) {                                   // keys differ: as many come before one as are larger
-      const uint64_t k = from[tid];
-      int rank = 0;
-      for (int j = 0; j < n; ++j) rank += from[j] > k;
-      if (rank < p.best) top_s[rank] = k;
-    }
-    __syncthreads();
-    have = min(n, p.best);
-    if (tid < have) buf[tid] = top_s[tid];
-    if (tid == 0) count_s = have;
-    if (have == p.best) tau = unordered((uint32_t)(top_s[have - 1] >> 32));
-    __syncthreads();
+    asm volatile("cp.async.commit_group;" ::: "memory");
   };
 
-  for (int64_t c0 = p0; c0 < p1; c0 += 2 * kStripThreads) {
+  float m = -INFINITY, r = 0.f, s = 0.f;
+  WarpList list = {buf_s[warp], 0, -INFINITY};
+  const int spare = kWarpBuffer - 32;                // keys that leave room for those of another element of all lanes
+  const int enough = min(spare, max(32, 2 * best));  // keys from which on a new threshold is worth its price
+  volatile unsigned* shared_tau = &tau_s;
+#pragma unroll
+  for (int k = 0; k < kStripStages - 1; ++k) fetch(p0 + k * 32 * P, k);
+  int stage = 0;
+  for (int c0 = p0; c0 < p1; c0 += 32 * P) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStripStages - 2) : "memory");
+    __syncwarp();                                    // what lies in the stage, and that the one before has been read
+    fetch(c0 + (kStripStages - 1) * 32 * P, stage == 0 ? kStripStages - 1 : stage - 1);
     float v[N];
+    {
+      const uint8_t* from = ring + stage * kStripStage;
+      stage = stage + 1 == kStripStages ? 0 : stage + 1;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int64_t piece = c0 + h * kStripThreads + tid, e0 = piece * VEC;
-      Pack<T, VEC> k;
-      if (piece < p1 && (skew == 0 ? e0 + VEC <= p.vocab : piece > 0 && e0 + 2 * VEC - skew <= p.vocab)) {
-        *reinterpret_cast<uint4*>(&k) = skew == 0 ? __ldcs(reinterpret_cast<const uint4*>(x + e0)) : load_skewed(x + e0 - skew, skew * (int)sizeof(T));
-      } else {
+      for (int h = 0; h < P; ++h) {
+        const int piece = c0 + h * 32 + lane;
+        Pack<T, VEC> k;
+        if (piece < min(p1, whole) && piece >= first) {
+          const uint4* at = reinterpret_cast<const uint4*>(from) + h * 32 + lane;
+          *reinterpret_cast<uint4*>(&k) = skew == 0 ? *at : load_skewed(at, bytes);
+        } else {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) k.v[e] = piece < p1 && e0 + e < p.vocab ? x[e0 + e] : from_f<T>(-INFINITY);
+          for (int e = 0; e < VEC; ++e) k.v[e] = piece < p1 && (int64_t)piece * VEC + e < vocab ? x[(int64_t)piece * VEC + e] : from_f<T>(-INFINITY);
+        }
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[h * VEC + e] = to_f(k.v[e]);
       }
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) v[h * VEC + e] = to_f(k.v[e]);
     }
     float high = v[0];
 #pragma unroll
-    for (int e = 1; e < N; ++e) high = fmaxf(high, v[e]);
+    for (int e = 1; e + 1 < N; e += 2) high = max3(high, v[e], v[e + 1]);
+    high = fmaxf(high, v[N - 1]);
     if (high > m) {
-      const float next = high * kHi;
-      if (m > -INFINITY) s *= exp2_approx(r - next);
+      const float to = ceilf(high * kHi);
+      if (m > -INFINITY) s *= power2(r - to);
       m = high;
-      r = next;
+      r = to;
     }
-    float2 sum = make_float2(0.f, 0.f);
+    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
     for (int e = 0; e < N; e += 2) {
       const float2 y = make_float2(v[e], v[e + 1]);
       const float2 z = __ffma2_rn(y, make_float2(kLo, kLo), __ffma2_rn(y, make_float2(kHi, kHi), make_float2(-r, -r)));
-      sum = __fadd2_rn(sum, make_float2(exp2_approx(z.x), exp2_approx(z.y)));
+      sum[e >> 1 & 1] = __fadd2_rn(sum[e >> 1 & 1], make_float2(exp2_approx(z.x), exp2_approx(z.y)));
     }
-    s += sum.x + sum.y;
+    s += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
     // candidates: later elements of the same value as the threshold lose the tie
-    if (!__syncthreads_or(high > tau)) continue;
-    float least = tau;                               // of this chunk's, those above it, or from it on
-    bool from = false;
-    int mine = 0;
+    if (!__any_sync(0xffffffffu, high > list.tau)) continue;
+    // of these elements, those above the threshold and from here on: another warp's threshold bounds the block's best from
+    // below too, but elements equal to it may have lower numbers than that warp's
+    const unsigned theirs = *shared_tau;
+    float from = theirs ? unordered(theirs) : -INFINITY;
+    if (!__any_sync(0xffffffffu, high >= from)) continue;
+    if (list.tau == -INFINITY && theirs == 0) {
+      // at first as many lanes' largest elements bound the best from below, or all lanes' two largest
+      if (best <= 32) {
+        int rank = 0;
 #pragma unroll
-    for (int e = 0; e < N; ++e) mine += v[e] > tau;
-    if (__syncthreads_count(mine > 0) >= p.best) {
-      // `best` threads' largest elements bound the strip's best-th from below
-      uint32_t t = 0;
-      const uint32_t h = high > tau ? ordered(high) : 0;
-#pragma unroll 1
-      for (int bit = 31; bit >= 0; --bit)
-        if (__syncthreads_count(h >= (t | 1u << bit)) >= p.best) t |= 1u << bit;
-      least = unordered(t);
-      from = true;
-    }
+        for (int d = 0; d < 32; ++d) {
+          const float y = __shfl_sync(0xffffffffu, high, d);
+          rank += y > high || (y == high && d < lane);
+        }
+        from = __shfl_sync(0xffffffffu, high, __ffs(__ballot_sync(0xffffffffu, rank == best - 1)) - 1);
+      } else {
+        float a = -INFINITY, z = -INFINITY;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+        for (int e = 0; e < N; ++e) {
+          z = fmaxf(z, fminf(a, v[e]));
+          a = fmaxf(a, v[e]);
+        }
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        const float y = v[h * VEC + e];
-        if (y > tau && (from ? y >= least : y > least))
-          buf[atomicAdd(&count_s, 1)] = beam_key(y, (uint32_t)((c0 + h * kStripThreads + tid) * VEC + e));
+        for (int d = 16; d > 0; d >>= 1) z = fminf(z, __shfl_xor_sync(0xffffffffu, z, d));
+        from = z;
       }
-    __syncthreads();
-    have = count_s;
-    __syncthreads();
-    if (have > 256 || tau == -INFINITY) prune();
+    }
+    auto count = [&] {
+      int n = 0;
+#pragma unroll
+      for (int e = 0; e < N; ++e) n += v[e] > list.tau && v[e] >= from;
+      return n;
+    };
+    auto append = [&](int at) {                      // in any order: keys differ
+#pragma unroll
+      for (int h = 0; h < P; ++h)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          const float y = v[h * VEC + e];
+          if (y > list.tau && y >= from) list.buf[at++] = beam_key(y, (uint32_t)((c0 + h * 32 + lane) * VEC + e));
+        }
+    };
+    const int mine = count(), more = __reduce_add_sync(0xffffffffu, mine);
+    if (list.have + more <= kWarpBuffer) {
+      if (lane == 0) count_s[warp] = list.have;
+      __syncwarp();
+      if (mine) append(atomicAdd(&count_s[warp], mine));
+      list.have += more;
+    } else {                                         // rows that rise, or are all the same: lane by lane
+#pragma unroll 1
+      for (int d = 0; d < 32; ++d) {
+        const int now = __shfl_sync(0xffffffffu, count(), d);
+        if (now == 0) continue;
+        if (list.have > spare) {
+          // The threshold is of elements with any numbers then: what is left of this round counts from it on.
+          const float before = list.tau;
+          warp_prune(list, best);
+          from = fmaxf(from, list.tau);
+          list.tau = before;
+          --d;
+          continue;
+        }
+        if (lane == d) append(list.have);
+        list.have += now;
+      }
+    }
+    __syncwarp();
+    if (list.have >= enough || (list.tau == -INFINITY && list.have >= best)) {
+      warp_prune(list, best);
+      if (lane == 0 && list.have == best) atomicMax(&tau_s, ordered(list.tau));
+    }
   }
-  if (have > 0) prune();
-  uint64_t* list = p.lists + (int64_t)blockIdx.x * p.best;
-  if (tid < p.best) list[tid] = tid < have ? buf[tid] : 0;
+  warp_prune(list, best);
+  if (lane == 0) have_s[warp] = list.have;
   // the threads' sums
   float high = m == -INFINITY ? -INFINITY : r;
 #pragma unroll
@@ -202,95 +291,133 @@ __global__ void __launch_bounds__(kStripThreads) beam_strip_kernel(const __grid_
   if (lane == 0) high_s[warp] = high;
   __syncthreads();
   high = high_s[0];
-  for (int w = 1; w < kStripThreads / 32; ++w) high = fmaxf(high, high_s[w]);
-  double sum = s == 0.f ? 0. : (double)(s * exp2f(r - (high == -INFINITY ? 0.f : high)));
+#pragma unroll
+  for (int w = 1; w < WARPS; ++w) high = fmaxf(high, high_s[w]);
+  // (a power of two below what floats hold is below what counts, and an infinite r has made s NaN)
+  double sum = s == 0.f ? 0. : (double)(s * power2(r - (high == -INFINITY ? 0.f : high)));
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
   if (lane == 0) sum_s[warp] = sum;
+  // the warps' lists: a key's place is its own and what the others have above it
+  uint64_t* out = p.lists + (int64_t)blockIdx.x * best;
+  int all = 0;
+#pragma unroll
+  for (int w = 0; w < WARPS; ++w) all += have_s[w];
+  for (int i = lane; i < list.have; i += 32) {
+    const uint64_t k = list.buf[i];
+    int rank = i;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w)
+      if (w != warp) rank += above(buf_s[w], have_s[w], k);
+    if (rank < best) out[rank] = k;
+  }
+  for (int i = all + tid; i < best; i += kStripThreads) out[i] = 0;
   __syncthreads();
   if (tid == 0) {
-    for (int w = 1; w < kStripThreads / 32; ++w) sum += sum_s[w];
+    for (int w = 1; w < WARPS; ++w) sum += sum_s[w];
     p.sums[blockIdx.x] = {sum, high};
   }
 }
 
-constexpr int kJoinWarps = 8;
+constexpr int kJoinThreads = 256;
 
-// One group to a block: a warp joins the strips of a row at a time, the first warp joins the rows.
-__global__ void __launch_bounds__(32 * kJoinWarps) beam_join_kernel(const __grid_constant__ BeamParams p) {
-  __shared__ uint64_t list_s[kBeamMost][kBeamMost];  // [hypothesis][rank]
-  __shared__ double base_s[kBeamMost];               // what is added to a logit
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t group = blockIdx.x;
+// One group to a block: first the strips of every row, then the rows, each time a candidate's place being how many of the
+// other lists' are before it.
+__global__ void __launch_bounds__(kJoinThreads) beam_join_kernel(const __grid_constant__ BeamParams p) {
+  extern __shared__ __align__(16) uint64_t join_smem[];
+  __shared__ double base_s[kBeamMost];               // a row's sum; then what is added to a logit
+  __shared__ float top_s[kBeamMost];
+  __shared__ int taken_s;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, best = p.best, beams = p.beams, strips = p.strips;
+  const int64_t group = blockIdx.x, row0 = group * beams;
+  uint64_t* rows = join_smem;                        // [beams][best]
+  uint64_t* values = rows + beams * best;            // the same, as they are ordered: comparing 64-bit floats takes long here
+  uint64_t* lists = values + beams * best;           // [warps][strips][best]
+  if (tid == 0) taken_s = 0;
   pdl_wait();
-  for (int b = warp; b < p.beams; b += kJoinWarps) {
-    const int64_t row = group * p.beams + b;
-    const float score = p.score[row];
-    if (p.ended && p.ended[row]) {
-      for (int i = lane; i < p.best; i += 32) list_s[b][i] = i == 0 ? beam_key(0.f, (uint32_t)p.end) : 0;
-      if (lane == 0) base_s[b] = (double)score;
-      continue;
-    }
-    const BeamSum part = lane < p.strips ? p.sums[row * p.strips + lane] : BeamSum{0., -INFINITY};
-    float top = part.r;
+  for (int b = warp; b < beams; b += kJoinThreads / 32) {
+    const int64_t row = row0 + b;
+    const bool ended = p.ended && p.ended[row];
+    uint64_t* mine = rows + b * best;
+    if (ended) {
+      for (int i = lane; i < best; i += 32) mine[i] = i == 0 ? beam_key(0.f, (uint32_t)p.end) : 0;
+      if (lane == 0) {
+        base_s[b] = 1.;
+        top_s[b] = 0.f;
+      }
+    } else {
+      const BeamSum part = lane < strips ? p.sums[row * strips + lane] : BeamSum{0., -INFINITY};
+      const uint64_t* from = p.lists + row * strips * best;
+      uint64_t* to = strips == 1 ? mine : lists + warp * strips * best;
+      for (int i = lane; i < strips * best; i += 32) to[i] = from[i];
+      float top = part.r;
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-    double sum = part.s == 0. ? 0. : part.s * exp2((double)part.r - (double)top);
+      for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+      double sum = part.s == 0. ? 0. : part.s * (double)power2(part.r - (top == -INFINITY ? 0.f : top));
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    if (lane == 0) base_s[b] = (double)score - ((double)top + log2(sum)) * 0.6931471805599453;
-    // the strips' lists, each in order, into one
-    const uint64_t* list = p.lists + (row * p.strips + lane) * p.best;
-    int at = 0;
-    uint64_t head = lane < p.strips ? list[0] : 0;
-    for (int i = 0; i < p.best; ++i) {
-      uint64_t k = head;
-#pragma unroll
-      for (int d = 16; d > 0; d >>= 1) k = max(k, __shfl_xor_sync(0xffffffffu, k, d));
-      if (lane == 0) list_s[b][i] = k;
-      if (k != 0 && head == k) head = ++at < p.best ? list[at] : 0;
+      for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+      if (lane == 0) {
+        base_s[b] = sum;
+        top_s[b] = top;
+      }
+      __syncwarp();
+      if (strips > 1) {
+        for (int i = lane; i < best; i += 32) mine[i] = 0;
+        __syncwarp();
+        for (int i = lane; i < strips * best; i += 32) {
+          const uint64_t k = to[i];
+          if (k == 0) continue;
+          const int s = i / best;
+          int rank = i - s * best;
+          for (int t = 0; t < strips && rank < best; ++t)
+            if (t != s) rank += above(to + t * best, best, k);
+          if (rank < best) mine[rank] = k;
+        }
+        __syncwarp();
+      }
     }
   }
   __syncthreads();
-  if (warp != 0) return;
-  // rows lane and lane + 32
-  int at[2] = {0, 0};
-  uint64_t key[2];
-  double value[2];
-  auto fetch = [&](int h) {
-    const int b = lane + 32 * h;
-    key[h] = b < p.beams && at[h] < p.best ? list_s[b][at[h]] : 0;
-    value[h] = key[h] ? base_s[b] + (double)unordered((uint32_t)(key[h] >> 32)) : -INFINITY;
-    if (!(value[h] > -INFINITY)) {                   // none, or NaN
-      value[h] = -INFINITY;
-      key[h] = 0;
+  // 64-bit arithmetic is slow here: one logarithm for all rows
+  if (tid < beams) base_s[tid] = (double)p.score[row0 + tid] - ((double)top_s[tid] + log2(base_s[tid])) * 0.6931471805599453;
+  __syncthreads();
+  for (int i = tid; i < beams * best; i += kJoinThreads) {
+    const uint64_t k = rows[i];
+    const double v = k ? base_s[i / best] + (double)unordered((uint32_t)(k >> 32)) : -INFINITY;
+    const uint64_t u = (uint64_t)__double_as_longlong(v + 0.);
+    values[i] = !(v > -INFINITY) ? 0 : u >> 63 ? ~u : u | 1ull << 63;        // 0: none, or NaN
+  }
+  __syncthreads();
+  int taken = 0;
+  for (int i = tid; i < beams * best; i += kJoinThreads) {
+    const uint64_t v = values[i];
+    if (v == 0) continue;
+    const int b = i / best;
+    int rank = i - b * best;
+    for (int c = 0; c < beams && rank < best; ++c) {
+      if (c == b) continue;
+      const uint64_t* list = values + c * best;      // falling; of equal values those of lower rows come first
+      int a = 0, z = best;
+      while (a < z) {
+        const int mid = (a + z) / 2;
+        if (c < b ? list[mid] >= v : list[mid] > v) a = mid + 1; else z = mid;
+      }
+      rank += a;
     }
-  };
-  fetch(0);
-  fetch(1);
-  for (int i = 0; i < p.best; ++i) {
-    double v = value[0];
-    uint64_t k = key[0];
-    int b = lane;
-    if (value[1] > v) { v = value[1]; k = key[1]; b = lane + 32; }
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-      const double v2 = __shfl_xor_sync(0xffffffffu, v, d);
-      const uint64_t k2 = __shfl_xor_sync(0xffffffffu, k, d);
-      const int b2 = __shfl_xor_sync(0xffffffffu, b, d);
-      if (v2 > v || (v2 == v && b2 < b)) { v = v2; k = k2; b = b2; }
-    }
-    if (lane == 0) {
-      const int64_t o = group * p.best + i;
-      const bool none = v == -INFINITY;
-      p.out_score[o] = (float)v;
-      p.out_parent[o] = none ? 0 : b;
-      p.out_token[o] = none ? -1 : (int)~(uint32_t)k;
-    }
-    if (v > -INFINITY && b % 32 == lane) {
-      const int h = b / 32;
-      if (h == 0) { ++at[0]; fetch(0); } else { ++at[1]; fetch(1); }
-    }
+    if (rank >= best) continue;
+    const int64_t o = group * best + rank;
+    p.out_score[o] = (float)__longlong_as_double((long long)(v >> 63 ? v & ~(1ull << 63) : ~v));
+    p.out_parent[o] = b;
+    p.out_token[o] = (int)~(uint32_t)rows[i];
+    ++taken;
+  }
+  atomicAdd(&taken_s, taken);
+  __syncthreads();
+  for (int i = taken_s + tid; i < best; i += kJoinThreads) {
+    const int64_t o = group * best + i;
+    p.out_score[o] = -INFINITY;
+    p.out_parent[o] = 0;
+    p.out_token[o] = -1;
   }
 }
 

@@ -21,7 +21,7 @@ struct PagedParams {
   uint32_t* err;
 };
 
-struct PagedSequence { int q0, nq, len, first, shared; };   // first: whose pages the keys below `shared` are read through
+struct PagedSequence { int q0, nq, len, group, first, shared; };   // first: whose pages the keys below `shared` are read through
 
 // The positions that a row of the table can hold.
 __device__ __forceinline__ int paged_room(const PagedParams& p) {
@@ -40,19 +40,35 @@ __device__ __forceinline__ int paged_shared(const PagedParams& p, int g, bool* b
   return cut;
 }
 __device__ __forceinline__ PagedSequence paged_sequence(const PagedParams& p, int b, bool* bad) {
+  // The group that sequence b would be of if all were as large is looked at beside the sequence itself: one round of loads.
   PagedSequence s;
+  int g = -1, g0 = 0, g1 = 0, shared = 0;
+  if (p.n_groups > 0) {
+    g = min((int)((float)b / (float)p.n_seqs * (float)p.n_groups), p.n_groups - 1);
+    g0 = p.group_start[g];
+    g1 = p.group_start[g + 1];
+    shared = p.shared_len[g];
+  }
+  const int len = p.kv_len[b];
   const int2 q = paged_queries(p, b, bad);
   s.q0 = q.x;
   s.nq = q.y - q.x;
-  const int len = p.kv_len[b];
   s.len = min(max(len, 0), paged_room(p));
   *bad = *bad || len != s.len;
   s.first = b;
   s.shared = 0;
-  const int g = p.n_groups > 0 ? sequence_of(p.group_start, p.n_groups, p.n_seqs, b) : -1;
+  if (g >= 0 && !(b >= g0 && b < g1)) {
+    g = sequence_of(p.group_start, p.n_groups, p.n_seqs, b);
+    if (g >= 0) {
+      g0 = p.group_start[g];
+      shared = p.shared_len[g];
+    }
+  }
+  s.group = g;
   if (g >= 0) {
-    s.first = max(p.group_start[g], 0);
-    s.shared = paged_shared(p, g, bad);
+    s.first = max(g0, 0);
+    s.shared = min(max(shared, 0), paged_room(p));
+    *bad = *bad || shared != s.shared;
   }
   return s;
 }

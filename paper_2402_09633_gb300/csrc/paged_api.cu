@@ -65,13 +65,15 @@ PagedPlan paged_plan(const gnn_pages* c, const gnn_paged_call* a, int n_sm) {
   g.group = a->q.n_heads / c->k.n_heads;
   g.tile_q = kTileQ / g.group;
   g.box_a = (int)std::min<int64_t>(g.tile_q, n);
-  g.box_b = (int)std::min<int64_t>(g.tile_q, max_q);
+  g.pack = 1;
+  // (and keys that are counted in 32 bits)
+  while (g.pack < kPackMost && 2 * g.pack * max_q <= g.tile_q && 2 * g.pack * ((int64_t)c->table_width * c->page_size) <= 1 << 30) g.pack *= 2;
+  g.box_b = (int)std::min<int64_t>(g.tile_q, g.pack * max_q);
   g.box = std::min(c->page_size, kKeys);
   g.rows_a = g.box_a * g.group;
   g.rows_b = g.box_b * g.group;
   const int64_t n_a = a->n_groups > 0 ? (n / (2 * g.tile_q) + a->n_groups) * c->k.n_heads : 0;
-  const int64_t n_b = (n / g.tile_q + c->n_seqs) * c->k.n_heads;
-  g.n_a = n_a;
+  const int64_t n_b = (g.pack > 1 ? (c->n_seqs + g.pack - 1) / g.pack : n / g.tile_q + c->n_seqs) * (int64_t)c->k.n_heads;
   const int64_t sums_a = n_a > 0 ? 2 * (n_a + r.blocks) * g.rows_a : 0, sums_b = 2 * (n_b + r.blocks) * g.rows_b;
   char* at = static_cast<char*>(a->workspace);
   auto take = [&](int64_t bytes) {
@@ -118,7 +120,7 @@ cudaError_t launch_paged(const PagedParams& p, const PagedPlan& plan, const CUte
   cudaError_t err = cudaFuncSetAttribute(paged_tile_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, paged_smem_bytes<DP>());
   if (err == cudaSuccess)
     err = launch_pdl(paged_tile_kernel<T, DP>, plan.blocks, kAttendThreads, paged_smem_bytes<DP>(), st, p, plan.g, maps[0], maps[1],
-                     maps[2], maps[3]);
+                     maps[2], maps[3], maps[4], maps[5]);
   const int64_t rows = (int64_t)p.n_q_rows * p.heads;
   if (err == cudaSuccess)
     err = launch_pdl(paged_join_kernel<T>, (unsigned)((rows + kPagedJoinWarps - 1) / kPagedJoinWarps), 32 * kPagedJoinWarps, 0, st, p,
@@ -133,14 +135,21 @@ bool beam_ok(const gnn_beam_call* c) {
   return count_ok(c->n_groups) && count_ok(c->n_groups * c->beams) && c->row_stride >= 0 && c->row_stride < (int64_t)1 << 39;
 }
 
-// Strips of a row: enough blocks for every SM, of at least two chunks each.
+// Strips of a row.  A block's time is a few rounds of its warps' for its start and end, and its strip's rounds; rounds of
+// blocks that do not fill the SMs are lost.
 int beam_strips(const gnn_beam_call* c, int n_sm) {
-  const int64_t rows = c->n_groups * c->beams, chunk = kStripThreads * 32 / elem_bytes(c->dtype);
-  const int64_t want = (4 * (int64_t)n_sm + rows - 1) / rows, most = (c->vocab + 2 * chunk - 1) / (2 * chunk);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), kStripsMost));
+  const int64_t rows = c->n_groups * c->beams, slots = 3 * (int64_t)n_sm, round = kStripThreads * kStripPieces * 16 / elem_bytes(c->dtype);
+  const int64_t rounds = (c->vocab + round - 1) / round;
+  int64_t best = 1, least = 0;
+  for (int64_t s = 1; s <= std::min<int64_t>(kStripsMost, rounds); ++s) {
+    const int64_t time = (rows * s + slots - 1) / slots * ((rounds + s - 1) / s + 8);
+    if (s == 1 || time < least) best = s, least = time;
+  }
+  return (int)best;
 }
 
-constexpr int kMostSms = 160;        // that strips are counted for where no device need be asked
+constexpr int kJoinSmem = 16 * kBeamMost * kBeamMost + 8 * (kJoinThreads / 32) * kStripsMost * kBeamMost;
+constexpr int kMostSms = 152;        // that strips are counted for where no device need be asked
 
 uint64_t beam_bytes(const gnn_beam_call* c) {
   const uint64_t strips = (uint64_t)c->n_groups * c->beams * beam_strips(c, kMostSms);
@@ -249,11 +258,12 @@ int gnn_paged_attend(const gnn_pages* c, const gnn_paged_call* a, gnn_stream_t s
   // a scale of zero as one too small to be seen, so that -inf, a score that is not seen, stays -inf
   p.scale_log2 = a->scale == 0.f ? 1e-30f : (float)((double)a->scale * 1.4426950408889634);
   p.err = c->status;
-  CUtensorMap maps[4];
+  CUtensorMap maps[6];
   const int64_t rows = c->n_pages * c->page_size;
   if (!paged_map(&maps[0], a->q, a->n_q_rows, c->dtype, p.dim, plan.g.group, plan.g.box_a) ||
       !paged_map(&maps[1], a->q, a->n_q_rows, c->dtype, p.dim, plan.g.group, plan.g.box_b) ||
-      !paged_map(&maps[2], c->k, rows, c->dtype, p.dim, 1, plan.g.box) || !paged_map(&maps[3], c->v, rows, c->dtype, p.dim, 1, plan.g.box))
+      !paged_map(&maps[2], c->k, rows, c->dtype, p.dim, 1, plan.g.box) || !paged_map(&maps[3], c->v, rows, c->dtype, p.dim, 1, plan.g.box) ||
+      !paged_map(&maps[4], c->k, rows, c->dtype, p.dim, 1, kPiece) || !paged_map(&maps[5], c->v, rows, c->dtype, p.dim, 1, kPiece))
     return GNN_ERR_INVALID_ARG;
   const cudaStream_t st = (cudaStream_t)stream;
   const cudaError_t err = c->dtype == GNN_DTYPE_BF16
@@ -295,10 +305,16 @@ int gnn_beam_select(const gnn_beam_call* c, gnn_stream_t stream) {
   p.out_token = c->out_tokens;
   const cudaStream_t st = (cudaStream_t)stream;
   const unsigned grid = (unsigned)(p.rows * p.strips);
-  cudaError_t err = c->dtype == GNN_DTYPE_FP32   ? launch_pdl(beam_strip_kernel<float>, grid, kStripThreads, 0, st, p)
-                    : c->dtype == GNN_DTYPE_BF16 ? launch_pdl(beam_strip_kernel<__nv_bfloat16>, grid, kStripThreads, 0, st, p)
-                                                 : launch_pdl(beam_strip_kernel<__half>, grid, kStripThreads, 0, st, p);
-  if (err == cudaSuccess) err = launch_pdl(beam_join_kernel, (unsigned)c->n_groups, 32 * kJoinWarps, 0, st, p);
+  auto strips = [&](auto kernel) {
+    const cudaError_t set = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kStripSmem);
+    return set != cudaSuccess ? set : launch_pdl(kernel, grid, kStripThreads, kStripSmem, st, p);
+  };
+  cudaError_t err = c->dtype == GNN_DTYPE_FP32   ? strips(beam_strip_kernel<float>)
+                    : c->dtype == GNN_DTYPE_BF16 ? strips(beam_strip_kernel<__nv_bfloat16>)
+                                                 : strips(beam_strip_kernel<__half>);
+  const size_t smem = 16 * (size_t)p.beams * p.best + (p.strips > 1 ? 8 * (size_t)(kJoinThreads / 32) * p.strips * p.best : 0);
+  if (err == cudaSuccess) err = cudaFuncSetAttribute(beam_join_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kJoinSmem);
+  if (err == cudaSuccess) err = launch_pdl(beam_join_kernel, (unsigned)c->n_groups, kJoinThreads, smem, st, p);
   return err == cudaSuccess ? GNN_OK : cuda_fail(err);
 }
 

@@ -1,10 +1,11 @@
 // Attention over keys in pages, by tiles of 128 rows on tcgen05: what hypotheses share is read once for all of them.
 //
 // The query heads that read a key head lie side by side as rows (row r of a tile: query r / G of the tile, head r % G of
-// the group), so that the hypotheses of a group fill tiles together: S = Q K^T and O = P V over the group's shared keys, two
-// tiles of rows at a time (an item).  A sequence's own keys are items of their own, with the rows of that sequence.  Items
-// of one tile have their blocks of 128 keys in turn on the two tiles of tensor memory, so that one block's products run
-// beside the other's softmax.
+// the group).  A group's shared keys are an item of work for every two tiles of its hypotheses' rows: S = Q K^T and
+// O = P V.  The sequences' own keys are items too, of a pack of consecutive sequences whose rows fit a tile: their keys follow
+// each other in pieces of 16 rows, and a row sees the range that is its sequence's.  A tile costs the same with few
+// rows as with 128, so that packing costs nothing, and short sequences fill blocks of keys together.  Items of one tile have
+// their blocks in turn on the two tiles of tensor memory, so that one block's products run beside the other's softmax.
 //
 // All blocks of all items are one list, of which every thread block takes an equal share: it sums up the lengths, finds its
 // place and goes on from there, so the host knows no lengths and no SM idles over ragged ones.  A share's part of an item leaves
@@ -18,22 +19,26 @@
 
 namespace gnn {
 
-constexpr int kPagedCost = 1;        // what an item's start and end take, in blocks of one tile
+constexpr int kPagedCost = 2;        // what an item's start and end take, in blocks
+constexpr int kPiece = 16;           // keys of a piece: pages have whole pieces
+constexpr int kPieces = kKeys / kPiece;
+constexpr int kPackMost = 32;        // sequences of a pack: a lane to each
+constexpr int kPagedKept = 768, kGroupsKept = 64;              // sequences and groups that a thread block keeps what it has found out about
 
 struct PagedGrid {
-  int tile_q, box_a, box_b;          // queries of a tile; queries that a load of a group's, of a sequence's brings
-  int box;                           // rows of a load of keys: of a page, at most a block's
+  int tile_q, box_a, box_b;          // queries of a tile; queries that a load of a group's, of a pack's brings
+  int box;                           // rows of a load of shared keys: of a page, at most a block's
   int group;                         // query heads to a key head
+  int pack;                          // sequences of a pack, a power of two; 1: a sequence may have several tiles
   int rows_a, rows_b;                // rows of a place
-  int64_t n_a;                       // ordinals of shared items
   int2 *first_a, *first_b;           // [ordinal]: the first thread block of an item, and how many have a part
   float *out_a, *out_b;              // [ordinal + thread block][2 places][rows][dim]
   float2 *sum_a, *sum_b;             // the same, [rows]: scaled maximum and sum
 };
 
-// What a group (of its shared keys) or a sequence (of its own) has to do: `twos` items of two tiles and `ones` of one for each key
-// head, over `blocks` blocks of keys from position `base` on.
-struct PagedWork { int q0, nq, table, base, lo, len, blocks, twos, ones; };
+// What a group has to do over its shared keys, or a pack over its own: `twos` items of two tiles and `ones` of one for each key
+// head, over `blocks` blocks of keys.
+struct PagedWork { int q0, nq, table, len, blocks, twos, ones; };
 
 __device__ __forceinline__ PagedWork paged_group_work(const PagedParams& p, const PagedGrid& g, int i, bool* bad) {
   PagedWork w = {};
@@ -52,65 +57,111 @@ __device__ __forceinline__ PagedWork paged_group_work(const PagedParams& p, cons
   return w;
 }
 
-__device__ __forceinline__ PagedWork paged_own_work(const PagedParams& p, const PagedGrid& g, int b, bool* bad) {
-  PagedWork w = {};
+// A sequence's own keys: positions shared .. len - 1, in `pieces` pieces from position base on.
+struct PagedOwn { int q0, nq, base, shared, len, pieces; };
+__device__ __forceinline__ PagedOwn paged_own(const PagedParams& p, int b, bool* bad) {
   const PagedSequence s = paged_sequence(p, b, bad);
   *bad = *bad || s.nq > p.max_q;
-  w.q0 = s.q0;
-  w.nq = min(s.nq, p.max_q);
-  w.table = b;
-  w.len = s.len;
-  w.base = s.shared / g.box * g.box;                 // a load begins where a page does
-  w.lo = s.shared - w.base;
+  const int base = s.shared / kPiece * kPiece;
   // queries below the shared length are left to the join, row by row
-  w.blocks = s.len - s.nq < s.shared ? 0 : (w.len - w.base + kKeys - 1) / kKeys;
-  w.ones = (w.nq + g.tile_q - 1) / g.tile_q;
+  const int pieces = s.nq == 0 || s.len - s.nq < s.shared ? 0 : (s.len - base + kPiece - 1) / kPiece;
+  return {s.q0, min(s.nq, p.max_q), base, s.shared, s.len, pieces};
+}
+
+// A pack's work, on every one of its lanes (a lane to a sequence, `pack` lanes side by side); prefix: pieces of those before.
+__device__ __forceinline__ PagedWork paged_pack_work(const PagedGrid& g, const PagedOwn& o, int* prefix) {
+  const int lane = threadIdx.x & 31;
+  int upto = o.pieces, all = o.pieces, q0 = o.q0, q1 = o.q0 + o.nq;
+  for (int d = 1; d < g.pack; d *= 2) {
+    const int y = __shfl_up_sync(0xffffffffu, upto, d);
+    if ((lane & (g.pack - 1)) >= d) upto += y;
+    all += __shfl_xor_sync(0xffffffffu, all, d);
+    q0 = min(q0, __shfl_xor_sync(0xffffffffu, q0, d));
+    q1 = max(q1, __shfl_xor_sync(0xffffffffu, q1, d));
+  }
+  *prefix = upto - o.pieces;
+  PagedWork w = {};
+  w.q0 = q0;
+  w.nq = q1 - q0;
+  w.blocks = (all + kPieces - 1) / kPieces;
+  w.ones = g.pack > 1 ? (w.nq > 0 ? 1 : 0) : (w.nq + g.tile_q - 1) / g.tile_q;
   return w;
 }
 
 __device__ __forceinline__ int64_t paged_weight(const PagedParams& p, const PagedWork& w) {
   if (w.blocks == 0) return 0;
-  return (int64_t)p.kv_heads * ((int64_t)w.twos * (2 * (int64_t)w.blocks + kPagedCost) + (int64_t)w.ones * (w.blocks + kPagedCost));
+  return (int64_t)p.kv_heads * (w.twos + w.ones) * (w.blocks + kPagedCost);
 }
 
 // Ordinals leave room for every item, whatever lies before it: no sum over the groups or sequences is needed.
-__device__ __forceinline__ int64_t paged_ordinal_a(const PagedGrid& g, int group, int q0) { return (int64_t)q0 / (2 * g.tile_q) + group; }
-__device__ __forceinline__ int64_t paged_ordinal_b(const PagedGrid& g, int seq, int q0) { return (int64_t)q0 / g.tile_q + seq; }
+__device__ __forceinline__ int64_t paged_ordinal_a(const PagedGrid& g, int group, int q0) { return (int64_t)(q0 / (2 * g.tile_q)) + group; }
+__device__ __forceinline__ int64_t paged_ordinal_b(const PagedGrid& g, int pack, int q0) {
+  return g.pack > 1 ? (int64_t)pack : (int64_t)(q0 / g.tile_q) + pack;
+}
+// Divisions of what is not negative, in 32 bits where that does: 64 bits take a warp with few registers thousands of cycles.
+__device__ __forceinline__ int64_t paged_divide(int64_t a, int64_t b) {
+  return (a | b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
+}
 
-// A part of an item, as the softmax and the products need it.
+// A part of an item, as the softmax and the products need it.  Query i of the tile, of the last segment with q0 <= i, sees the
+// keys from lo to below limit + (i - q0) * step.
+struct PagedSegment { int q0, lo, limit; };
 struct PagedItem {
   int n, first;                      // blocks of this part (-1: there is no more work), and the first one's number
-  int both;                          // two tiles over the same blocks, or one tile over every second
+  int both, start;                   // two tiles over the same blocks; or one tile, the first block on tile `start`
   int rows[2];                       // of each tile
-  int lo, len;                       // keys that there are, from the item's first block on
-  int limit[2], step;                // row r of a tile sees keys below limit + (r / G) * step
+  int query[2];                      // each tile's first
+  int segments, step;
   float* out[2];
   float2* sum[2];
+  PagedSegment seg[kPackMost];
 };
 
 struct PagedBars {
-  uint64_t q_full[2], q_empty[2], kv_full[8], kv_empty[8], drain[2];
+  uint64_t q_full[4], q_empty[4], kv_full[8], kv_empty[8], drain[2];
   uint64_t s_full[2], s_free[2], p_half[2], p_full[2], pv_done[2];
   uint64_t item_full[kItemSlots], item_empty[kItemSlots];
   PagedItem item[kItemSlots];
   int64_t scan[2][kAttendThreads / 32];
   int64_t before;
-  int at, own;
+  int at;
+  PagedOwn own[kPagedKept];          // the first sequences
+  PagedWork shared[kGroupsKept];     // the first groups
+  uint16_t there[8][kPieces];        // of a stage of values: the rows of a piece that are keys, first | end << 8
   uint32_t tmem;
   int abort;
 };
 template <int DP>
 constexpr int paged_smem_bytes() { return AttendShape<DP>::kSmem + (int)sizeof(PagedBars) + 1024; }
 
-// Block b's share of the list: positions [start, end), the group or sequence (own) that start falls on, and its position.
+// Block b's share of the list: positions [start, end), the group or pack (own) that start falls on, and its position.
 struct PagedShare { int64_t start, end, share, before; int at; bool own; };
 __device__ __forceinline__ PagedShare paged_share(const PagedParams& p, const PagedGrid& g, PagedBars& s) {
   constexpr int W = kAttendThreads / 32;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  int64_t sum[2] = {0, 0};
+  constexpr int KEEP = kPagedKept / kAttendThreads;
   bool bad = false;
-  for (int i = tid; i < p.n_groups; i += kAttendThreads) sum[0] += paged_weight(p, paged_group_work(p, g, i, &bad));
-  for (int i = tid; i < p.n_seqs; i += kAttendThreads) sum[1] += paged_weight(p, paged_own_work(p, g, i, &bad));
+  auto weight = [&](bool own, int i) {               // of a group, or of a pack, on its first sequence's thread
+    if (!own) {
+      if (i >= p.n_groups) return (int64_t)0;
+      const PagedWork w = paged_group_work(p, g, i, &bad);
+      if (i < kGroupsKept) s.shared[i] = w;
+      return paged_weight(p, w);
+    }
+    PagedOwn o = {p.n_q_rows, 0, 0, 0, 0, 0};
+    if (i < p.n_seqs) o = paged_own(p, i, &bad);
+    if (i < kPagedKept) s.own[i] = o;
+    int prefix;
+    const PagedWork w = paged_pack_work(g, o, &prefix);
+    return (lane & (g.pack - 1)) == 0 ? paged_weight(p, w) : (int64_t)0;
+  };
+  int64_t sum[2] = {0, 0}, kept[KEEP] = {};
+  // (groups from the last thread on: where there are few of both, other warps look at them)
+  for (int c = 0; c < p.n_groups; c += kAttendThreads) sum[0] += weight(false, c + kAttendThreads - 1 - tid);
+#pragma unroll
+  for (int k = 0; k < KEEP; ++k)
+    if (k * kAttendThreads < p.n_seqs) sum[1] += kept[k] = weight(true, k * kAttendThreads + tid);
+  for (int c = kPagedKept; c < p.n_seqs; c += kAttendThreads) sum[1] += weight(true, c + tid);
   if (bad && blockIdx.x == 0) atomicOr(p.err, DEV_ERR_INDEX_RANGE);
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
@@ -127,7 +178,7 @@ __device__ __forceinline__ PagedShare paged_share(const PagedParams& p, const Pa
   __syncthreads();
   PagedShare r;
   const int64_t all = sum[0] + sum[1];
-  r.share = max((int64_t)2, (all + gridDim.x - 1) / gridDim.x);      // two: every share that an item spans has a block of it
+  r.share = max((int64_t)1, paged_divide(all + gridDim.x - 1, gridDim.x));
   r.start = min(all, (int64_t)blockIdx.x * r.share);
   r.end = min(all, r.start + r.share);
   r.own = r.start >= sum[0];
@@ -136,9 +187,14 @@ __device__ __forceinline__ PagedShare paged_share(const PagedParams& p, const Pa
   if (r.start >= r.end) return r;
   const int n = r.own ? p.n_seqs : p.n_groups;
   for (int c = 0; c < n; c += kAttendThreads) {
-    const int i = c + tid;
     int64_t w = 0;
-    if (i < n) w = paged_weight(p, r.own ? paged_own_work(p, g, i, &bad) : paged_group_work(p, g, i, &bad));
+    if (r.own && c < kPagedKept) {
+#pragma unroll
+      for (int k = 0; k < KEEP; ++k)
+        if (c == k * kAttendThreads) w = kept[k];
+    } else {
+      w = weight(r.own, c + tid);
+    }
     int64_t upto = w;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
@@ -154,7 +210,7 @@ __device__ __forceinline__ PagedShare paged_share(const PagedParams& p, const Pa
     }
     const int64_t here = r.start - r.before;
     if (here >= upto - w && here < upto) {
-      s.at = i;
+      s.at = r.own ? (c + tid) / g.pack : c + tid;
       s.before = r.before + upto - w;
     }
     __syncthreads();
@@ -167,62 +223,73 @@ __device__ __forceinline__ PagedShare paged_share(const PagedParams& p, const Pa
   return r;
 }
 
-// Goes through a share, by one warp: part(work, own, group or sequence, its item s, the item's blocks [b0, b1) that the share has,
-// where its first block stands in the list), until ok is false.
+// Goes through a share, by one warp: part(work, own, group or pack, its item s, the item's blocks [b0, b1) that the share has,
+// where its first block stands in the list, the sequence of the pack that is this lane's and the pieces before it), until ok is
+// false.
 template <typename F>
-__device__ __forceinline__ void paged_walk(const PagedParams& p, const PagedGrid& g, const PagedShare& share, F& part, bool& ok) {
+__device__ __forceinline__ void paged_walk(const PagedParams& p, const PagedGrid& g, const PagedShare& share, const PagedBars& s_bars, F& part, bool& ok) {
   const int lane = threadIdx.x & 31;
-  int64_t at = share.before;                         // where the next group or sequence stands in the list
+  int64_t at = share.before;                         // where the next group or pack stands in the list
   bool own = share.own;
   int index = share.at, chunk0 = -1;
-  PagedWork chunk = {};                              // of chunk0 + lane
+  PagedWork chunk = {};                              // of group chunk0 + lane, or of the pack of sequence chunk0 + lane
+  PagedOwn seq = {};
+  int before = 0;
   while (ok && at < share.end) {
-    const int n = own ? p.n_seqs : p.n_groups;
-    if (index >= n) {
+    const int first = own ? index * g.pack : index, n = own ? p.n_seqs : p.n_groups;
+    if (first >= n) {
       if (own) break;
       own = true;
       index = 0;
       chunk0 = -1;
       continue;
     }
-    if (chunk0 < 0 || index >= chunk0 + 32) {
-      chunk0 = index;
+    if (chunk0 < 0 || first >= chunk0 + 32) {
+      chunk0 = first;
       bool bad = false;
-      chunk = PagedWork{};
-      if (chunk0 + lane < n) chunk = own ? paged_own_work(p, g, chunk0 + lane, &bad) : paged_group_work(p, g, chunk0 + lane, &bad);
+      if (own) {
+        seq = {p.n_q_rows, 0, 0, 0, 0, 0};
+        if (chunk0 + lane < n) seq = chunk0 + lane < kPagedKept ? s_bars.own[chunk0 + lane] : paged_own(p, chunk0 + lane, &bad);
+        chunk = paged_pack_work(g, seq, &before);
+      } else {
+        chunk = PagedWork{};
+        if (chunk0 + lane < n) chunk = chunk0 + lane < kGroupsKept ? s_bars.shared[chunk0 + lane] : paged_group_work(p, g, chunk0 + lane, &bad);
+      }
     }
+    const int from = first - chunk0;
     PagedWork w;
-    const int from = index - chunk0;
     w.q0 = __shfl_sync(0xffffffffu, chunk.q0, from);
     w.nq = __shfl_sync(0xffffffffu, chunk.nq, from);
     w.table = __shfl_sync(0xffffffffu, chunk.table, from);
-    w.base = __shfl_sync(0xffffffffu, chunk.base, from);
-    w.lo = __shfl_sync(0xffffffffu, chunk.lo, from);
     w.len = __shfl_sync(0xffffffffu, chunk.len, from);
     w.blocks = __shfl_sync(0xffffffffu, chunk.blocks, from);
     w.twos = __shfl_sync(0xffffffffu, chunk.twos, from);
     w.ones = __shfl_sync(0xffffffffu, chunk.ones, from);
     const int64_t weight = paged_weight(p, w);
     if (weight > 0 && at + weight > share.start) {
-      const int64_t two = 2 * (int64_t)w.blocks + kPagedCost, one = w.blocks + kPagedCost;
-      const int64_t twos = (int64_t)w.twos * p.kv_heads, all = twos + (int64_t)w.ones * p.kv_heads;
+      PagedOwn mine = {};                            // lane l of the pack's: its sequence l
+      int prefix = 0;
+      if (own) {
+        const int l = (from + lane) & 31;
+        mine.q0 = __shfl_sync(0xffffffffu, seq.q0, l);
+        mine.nq = __shfl_sync(0xffffffffu, seq.nq, l);
+        mine.base = __shfl_sync(0xffffffffu, seq.base, l);
+        mine.shared = __shfl_sync(0xffffffffu, seq.shared, l);
+        mine.len = __shfl_sync(0xffffffffu, seq.len, l);
+        mine.pieces = __shfl_sync(0xffffffffu, seq.pieces, l);
+        prefix = __shfl_sync(0xffffffffu, before, l);
+        w.table = first;
+      }
+      const int64_t one = w.blocks + kPagedCost, all = (int64_t)(w.twos + w.ones) * p.kv_heads;
       int64_t s = 0, pos = at;                       // the item, and where it stands
       if (share.start > at) {
-        s = min((share.start - at) / two, twos);
-        pos = at + s * two;
-        if (s == twos) {
-          const int64_t more = (share.start - pos) / one;
-          s += more;
-          pos += more * one;
-        }
+        s = paged_divide(share.start - at, one);
+        pos = at + s * one;
       }
-      for (; ok && s < all && pos < share.end; ++s) {
-        const int step = s < twos ? 2 : 1;
+      for (; ok && s < all && pos < share.end; ++s, pos += one) {
         const int64_t u0 = pos + kPagedCost;
-        const int64_t skip = max((int64_t)0, share.start - u0), upto = max((int64_t)0, share.end - u0);
-        const int b0 = (int)min((int64_t)w.blocks, (skip + step - 1) / step), b1 = (int)min((int64_t)w.blocks, (upto + step - 1) / step);
-        if (b1 > b0) part(w, own, index, (uint32_t)s, b0, b1, u0);
-        pos += step == 2 ? two : one;
+        const int b0 = (int)min((int64_t)w.blocks, max((int64_t)0, share.start - u0)), b1 = (int)min((int64_t)w.blocks, max((int64_t)0, share.end - u0));
+        if (b1 > b0) part(w, own, index, (uint32_t)s, b0, b1, u0, mine, prefix);
       }
     }
     at += weight;
@@ -234,26 +301,29 @@ template <typename T, int DP>
 __global__ void __launch_bounds__(kAttendThreads, 1)
     paged_tile_kernel(const __grid_constant__ PagedParams p, const __grid_constant__ PagedGrid g,
                       const __grid_constant__ CUtensorMap map_qa, const __grid_constant__ CUtensorMap map_qb,
-                      const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+                      const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                      const __grid_constant__ CUtensorMap map_k16, const __grid_constant__ CUtensorMap map_v16) {
   using S = AttendShape<DP>;
+  constexpr int QT = 2 * S::kQBufs;                  // places of a tile's queries
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   uint8_t* q_buf = smem;
-  uint8_t* kv_buf = smem + S::kQBufs * 2 * S::kQBytes;
+  uint8_t* kv_buf = smem + QT * S::kQBytes;
   PagedBars& b = *reinterpret_cast<PagedBars*>(smem + S::kSmem);
   const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
   volatile int* abort = &b.abort;
 
   if (warp == kCopyWarp && lane == 0) {
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 4; ++i) {
       mbar_init(&b.q_full[i], 1);
       mbar_init(&b.q_empty[i], S::kMmaWarps);
+    }
+    for (int i = 0; i < 2; ++i) {
       mbar_init(&b.s_full[i], 1);
       mbar_init(&b.s_free[i], 4);
       mbar_init(&b.p_half[i], 4);
       mbar_init(&b.p_full[i], 4);
       mbar_init(&b.pv_done[i], 1);
-      mbar_init(&b.drain[i], 1);
     }
     for (int i = 0; i < 8; ++i) {
       mbar_init(&b.kv_full[i], 1);
@@ -263,6 +333,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
       mbar_init(&b.item_full[i], 1);
       mbar_init(&b.item_empty[i], kSoftmaxWarps + S::kMmaWarps);
     }
+    for (int i = 0; i < 2; ++i) mbar_init(&b.drain[i], 1);
     b.abort = 0;
     fence_mbar_init();
   }
@@ -297,39 +368,76 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
   };
   if (warp >= kSoftmaxWarps) {
     regs_down<kControlRegs>();
-    if (warp == kCopyWarp) {
-      // ---------------- the work, part by part; its queries, and its keys and values through the ring
-      const int boxes = kKeys / g.box;               // of a block, a lane to each and each half of a head
-      const int box = lane / halves, half = lane % halves;
-      uint32_t kv = 0, q = 0, items = 0;
+    if (warp >= kCopyWarp) {
+      // ---------------- the work, part by part: one warp hands it on and fetches queries and keys, the other values.  (A load of
+      // pieces is 8 or 16 boxes, and a warp issues them one after another, at some 40 ns each.)
+      const int kind = warp - kCopyWarp;
+      uint32_t kv = kind, q = 0, items = 0, turn = 0;   // turn: the tile of tensor memory that the next block of one tile is on
       bool ok = true;
-      auto hand_over = [&](const PagedItem& it) {
+      // A block's keys or values: this lane's box of `rows` rows, from `row` on (mine: there are such), to row `to` of the stage.
+      auto load = [&](bool mine, int row, int to, int rows, int half, int head, const CUtensorMap* mk, const CUtensorMap* mv,
+                      uint32_t there) {
+        const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, mine)) * (uint32_t)rows * 128;
+        const uint32_t st = kv % S::kStages;
+        if (kv >= S::kStages) ok = wait(&b.kv_empty[st], kv / S::kStages - 1);
+        if (!ok) return;
+        if (kind && lane < kPieces) b.there[st][lane] = (uint16_t)there;
+        __syncwarp();
+        if (lane == 0) mbar_arrive_expect_tx(&b.kv_full[st], bytes);
+        __syncwarp();
+        if (mine)
+          tma_load_3d(kv_buf + st * S::kKvBytes + half * kKeys * 128 + to * 128, kind ? mv : mk, 64 * half, head, row, &b.kv_full[st]);
+        __syncwarp();
+        kv += 2;
+      };
+      // The page of position pos of a sequence, and the row there; nowhere, where zeros are read, if there is no such page.
+      auto page_of = [&](bool mine, int seq, int pos) { return mine ? p.table[(int64_t)seq * p.table_stride + (pos >> p.shift)] : 0; };
+      auto row_of = [&](int page, int pos) {
+        if (page >= 0 && page < p.n_pages) return (page << p.shift) + (pos & ((1 << p.shift) - 1));
+        atomicOr(p.err, DEV_ERR_INDEX_RANGE);
+        return (int)(p.n_pages << p.shift);
+      };
+      auto clip = [](int x) { return (uint32_t)min(max(x, 0), kPiece); };
+      auto hand_over = [&](const PagedItem& it, const PagedSegment& segment) {
         const uint32_t slot = items % kItemSlots;
         if (items >= kItemSlots) ok = wait(&b.item_empty[slot], items / kItemSlots - 1);
         if (!ok) return;
         if (lane == 0) {
-          b.item[slot] = it;
-          mbar_arrive(&b.item_full[slot]);
+          PagedItem& to = b.item[slot];
+          to.n = it.n; to.first = it.first; to.both = it.both; to.start = it.start; to.segments = it.segments; to.step = it.step;
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            to.rows[t] = it.rows[t]; to.query[t] = it.query[t]; to.out[t] = it.out[t]; to.sum[t] = it.sum[t];
+          }
         }
+        if (lane < it.segments) b.item[slot].seg[lane] = segment;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&b.item_full[slot]);
         ++items;
       };
       // Item s of what w has to do, its blocks [b0, b1); u0: where its first block stands in the list.
-      auto part = [&](const PagedWork& w, bool own, int index, uint32_t s, int b0, int b1, int64_t u0) {
+      auto part = [&](const PagedWork& w, bool own, int index, uint32_t s, int b0, int b1, int64_t u0, const PagedOwn& mine, int prefix) {
         const uint32_t e = s / (uint32_t)p.kv_heads;
         const int head = (int)(s - e * (uint32_t)p.kv_heads);
-        PagedItem it = {};
+        PagedItem it;
         it.n = b1 - b0;
         it.first = b0;
         it.both = e < (uint32_t)w.twos;
-        const int tile = own ? (int)e : 2 * (int)e, row0 = w.q0 + tile * g.tile_q;
-        const int have = w.nq - tile * g.tile_q;
-        it.rows[0] = min(have, g.tile_q) * g.group;
-        it.rows[1] = it.both ? min(have - g.tile_q, g.tile_q) * g.group : it.rows[0];
-        it.lo = w.lo;
-        it.len = w.len - w.base;
+        it.start = (int)(turn & 1);
+        if (!it.both) turn += (uint32_t)it.n;
+        const int tile = own ? (int)e : 2 * (int)e, row0 = w.q0 + tile * g.tile_q, have = w.nq - tile * g.tile_q;
+        const int most = own ? g.box_b : g.box_a;
+        it.rows[0] = min(have, most) * g.group;
+        it.rows[1] = it.both ? min(have - g.tile_q, most) * g.group : it.rows[0];
+        it.query[0] = tile * g.tile_q;
+        it.query[1] = it.both ? it.query[0] + g.tile_q : it.query[0];
         it.step = own ? 1 : 0;
-        it.limit[0] = own ? w.len - w.nq + tile * g.tile_q + 1 - w.base : it.len;
-        it.limit[1] = it.limit[0];
+        it.segments = own ? g.pack : 1;
+        PagedSegment segment = {0, 0, w.len};
+        if (own) {                                   // this lane's sequence; one without pieces sees nothing
+          const int key0 = prefix * kPiece - mine.base;
+          segment = {mine.q0 - w.q0, mine.pieces ? key0 + mine.shared : INT_MAX, mine.pieces ? key0 + mine.len - mine.nq + 1 : 0};
+        }
         const int64_t ordinal = ((own ? paged_ordinal_b(g, index, w.q0) : paged_ordinal_a(g, index, w.q0)) + e) * p.kv_heads + head;
         const int64_t place = 2 * (ordinal + blockIdx.x);
         const int place_rows = own ? g.rows_b : g.rows_a;
@@ -338,65 +446,84 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
           it.out[t] = (own ? g.out_b : g.out_a) + (place + t) * place_rows * p.dim;
           it.sum[t] = (own ? g.sum_b : g.sum_a) + (place + t) * place_rows;
         }
-        if (b0 == 0 && lane == 0) {
-          const int64_t last = u0 + (int64_t)(w.blocks - 1) * (it.both ? 2 : 1);
-          (own ? g.first_b : g.first_a)[ordinal] = make_int2(blockIdx.x, (int)((last - share.start) / share.share) + 1);
+        if (b0 == 0 && lane == 0 && kind == 0) {
+          const int64_t last = u0 + w.blocks - 1;
+          (own ? g.first_b : g.first_a)[ordinal] =
+              make_int2(blockIdx.x, last < share.end ? 1 : (int)paged_divide(last - share.start, share.share) + 1);
         }
-        hand_over(it);
+        if (kind == 0) hand_over(it, segment);
         if (!ok) return;
-        const uint32_t qb = q % S::kQBufs;
-        if (q >= S::kQBufs) ok = wait(&b.q_empty[qb], q / S::kQBufs - 1);
-        if (!ok) return;
-        const int tiles = it.both ? 2 : 1, q_box = own ? g.box_b : g.box_a;
-        if (lane == 0) mbar_arrive_expect_tx(&b.q_full[qb], (uint32_t)(tiles * halves * q_box * g.group * 128));
-        __syncwarp();
-        if (lane < tiles * halves)
-          tma_load_3d(q_buf + (qb * 2 + lane / halves) * S::kQBytes + (lane % halves) * kTileQ * 128, own ? &map_qb : &map_qa,
-                      64 * (lane % halves), head * g.group, row0 + lane / halves * g.tile_q, &b.q_full[qb]);
-        ++q;
-        const int* table = p.table + (int64_t)w.table * p.table_stride;
+        const int tiles = kind ? 0 : it.both ? 2 : 1;
 #pragma unroll 1
-        for (int i = b0; i < b1 && ok; ++i) {
-          const int pos = w.base + i * kKeys + box * g.box;
-          const bool mine = box < boxes && pos < w.len;
-          int row = 0;
-          if (mine) {
-            const int page = table[pos >> p.shift];
-            if (page >= 0 && page < p.n_pages) {
-              row = (page << p.shift) + (pos & ((1 << p.shift) - 1));
-            } else {                                 // nowhere: zeros
-              row = (int)(p.n_pages << p.shift);
-              atomicOr(p.err, DEV_ERR_INDEX_RANGE);
+        for (int t = 0; t < tiles; ++t, ++q) {
+          const uint32_t qb = q % QT;
+          if (q >= QT) ok = wait(&b.q_empty[qb], q / QT - 1);
+          if (!ok) return;
+          if (lane == 0) mbar_arrive_expect_tx(&b.q_full[qb], (uint32_t)(halves * most * g.group * 128));
+          __syncwarp();
+          if (lane < halves)
+            tma_load_3d(q_buf + qb * S::kQBytes + lane * kTileQ * 128, own ? &map_qb : &map_qa, 64 * lane, head * g.group,
+                        row0 + t * g.tile_q, &b.q_full[qb]);
+          __syncwarp();
+        }
+        // A lane to a box, the halves of a head one after another; the next block's pages are looked up while this one's stage is
+        // waited for.
+        const int piece = lane & (kPieces - 1);
+        if (own) {
+          const int half = lane / kPieces;
+          const int shift = mine.base - prefix * kPiece, end = mine.pieces ? mine.len : 0;
+          auto place = [&](int i, int* pos, uint32_t* there, int* page) {
+            const int at = i * kPieces + piece;
+            int f = 0;                               // the last sequence with so many pieces before it
+#pragma unroll 1
+            for (int d = g.pack / 2; d > 0; d /= 2) {
+              const int before = __shfl_sync(0xffffffffu, prefix, f + d);
+              if (before <= at) f += d;
             }
-          }
-          const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, mine)) * (uint32_t)g.box * 128;
+            *pos = __shfl_sync(0xffffffffu, shift, f) + at * kPiece;
+            const int lo = __shfl_sync(0xffffffffu, mine.shared, f), hi = __shfl_sync(0xffffffffu, end, f);
+            const bool have = *pos < hi;
+            *there = have ? clip(lo - *pos) | clip(hi - *pos) << 8 : 0;
+            *page = page_of(have && half < halves, w.table + f, *pos);
+            return have && half < halves;
+          };
+          int pos, page;
+          uint32_t there;
+          bool have_it = place(b0, &pos, &there, &page);
 #pragma unroll 1
-          for (int kind = 0; kind < 2; ++kind, ++kv) {
-            const uint32_t st = kv % S::kStages;
-            if (kv >= S::kStages) ok = wait(&b.kv_empty[st], kv / S::kStages - 1);
-            if (!ok) break;
-            if (lane == 0) mbar_arrive_expect_tx(&b.kv_full[st], bytes);
-            __syncwarp();
-            if (mine)
-              tma_load_3d(kv_buf + st * S::kKvBytes + half * kKeys * 128 + box * g.box * 128, kind ? &map_v : &map_k, 64 * half, head,
-                          row, &b.kv_full[st]);
-            __syncwarp();
+          for (int i = b0; i < b1 && ok; ++i) {
+            const bool now = have_it;
+            const int row = now ? row_of(page, pos) : 0;
+            const uint32_t rows_there = there;
+            if (i + 1 < b1) have_it = place(i + 1, &pos, &there, &page);
+            load(now, row, piece * kPiece, kPiece, half, head, &map_k16, &map_v16, rows_there);
+          }
+        } else {
+          const int boxes = kKeys / g.box, half = lane / boxes, box = lane - half * boxes;
+          int pos = b0 * kKeys + box * g.box, page = page_of(half < halves && pos < w.len, w.table, pos);
+#pragma unroll 1
+          for (int i = b0; i < b1 && ok; ++i) {
+            const bool now = half < halves && pos < w.len;
+            const int row = now ? row_of(page, pos) : 0;
+            pos += kKeys;
+            if (i + 1 < b1) page = page_of(half < halves && pos < w.len, w.table, pos);
+            load(now, row, box * g.box, g.box, half, head, &map_k, &map_v, clip(w.len - i * kKeys - piece * kPiece) << 8);
           }
         }
       };
-      paged_walk(p, g, share, part, ok);
-      if (ok) {
+      paged_walk(p, g, share, b, part, ok);
+      if (ok && kind == 0) {
         PagedItem end = {};
         end.n = -1;
-        hand_over(end);
+        hand_over(end, PagedSegment{});
       }
       // every copy lands before the block leaves
 #pragma unroll 1
-      for (uint32_t i = 0; i < S::kStages; ++i)
-        if (kv > i) drain_wait(&b.kv_full[(kv - 1 - i) % S::kStages], (kv - 1 - i) / S::kStages & 1);
+      for (uint32_t i = 2; i <= S::kStages; i += 2)
+        if (kv >= i + kind) drain_wait(&b.kv_full[(kv - i) % S::kStages], (kv - i) / S::kStages & 1);
 #pragma unroll 1
-      for (uint32_t i = 0; i < S::kQBufs; ++i)
-        if (q > i) drain_wait(&b.q_full[(q - 1 - i) % S::kQBufs], (q - 1 - i) / S::kQBufs & 1);
+      for (uint32_t i = 0; i < QT; ++i)
+        if (q > i) drain_wait(&b.q_full[(q - 1 - i) % QT], (q - 1 - i) / QT & 1);
     } else if (warp < kMmaWarp + S::kMmaWarps) {
       // ---------------- the products of tiles mine .. mine + NT - 1
       constexpr int NT = 2 / S::kMmaWarps;
@@ -414,22 +541,20 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         const uint32_t slot = items % kItemSlots;
         ok = wait(&b.item_full[slot], items / kItemSlots);
         if (!ok) break;
-        const int n = uniform(b.item[slot].n), first = uniform(b.item[slot].first), both = uniform(b.item[slot].both),
-                  lo = uniform(b.item[slot].lo), len = uniform(b.item[slot].len);
+        const int n = uniform(b.item[slot].n), both = uniform(b.item[slot].both), start = uniform(b.item[slot].start);
         __syncwarp();
         if (lane == 0) mbar_arrive(&b.item_empty[slot]);
         ++items;
         if (n < 0) break;
-        const uint32_t qb = q % S::kQBufs;
         bool fresh[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) fresh[t] = true;
-        auto has = [&](int t, int i) { return both || (i & 1) == mine + t; };      // block i of the part
+        auto has = [&](int t, int i) { return both || ((i + start) & 1) == mine + t; };       // block i of the part
         auto qk = [&](int t, uint32_t st) {          // S = Q K^T, once the last scores have been read
           if (S::kApart && qk_n[t] > 0) ok = wait(&b.s_free[mine + t], qk_n[t] - 1);
           if (!ok) return;
           tc_fence_after();
-          const uint64_t qa = q_desc + ((qb * 2 + (both ? mine + t : 0)) * S::kQBytes >> 4), ka = k_desc + (st * S::kKvBytes >> 4);
+          const uint64_t qa = q_desc + (((q + (both ? mine + t : 0)) % QT) * S::kQBytes >> 4), ka = k_desc + (st * S::kKvBytes >> 4);
           if (elect_one()) {
 #pragma unroll
             for (int k = 0; k < DP / 16; ++k) {
@@ -444,7 +569,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         };
         // Scores in places of their own, or of the tile whose turn it is next, need not wait for the weights of this block.
         const bool ahead = S::kApart || !both;
-        ok = wait(&b.q_full[qb], q / S::kQBufs);
+        ok = wait(&b.q_full[q % QT], q / QT) && (!both || wait(&b.q_full[(q + 1) % QT], (q + 1) / QT));
         for (int i = -1; i < n && ok; ++i) {
           const bool more = i + 1 < n;
           const uint32_t kn = kv + 2 * (i + 1), vn = kv + 2 * i + 1;
@@ -462,15 +587,22 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
           if (i >= 0) {
             ok = wait(&b.kv_full[vs], vn / S::kStages);
             if (!ok) break;
-            // Values of rows that are no keys of the item: zeros, so that weights of zero leave no trace of them.  (Where
-            // several warps do this, each does before its own products.)
-            const int key0 = (first + i) * kKeys;
-            if (key0 < lo || key0 + kKeys > len) {
+            // Values of rows that are no keys: zeros, so that weights of zero leave no trace of them.  (Where several warps do this,
+            // each does before its own products.)
+            const uint32_t there = b.there[vs][lane / 4], row4 = lane % 4 * 4;                // lane l: rows 4 l .. 4 l + 3
+            uint32_t gone = 0;
+#pragma unroll
+            for (uint32_t r = 0; r < 4; ++r) gone |= row4 + r < (there & 255) || row4 + r >= there >> 8 ? 1u << r : 0u;
+            uint32_t some = __ballot_sync(0xffffffffu, gone != 0);
+            if (some) {
 #pragma unroll 1
-              for (int r = lane; r < kKeys * 8; r += 32)
-                if (key0 + r / 8 < lo || key0 + r / 8 >= len)
+              for (; some; some &= some - 1) {
+                const int four = __ffs(some) - 1, r = lane / 8;
+                if (__shfl_sync(0xffffffffu, gone, four) >> r & 1u)
                   for (int h = 0; h < halves; ++h)
-                    *reinterpret_cast<uint4*>(kv_buf + vs * S::kKvBytes + h * kKeys * 128 + r * 16) = make_uint4(0, 0, 0, 0);
+                    *reinterpret_cast<uint4*>(kv_buf + vs * S::kKvBytes + h * kKeys * 128 + (4 * four + r) * 128 + lane % 8 * 16) =
+                        make_uint4(0, 0, 0, 0);
+              }
               fence_async_shared();
               __syncwarp();
             }
@@ -505,12 +637,15 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
           if (elect_one()) {
             if (more && !ahead) mma_commit(&b.kv_empty[ks]);
             if (i >= 0) mma_commit(&b.kv_empty[vs]);
-            if (i + 2 == n) mma_commit(&b.q_empty[qb]);      // the part's last Q K^T is out
+            if (i + 2 == n) {                        // the part's last Q K^T is out
+              mma_commit(&b.q_empty[q % QT]);
+              if (both) mma_commit(&b.q_empty[(q + 1) % QT]);
+            }
           }
           __syncwarp();
         }
         kv += 2 * n;
-        ++q;
+        q += both ? 2 : 1;
       }
       if (elect_one()) mma_commit(&b.drain[mine]);
       __syncwarp();
@@ -519,7 +654,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
   } else {
     regs_up<kSoftmaxRegs>();
     // ---------------- softmax: a warpgroup to a tile, a row to a thread
-    const int wg = warp >> 2, w0 = (warp & 3) * 32, row = w0 + lane, query = row / g.group;
+    const int wg = warp >> 2, w0 = (warp & 3) * 32, row = w0 + lane, row_query = row / g.group;
     const uint32_t lanes = (uint32_t)w0 << 16;
     constexpr int PARTS = kKeys / 32;
     const uint32_t ts = tmem + lanes + kKeys * wg, tp = tmem + lanes + S::kP + S::kPStep * wg, to = tmem + lanes + S::kO + DP * wg;
@@ -532,17 +667,30 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
       ok = wait(&b.item_full[slot], items / kItemSlots);
       if (!ok) break;
       const PagedItem& item = b.item[slot];
-      const int all = item.n, both = item.both, rows = item.rows[wg], len = item.len, lo = item.lo;
-      const int low = item.limit[wg], limit = min(len, low + query * item.step);      // the tile's first row's, and the row's
-      const int first = item.first + (both ? 0 : wg);
+      const int all = item.n, both = item.both, rows = item.rows[wg];
+      const int skip = both || item.start == wg ? 0 : 1, first = item.first + skip;
       float* out = item.out[wg] + (int64_t)row * p.dim;
       float2* sum_at = item.sum[wg] + row;
+      int lo = INT_MAX, limit = 0;                   // the keys that the row sees; none where the tile has no such row
+      if (all > 0 && row < rows) {
+        const int query = item.query[wg] + row_query;
+        int a = 0, z = item.segments;
+#pragma unroll 1
+        while (z - a > 1) {
+          const int mid = (a + z) / 2;
+          if (item.seg[mid].q0 <= query) a = mid; else z = mid;
+        }
+        lo = item.seg[a].lo;
+        limit = item.seg[a].limit + (query - item.seg[a].q0) * item.step;
+      }
       __syncwarp();
       if (lane == 0) mbar_arrive(&b.item_empty[slot]);
       ++items;
       if (all < 0) break;
-      const int blocks = both ? all : (all + 1 - wg) / 2;
-      const bool idle = w0 >= rows;                  // the warp has no rows: what lies in its weights touches no other row
+      const int blocks = both ? all : (all + 1 - skip) / 2;
+      // what all rows of the warp see, and what some row does
+      const int whole_lo = __reduce_max_sync(0xffffffffu, row < rows ? lo : 0), whole_hi = __reduce_min_sync(0xffffffffu, row < rows ? limit : INT_MAX);
+      const int some_lo = __reduce_min_sync(0xffffffffu, lo), some_hi = __reduce_max_sync(0xffffffffu, limit);
       float m = row < rows ? -INFINITY : INFINITY, l = 0.f;        // rows that the tile does not have weigh nothing
       auto stored = [&](uint64_t* bar) {             // the weights so far are in place
         tmem_st_wait();
@@ -566,17 +714,18 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         ok = wait(&b.s_full[wg], n);
         if (!ok) break;
         tc_fence_after();
-        if (idle) {
-          // not before the others are through with the last block: their arrivals are counted together
+        if (key0 >= some_hi || key0 + kKeys <= some_lo) {
+          // No row of the warp sees any of it.  Not before the others are through with the last block: their arrivals are
+          // counted together, and the weights before are used.
           if (i > 0) ok = wait(&b.pv_done[wg], n - 1);
           if (!ok) break;
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) {
-            if (S::kApart) mbar_arrive(&b.s_free[wg]);
-            mbar_arrive(&b.p_half[wg]);
-            mbar_arrive(&b.p_full[wg]);
-          }
+          tc_fence_after();
+          const uint32_t none[16] = {};
+#pragma unroll
+          for (int c = 0; c < PARTS; ++c) tmem_st_32x16(tp + 16 * c, none);
+          if (S::kApart && lane == 0) mbar_arrive(&b.s_free[wg]);
+          stored(&b.p_half[wg]);
+          if (lane == 0) mbar_arrive(&b.p_full[wg]);
           __syncwarp();
           continue;
         }
@@ -594,7 +743,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
 #pragma unroll
           for (int e = 0; e < kKeys; ++e) s[e] = -s[e];
         }
-        if (key0 < lo || key0 + kKeys > low) {       // not every row sees all of it
+        if (key0 < whole_lo || key0 + kKeys > whole_hi) {            // not every row sees all of it
           auto below = [](int x) { return x >= 32 ? 0xffffffffu : x <= 0 ? 0u : (1u << x) - 1u; };
 #pragma unroll
           for (int c = 0; c < PARTS; ++c) {
@@ -639,17 +788,19 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         stored(&b.p_full[wg]);
       }
       if (!ok) break;
+      const bool some = blocks > 0 && row < rows && m > -INFINITY;   // NaN too: a sum of it is, with the maximum of what is not
+      const bool odd = blocks > 0 && row < rows && l != 0.f;
       if (blocks > 0) {
         ok = wait(&b.pv_done[wg], n - 1);
         if (!ok) break;
         tc_fence_after();
-        if (!idle) {
+        if (__any_sync(0xffffffffu, some || odd)) {
 #pragma unroll 1
           for (int c = 0; c < DP; c += 32) {
             float o[32];
             tmem_ld_32x32(to + c, o);
             tmem_wait_ld_32(o);
-            if (row < rows) {
+            if (some || odd) {
 #pragma unroll
               for (int e = 0; e < 32; e += 8)
                 if (c + e < p.dim) st_global_32b(out + c + e, reinterpret_cast<const uint32_t*>(o + e));
@@ -658,7 +809,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         }
         tc_fence_before();
       }
-      if (row < rows) *sum_at = blocks > 0 ? make_float2(m * scale, l) : make_float2(-INFINITY, 0.f);
+      if (row < rows) *sum_at = some || odd ? make_float2(some ? m * scale : 0.f, l) : make_float2(-INFINITY, 0.f);
     }
   }
   tc_fence_before();
@@ -670,7 +821,8 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
 // ------------------------------------------------------------------ join
 constexpr int kPagedJoinWarps = 4;
 
-// A row of a head to a warp: the parts of its shared and of its own keys into one, four elements to a lane.
+// A row of a head to a warp: the parts of its shared and of its own keys into one, four elements to a lane.  Bound by its chain of
+// dependent loads: offsets, first blocks, sums, outputs.
 template <typename T>
 __global__ void __launch_bounds__(32 * kPagedJoinWarps) paged_join_kernel(const __grid_constant__ PagedParams p,
                                                                            const __grid_constant__ PagedGrid g, int blocks) {
@@ -679,11 +831,19 @@ __global__ void __launch_bounds__(32 * kPagedJoinWarps) paged_join_kernel(const 
   const int64_t at = (int64_t)blockIdx.x * kPagedJoinWarps + warp;
   pdl_wait();
   if (at >= (int64_t)p.n_q_rows * p.heads) return;
-  const int row = (int)(at / p.heads), head = (int)(at - (int64_t)row * p.heads), kv = head / g.group;
+  const int row = (int)paged_divide(at, p.heads), head = (int)(at - (int64_t)row * p.heads), kv = head / g.group;
   const int seq = sequence_of(p.q_start, p.n_seqs, p.n_q_rows, row);
   if (seq < 0) return;
   bool bad = false;
   const PagedSequence sq = paged_sequence(p, seq, &bad);
+  // first rows of the pack and of the group, and the group's last
+  const int pack = g.pack > 1 ? seq / g.pack : seq;
+  int pack0 = p.q_start[pack * g.pack], group0 = 0, group1 = 0;
+  if (sq.shared > 0) {
+    group0 = min(max(p.q_start[min(sq.first, p.n_seqs)], 0), p.n_q_rows);
+    group1 = min(max(p.q_start[min(max(p.group_start[sq.group + 1], sq.first), p.n_seqs)], group0), p.n_q_rows);
+  }
+  pack0 = min(max(pack0, 0), p.n_q_rows);
   const int i = row - sq.q0;
   if (i >= p.max_q) return;
   auto slowly = [&] {
@@ -697,82 +857,83 @@ __global__ void __launch_bounds__(32 * kPagedJoinWarps) paged_join_kernel(const 
     return;
   }
   // where the row's parts lie: of the shared keys, [0, na), and of its own, [na, na + nb)
-  const float *oa = nullptr, *ob = nullptr;
-  const float2 *sa = nullptr, *sb = nullptr;
-  int na = 0, nb = 0, every = 1;                     // every: shared parts of both places, or of one
+  int64_t ordinal_a = 0, ordinal_b;
+  int row_a = 0, row_b, tile_a = 0, every = 1;       // every: shared parts of both places (1), or of one (2)
   if (sq.shared > 0) {
-    const int group = sequence_of(p.group_start, p.n_groups, p.n_seqs, seq);
-    const PagedWork w = paged_group_work(p, g, max(group, 0), &bad);
-    if (group < 0 || row < w.q0 || row >= w.q0 + w.nq) return;         // offsets that contradict each other
-    const int tile = (row - w.q0) / g.tile_q, e = tile / 2, r = (row - w.q0 - tile * g.tile_q) * g.group + head % g.group;
-    every = e < w.twos ? 2 : 1;
-    const int64_t ordinal = (paged_ordinal_a(g, group, w.q0) + e) * p.kv_heads + kv;
-    const int2 f = g.first_a[ordinal];
-    const int first = min(max(f.x, 0), blocks - 1);
-    const int64_t place = 2 * (ordinal + first) + (every == 2 ? tile & 1 : 0);
-    na = min(max(f.y, 0), blocks - first) * (2 / every);
-    oa = g.out_a + (place * g.rows_a + r) * p.dim;
-    sa = g.sum_a + place * g.rows_a + r;
+    if (row < group0 || row >= group1) return;       // offsets that contradict each other
+    const int tile = (row - group0) / g.tile_q, tiles = (group1 - group0 + g.tile_q - 1) / g.tile_q;
+    row_a = (row - group0 - tile * g.tile_q) * g.group + head % g.group;
+    every = (tile | 1) < tiles ? 2 : 1;
+    tile_a = tile & 1;
+    ordinal_a = (paged_ordinal_a(g, sq.group, group0) + tile / 2) * p.kv_heads + kv;
   }
   {
-    const int tile = i / g.tile_q, r = (i - tile * g.tile_q) * g.group + head % g.group;
-    const int64_t ordinal = (paged_ordinal_b(g, seq, sq.q0) + tile) * p.kv_heads + kv;
-    const int2 f = g.first_b[ordinal];
-    const int first = min(max(f.x, 0), blocks - 1);
-    const int64_t place = 2 * (ordinal + first);
-    nb = min(max(f.y, 0), blocks - first) * 2;
-    ob = g.out_b + (place * g.rows_b + r) * p.dim;
-    sb = g.sum_b + place * g.rows_b + r;
+    const int q0 = g.pack > 1 ? pack0 : sq.q0, tile = g.pack > 1 ? 0 : i / g.tile_q, query = row - q0 - tile * g.tile_q;
+    if (query < 0 || query >= g.box_b) return;
+    row_b = query * g.group + head % g.group;
+    ordinal_b = (paged_ordinal_b(g, pack, q0) + tile) * p.kv_heads + kv;
   }
+  const int2 fa = sq.shared > 0 ? g.first_a[ordinal_a] : make_int2(0, 0), fb = g.first_b[ordinal_b];
+  const int first_a = min(max(fa.x, 0), blocks - 1), first_b = min(max(fb.x, 0), blocks - 1);
+  const int na = min(max(fa.y, 0), blocks - first_a) * (2 / every), nb = min(max(fb.y, 0), blocks - first_b) * 2;
+  const int64_t place_a = 2 * (ordinal_a + first_a) + (every == 2 ? tile_a : 0), place_b = 2 * (ordinal_b + first_b);
+  const float2 *sa = g.sum_a + place_a * g.rows_a + row_a, *sb = g.sum_b + place_b * g.rows_b + row_b;
+  const float *oa = g.out_a + (place_a * g.rows_a + row_a) * p.dim, *ob = g.out_b + (place_b * g.rows_b + row_b) * p.dim;
   const int64_t step_a = (int64_t)every * g.rows_a, step_b = g.rows_b;
   auto sums = [&](int k) { return k < na ? sa[k * step_a] : sb[(k - na) * step_b]; };
-  float top = -INFINITY;
-  for (int k = lane; k < na + nb; k += 32) top = fmaxf(top, sums(k).x);
+  const float2 mine = lane < na + nb ? sums(lane) : make_float2(-INFINITY, 0.f);           // the first parts, kept
+  float top = mine.x;
+  for (int k = lane + 32; k < na + nb; k += 32) top = fmaxf(top, sums(k).x);
 #pragma unroll
   for (int d = 16; d > 0; d /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
   const float ref = top == -INFINITY ? 0.f : top;
   float l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  const bool mine = 4 * lane < p.dim;
+  const bool have = 4 * lane < p.dim;
+  bool odd = false;                                  // something of its own keys' part is not finite
   for (int k0 = 0; k0 < na + nb; k0 += 32) {
     float z = 0.f;
     if (k0 + lane < na + nb) {
-      const float2 s = sums(k0 + lane);
+      const float2 s = k0 == 0 ? mine : sums(k0 + lane);
       z = s.x == -INFINITY ? 0.f : exp2f(s.x - ref);
       l = fmaf(s.y, z, l);
+      odd = odd || (k0 + lane >= na && !(fabsf(s.y) < INFINITY));
     }
-    const int n = min(32, na + nb - k0);
-    for (int k = 0; k < n; k += 4) {
-      float4 x[4];
-      float f[4];
+    // those that count, eight at a time with their loads together
+    for (uint32_t left = __ballot_sync(0xffffffffu, z != 0.f); left;) {
+      float4 x[8];
+      float f[8];
+      bool own[8];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int part = k0 + k + e;
-        f[e] = __shfl_sync(0xffffffffu, z, (k + e) & 31);
+      for (int e = 0; e < 8; ++e) {
+        const int k = left ? __ffs(left) - 1 : 0;
+        f[e] = __shfl_sync(0xffffffffu, z, k);
+        if (left == 0) f[e] = 0.f;
+        own[e] = k0 + k >= na;
         x[e] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (k + e < n && mine && f[e] != 0.f)
-          x[e] = __ldcs(reinterpret_cast<const float4*>(part < na ? oa + part * step_a * p.dim : ob + (part - na) * step_b * p.dim) + lane);
+        if (have && f[e] != 0.f)
+          x[e] = __ldcs(reinterpret_cast<const float4*>(own[e] ? ob + (k0 + k - na) * step_b * p.dim : oa + (k0 + k) * step_a * p.dim) + lane);
+        left &= left - 1;
       }
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (k + e < n) {
-          o.x = fmaf(x[e].x, f[e], o.x); o.y = fmaf(x[e].y, f[e], o.y);
-          o.z = fmaf(x[e].z, f[e], o.z); o.w = fmaf(x[e].w, f[e], o.w);
-        }
+      for (int e = 0; e < 8; ++e) {
+        o.x = fmaf(x[e].x, f[e], o.x); o.y = fmaf(x[e].y, f[e], o.y);
+        o.z = fmaf(x[e].z, f[e], o.z); o.w = fmaf(x[e].w, f[e], o.w);
+        odd = odd || (own[e] && !(fabsf(x[e].x) + fabsf(x[e].y) + fabsf(x[e].z) + fabsf(x[e].w) < INFINITY));
+      }
     }
   }
 #pragma unroll
   for (int d = 16; d > 0; d /= 2) l += __shfl_xor_sync(0xffffffffu, l, d);
   const float inv = l == 0.f ? 0.f : 1.f / l;
   o = l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-  // A weight of zero times a value that is not finite is NaN.  New rows are seen by some of a sequence's queries only, so a
-  // row that is not finite is done again, key by visible key.
-  const bool odd = mine && !(fabsf(o.x) + fabsf(o.y) + fabsf(o.z) + fabsf(o.w) < INFINITY);
-  if (sq.nq > 1 && __any_sync(0xffffffffu, odd)) {
+  // A weight of zero times a value that is not finite is NaN.  A pack's keys, and new rows, are seen by some of its queries only, so
+  // a row whose part of its own keys is not finite is done again, key by visible key; shared keys are seen by all.
+  if (__any_sync(0xffffffffu, odd)) {
     slowly();
     return;
   }
-  if (mine)
+  if (have)
     *reinterpret_cast<uint2*>(p.out.data + (int64_t)row * p.out.row_bytes + (int64_t)head * p.out.head_bytes + 8 * lane) =
         make_uint2(pack2<T>(o.x, o.y), pack2<T>(o.z, o.w));
 }

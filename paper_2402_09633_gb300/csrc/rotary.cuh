@@ -47,8 +47,7 @@ struct PagedRows {
 // The sequence that row t belongs to, the last that starts at or before it; -1 when there is none.  Looks first where
 // sequences of one length would have it.
 __device__ __forceinline__ int sequence_of(const int* start, int n_seqs, int64_t rows, int t) {
-  int a = (int)((int64_t)t * n_seqs / rows), z = n_seqs;
-  a = min(a, n_seqs - 1);
+  int a = min((int)((float)t / (float)rows * (float)n_seqs), n_seqs - 1), z = n_seqs;
   if (t >= start[a] && t < start[a + 1]) return a;
   a = 0;
 #pragma unroll 1

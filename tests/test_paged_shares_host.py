@@ -22,7 +22,7 @@ inline int64_t __shfl_up_sync(unsigned m, int64_t x, int by) {
 using namespace gnn;
 // out: own, index, item, b0, b1, first thread block, parts, ordinal, thread block, blocks, both
 extern "C" int walk(int grid, int n_q, int n_seqs, int n_groups, const int* q_start, const int* kv_len, const int* group_start,
-                    const int* shared, int max_q, int kv_heads, int group, int page, int width, long long* out, int most, unsigned* err,
+                    const int* shared, int max_q, int kv_heads, int group, int pack, int page, int width, long long* out, int most, unsigned* err,
                     long long* share_out) {
   PagedParams p = {};
   p.q_start = q_start; p.kv_len = kv_len; p.group_start = group_start; p.shared_len = shared;
@@ -30,7 +30,7 @@ extern "C" int walk(int grid, int n_q, int n_seqs, int n_groups, const int* q_st
   p.kv_heads = kv_heads; p.heads = kv_heads * group; p.err = err;
   while (1 << p.shift < page) ++p.shift;
   PagedGrid g = {};
-  g.group = group; g.tile_q = kTileQ / group; g.box = min(page, kKeys);
+  g.group = group; g.tile_q = kTileQ / group; g.box = min(page, kKeys); g.pack = pack;
   static PagedBars bars;
   int n = 0;
   gridDim.x = grid;
@@ -39,18 +39,19 @@ extern "C" int walk(int grid, int n_q, int n_seqs, int n_groups, const int* q_st
     if (threadIdx.x == 0) *share_out = share.share;
     if (threadIdx.x >= 32) return;
     bool ok = true;
-    auto part = [&](const PagedWork& w, bool own, int index, uint32_t s, int b0, int b1, int64_t u0) {
+    auto part = [&](const PagedWork& w, bool own, int index, uint32_t s, int b0, int b1, int64_t u0, const PagedOwn& mine,
+                    int prefix) {
       if (threadIdx.x != 0 || n >= most) return;
       const uint32_t e = s / kv_heads;
       const int both = e < (uint32_t)w.twos;
-      const int64_t last = u0 + (int64_t)(w.blocks - 1) * (both ? 2 : 1);
+      const int64_t last = u0 + w.blocks - 1;
       const int64_t ordinal = ((own ? paged_ordinal_b(g, index, w.q0) : paged_ordinal_a(g, index, w.q0)) + e) * kv_heads + s % kv_heads;
       const long long row[11] = {own, index, s, b0, b1, (long long)blockIdx.x, (last - share.start) / share.share + 1, ordinal,
                                  (long long)blockIdx.x, w.blocks, both};
       for (int i = 0; i < 11; ++i) out[(long long)n * 11 + i] = row[i];
       ++n;
     };
-    paged_walk(p, g, share, part, ok);
+    paged_walk(p, g, share, bars, part, ok);
   });
   return n;
 }
@@ -61,18 +62,25 @@ extern "C" int walk(int grid, int n_q, int n_seqs, int n_groups, const int* q_st
 def lib(tmp_path_factory):
     cut = host_cuda.between
     rotary, tile = host_cuda.source("rotary.cuh"), host_cuda.source("paged_tile.cuh")
-    text = "namespace gnn {\n#define INT_MAX 2147483647\nusing float_pair = float2;\n"
+    text = "namespace gnn {\n"
     text += cut(rotary, "struct HeadsView {", "struct PagedPlace {")
     text += "constexpr int kTileQ = 128, kKeys = 128, kAttendThreads = 384;\n"
     text += cut(host_cuda.source("paged.cuh"), "struct PagedParams {", "// The row of position j")
     text += cut(tile, "constexpr int kPagedCost", "// A part of an item, as")
-    text += "struct PagedBars { int64_t scan[2][12]; int64_t before; int at; };\n"
+    text += "struct PagedBars { int64_t scan[2][12]; int64_t before; int at; PagedOwn own[kPagedKept]; PagedWork shared[kGroupsKept]; };\n"
     text += cut(tile, "// Block b's share of the list", "template <typename T, int DP>\n__global__")
     lib = host_cuda.compile_host(tmp_path_factory.mktemp("host"), MAIN, [("shares.cuh", text + "}\n")])
     vp, i = ctypes.c_void_p, ctypes.c_int
-    lib.walk.argtypes = [i] * 4 + [vp] * 4 + [i] * 5 + [vp, i, vp, vp]
+    lib.walk.argtypes = [i] * 4 + [vp] * 4 + [i] * 6 + [vp, i, vp, vp]
     lib.walk.restype = i
     return lib
+
+
+def _pack(max_q, group):
+    n = 1
+    while n < 32 and 2 * n * max_q <= 128 // group:
+        n *= 2
+    return n
 
 
 def _walk(lib, grid, nq, kv_len, groups, shared, kv_heads, group, page, max_q=None, width=None, n_q=None, q_start=None):
@@ -84,20 +92,25 @@ def _walk(lib, grid, nq, kv_len, groups, shared, kv_heads, group, page, max_q=No
     out, err, share = np.zeros((400000, 11), np.int64), np.zeros(1, np.uint32), np.zeros(1, np.int64)
     at = lambda a: a.ctypes.data_as(ctypes.c_void_p)         # noqa: E731
     n = lib.walk(grid, n_q, kv_len.size, shared.size, at(q_start), at(kv_len), at(groups), at(shared),
-                 int(max(nq)) if max_q is None else max_q, kv_heads, group, page, width, at(out), len(out), at(err), at(share))
+                 int(max(nq)) if max_q is None else max_q, kv_heads, group,
+                 _pack(int(max(nq)) if max_q is None else max_q, group), page, width, at(out), len(out), at(err), at(share))
     return out[:n], int(err[0]), int(share[0]), n_q
 
 
-def _check(out, share, grid, n_q, n_seqs, n_groups, kv_heads, group):
+def _bounds(n_q, n_seqs, n_groups, kv_heads, group, pack):
     tile_q = 128 // group
-    bound = {0: (n_q // (2 * tile_q) + n_groups) * kv_heads, 1: (n_q // tile_q + n_seqs) * kv_heads}
+    return {0: (n_q // (2 * tile_q) + n_groups) * kv_heads,
+            1: (-(-n_seqs // pack) if pack > 1 else n_q // tile_q + n_seqs) * kv_heads}
+
+
+def _check(out, share, grid, bound):
     items, places, load = {}, set(), np.zeros(grid, np.int64)
     for own, index, s, b0, b1, first, parts, ordinal, block, blocks, both in out.tolist():
         assert 0 <= ordinal < bound[own] and (own, ordinal + block) not in places
         places.add((own, ordinal + block))                   # so places are below the bound and the grid
         items.setdefault((own, index, s), []).append((b0, b1, first, parts, ordinal, block, blocks))
-        load[block] += (b1 - b0) * (2 if both else 1)
-    assert load.max(initial=0) <= share + 1
+        load[block] += b1 - b0
+    assert load.max(initial=0) <= share
     for key, parts in items.items():
         parts.sort()
         assert parts[0][0] == 0 and parts[-1][1] == parts[0][6]
@@ -113,7 +126,7 @@ def test_every_block_once(lib, grid, seed):
     rng = np.random.default_rng(seed)
     n = int([1, 3, 31, 33, 385, 800][seed % 6])
     group, kv_heads, page = int(rng.choice([1, 3, 4, 32, 128])), int(rng.integers(1, 5)), int(rng.choice([16, 64, 128, 1024]))
-    nq = rng.integers(0, 4, n) if seed % 2 else np.ones(n, int)
+    nq = rng.integers(0, [4, 4, 40, 300][seed % 4], n) if seed % 2 or seed == 10 else np.ones(n, int)
     nq[0] = max(nq[0], 1)
     cuts = np.sort(rng.integers(0, n + 1, int(rng.integers(1, 6)))) if seed % 3 else np.array([0, n])
     shared = rng.integers(0, 5000, len(cuts) - 1)
@@ -125,17 +138,20 @@ def test_every_block_once(lib, grid, seed):
     kv_len = part + own
     out, err, share, n_q = _walk(lib, grid, nq, kv_len, cuts, shared, kv_heads, group, page)
     assert err == 0
-    items = _check(out, share, grid, n_q, n, len(shared), kv_heads, group)
-    tile_q, box = 128 // group, min(page, 128)
+    pack = _pack(int(max(nq)), group)
+    items = _check(out, share, grid, _bounds(n_q, n, len(shared), kv_heads, group, pack))
+    tile_q = 128 // group
     want = {}
     for g, s in enumerate(shared):
         tiles = -(-int(nq[cuts[g]:cuts[g + 1]].sum()) // tile_q)
         for i in range((tiles + 1) // 2 * kv_heads if s else 0):
             want[0, g, i] = -(-int(s) // 128)
-    for b in range(n):
-        base = part[b] // box * box
-        for i in range(-(-int(nq[b]) // tile_q) * kv_heads):
-            want[1, b, i] = -(-int(kv_len[b] - base) // 128)
+    pieces = np.where(nq > 0, -(-(kv_len - part // 16 * 16) // 16), 0)
+    for k in range(-(-n // pack)):
+        mine = slice(k * pack, (k + 1) * pack)
+        tiles = 1 if pack > 1 and nq[mine].sum() else -(-int(nq[mine].sum()) // tile_q)
+        for i in range(tiles * kv_heads):
+            want[1, k, i] = -(-int(pieces[mine].sum()) // 8)
     assert {k: v[0][6] for k, v in items.items()} == {k: v for k, v in want.items() if v > 0}
 
 
@@ -148,7 +164,7 @@ def test_offsets_that_contradict_each_other_stay_inside(lib, bad):
     assert _walk(lib, 13, **a)[1] == 0
     out, err, share, n_q = _walk(lib, 13, **{**a, **bad})
     assert err == 1
-    bound = {0: (12 // 64 + 2) * 2, 1: (12 // 32 + 4) * 2}
+    bound = _bounds(12, 4, 2, 2, 4, _pack(bad.get("max_q", 3), 4))
     assert all(0 <= r[7] < bound[r[0]] and r[3] < r[4] for r in out.tolist())
 
 
