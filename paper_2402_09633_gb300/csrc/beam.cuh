@@ -4,19 +4,20 @@
 // of a group in order, ties to the lowest b * vocab + t.  A hypothesis that has ended has one continuation, its score.
 //
 // Within a row the order is that of x, so one pass over the logits finds a row's candidates beside its sum: a warp has a
-// stretch of a row, a running maximum and sum to a lane, and a list of the elements above the stretch's best-th so far, with
-// no barrier between warps until the end.  A second kernel joins the lists row by row, then the rows by value in 64 bits,
+// stretch of a row, a running maximum and sum to a lane, and a sorted list of its best so far in registers; elements
+// below the list's last, or below what the block's lists bound the best by, cost a comparison.  A second kernel joins the lists row by row, then the rows by value in 64 bits,
 // so that rounding neither makes nor breaks ties.  Bound by HBM: logits are read once.
 #pragma once
 #include "attend_ptx.cuh"
+#include <cfloat>
 #include "rotary.cuh"
 
 namespace gnn {
 
 constexpr int kBeamMost = 64;        // hypotheses of a group, and continuations that are kept
-constexpr int kStripThreads = 256;
+constexpr float kLog2e = 1.44269504f;
+constexpr int kStripThreads = 256, kStripBlocks = 4;         // and blocks to an SM
 constexpr int kStripsMost = 32;      // strips of a row: one to a lane of the warp that joins them
-constexpr int kWarpBuffer = 128;     // keys that a warp collects before it keeps the best
 
 struct alignas(16) BeamSum { double s; float r; };    // the sum of 2^(x log2 e - r) over a strip
 struct BeamParams {
@@ -69,67 +70,80 @@ __device__ __forceinline__ int above(const uint64_t* list, int n, uint64_t k) {
   return a;
 }
 
-// A warp's best keys so far.
-struct WarpList {
-  uint64_t* buf;                     // [kWarpBuffer], the warp's own
-  int have;
-  float tau;                         // later elements count only above it
-};
+// A warp's best keys in falling order: place `lane` and, above 32 of them, place 32 + lane.
+struct WarpList { uint64_t a, z; };
 
-// Leaves the best keys in order, and the threshold at the last of them.  Keys differ: a key's place is how many are larger.
-template <int SLOTS>
-__device__ __forceinline__ void warp_rank(WarpList& l, int best) {
-  const int lane = threadIdx.x & 31;
-  uint64_t k[SLOTS];
-  int rank[SLOTS];
-#pragma unroll
-  for (int i = 0; i < SLOTS; ++i) {
-    k[i] = lane + 32 * i < l.have ? l.buf[lane + 32 * i] : 0;
-    rank[i] = 0;
-  }
-#pragma unroll 4
-  for (int j = 0; j < l.have; ++j) {
-    const uint64_t y = l.buf[j];
-#pragma unroll
-    for (int i = 0; i < SLOTS; ++i) rank[i] += y > k[i];
-  }
-  __syncwarp();
-#pragma unroll
-  for (int i = 0; i < SLOTS; ++i)
-    if (lane + 32 * i < l.have && rank[i] < best) l.buf[rank[i]] = k[i];
+__device__ __forceinline__ uint64_t exchange(uint64_t k, int d, bool larger) {
+  const uint64_t y = __shfl_xor_sync(0xffffffffu, k, d);
+  return (y > k) == larger ? y : k;
 }
-__device__ __noinline__ void warp_prune(WarpList& l, int best) {
-  __syncwarp();
-  if (l.have <= 32) warp_rank<1>(l, best); else warp_rank<kWarpBuffer / 32>(l, best);
-  __syncwarp();
-  l.have = min(l.have, best);
-  if (l.have == best) l.tau = unordered((uint32_t)(l.buf[best - 1] >> 32));
+// Keys that rise and then fall over the lanes, or the reverse, in falling order.
+__device__ __forceinline__ uint64_t merge_lanes(uint64_t k) {
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) k = exchange(k, d, (threadIdx.x & d) == 0);
+  return k;
+}
+// A key of every lane in falling order.  (A bitonic network: Batcher 1968.)
+__device__ __forceinline__ uint64_t sort_lanes(uint64_t k) {
+#pragma unroll
+  for (int n = 2; n <= 32; n *= 2)
+#pragma unroll
+    for (int d = n / 2; d > 0; d >>= 1) k = exchange(k, d, ((threadIdx.x & d) == 0) == ((threadIdx.x & n & 31) == 0));
+  return k;
+}
+// The best of a list and of a key of every lane (0: none).
+__device__ __forceinline__ void take_lanes(WarpList& l, uint64_t k, int best) {
+  k = __shfl_xor_sync(0xffffffffu, sort_lanes(k), 31);               // rising
+  if (best > 32) {
+    const uint64_t y = __shfl_xor_sync(0xffffffffu, merge_lanes(max(l.z, k)), 31);
+    const uint64_t hi = max(l.a, y), lo = min(l.a, y);
+    l.a = merge_lanes(hi);
+    l.z = merge_lanes(lo);
+  } else {
+    l.a = merge_lanes(max(l.a, k));
+  }
+}
+// The same for one key that all lanes know.
+__device__ __forceinline__ void take_one(WarpList& l, uint64_t k, int best) {
+  const int lane = threadIdx.x & 31;
+  if (best > 32) {
+    const uint64_t down = min(k, __shfl_sync(0xffffffffu, l.a, 31));  // what goes past the first 32 places
+    const int at = __popc(__ballot_sync(0xffffffffu, l.z > down));
+    const uint64_t up = __shfl_up_sync(0xffffffffu, l.z, 1);
+    l.z = lane < at ? l.z : lane == at ? down : up;
+  }
+  const int at = __popc(__ballot_sync(0xffffffffu, l.a > k));
+  const uint64_t up = __shfl_up_sync(0xffffffffu, l.a, 1);
+  l.a = lane < at ? l.a : lane == at ? k : up;
+}
+__device__ __forceinline__ uint64_t list_at(const WarpList& l, int i) {
+  return __shfl_sync(0xffffffffu, i < 32 ? l.a : l.z, i & 31);
 }
 
 // 2^n for a whole number that is not positive, exactly; zero where that is below what floats hold.
 __device__ __forceinline__ float power2(float n) { return n < -126.f ? 0.f : __int_as_float(((int)n + 127) << 23); }
 
-constexpr int kStripPieces = 4;      // of 16 bytes, that a lane takes at a time
-constexpr int kStripStages = 3;
-constexpr int kStripStage = (32 * kStripPieces + 1) * 16;       // and the one that rows which start between two reach into
-constexpr int kStripSmem = kStripThreads / 32 * kStripStages * kStripStage;
+constexpr int kLaneElements = 16;    // that a lane takes at a time
+template <typename T> constexpr int strip_stages() { return sizeof(T) == 4 ? 3 : 4; }            // what lets four blocks share an SM
+template <typename T> constexpr int strip_pieces() { return kLaneElements * (int)sizeof(T) / 16; }                // of 16 bytes
+template <typename T> constexpr int strip_stage() { return (32 * strip_pieces<T>() + 1) * 16; }    // and the one that rows which start between two reach into
+template <typename T> constexpr int strip_smem() { return kStripThreads / 32 * strip_stages<T>() * strip_stage<T>(); }
 
 template <typename T>
-__global__ void __launch_bounds__(kStripThreads, 3) beam_strip_kernel(const __grid_constant__ BeamParams p) {
-  constexpr int VEC = 16 / sizeof(T), P = kStripPieces, N = P * VEC, WARPS = kStripThreads / 32;     // elements of a piece, of a lane at a time
-  // log2 e in two pieces: the logarithm of a row's sum is to be good to 10^-8 or so, as rows' values are compared with each
-  // other.  Sums are relative to 2^r with a whole number r, so that joining them rounds nothing.
-  constexpr float kHi = 1.44269504f, kLo = (float)(1.4426950408889634 - (double)1.44269504f);
-  extern __shared__ __align__(16) uint8_t strip_smem[];
-  __shared__ uint64_t buf_s[WARPS][kWarpBuffer];
+__global__ void __launch_bounds__(kStripThreads, kStripBlocks) beam_strip_kernel(const __grid_constant__ BeamParams p) {
+  constexpr int VEC = 16 / sizeof(T), P = strip_pieces<T>(), N = kLaneElements, WARPS = kStripThreads / 32, STAGE = strip_stage<T>(), STAGES = strip_stages<T>();
+  // Sums are of 2^(c x - r) with c = log2 e rounded, and their logarithm is divided by c again: that leaves 1.3e-8 of the weights'
+  // entropy as an error, where c is off by 1.3e-8.  r is a whole number, so that joining sums rounds nothing.
+  extern __shared__ __align__(16) uint8_t strip_ring[];
+  __shared__ uint64_t list_s[WARPS][kBeamMost];
   __shared__ float high_s[WARPS];
   __shared__ double sum_s[WARPS];
-  __shared__ int have_s[WARPS], count_s[WARPS];
-  __shared__ unsigned tau_s;                         // the highest of the warps' thresholds, as it is ordered
+  __shared__ int have_s[WARPS];
+  __shared__ unsigned bound_s[WARPS];                // of each warp's list, the value at place best / 8, as it is ordered
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, best = p.best;
   const int row = p.strips == 1 ? (int)blockIdx.x : (int)(blockIdx.x / (unsigned)p.strips);
   const int strip = (int)blockIdx.x - row * p.strips;
-  if (tid == 0) tau_s = 0;
+  if (tid < WARPS) bound_s[tid] = 0;
   __syncthreads();
   pdl_wait();
   pdl_trigger();
@@ -137,54 +151,68 @@ __global__ void __launch_bounds__(kStripThreads, 3) beam_strip_kernel(const __gr
   const T* x = static_cast<const T*>(p.x) + row * p.stride;
   // Pieces by the elements' numbers: rows that hold the same have the same sum to the last bit, wherever in memory they start, so
   // that values which are equal compare so.  Those below `whole`, and not the first of a row that starts between two, come through
-  // shared memory, kStripStages rounds ahead of their use; the others element by element.
+  // shared memory, STAGES rounds ahead of their use; the others element by element.
   const int skew = (int)((uintptr_t)x / sizeof(T) % VEC), bytes = skew * (int)sizeof(T), vocab = p.vocab;
   const int pieces = (vocab + VEC - 1) / VEC, whole = skew == 0 ? vocab / VEC : (vocab + skew) / VEC - 1;
   const int per = (pieces + p.strips * WARPS - 1) / (p.strips * WARPS), p0 = min(pieces, (strip * WARPS + warp) * per),
             p1 = min(pieces, p0 + per);
   const uint4* wide = reinterpret_cast<const uint4*>(x - skew);
-  uint8_t* ring = strip_smem + warp * kStripStages * kStripStage;
+  uint8_t* ring = strip_ring + warp * STAGES * STAGE;
   // 16 bytes that lie in the row whole: pieces of memory first .. last - 1
   const int first = skew ? 1 : 0, last = (int)(((int64_t)vocab + skew) / VEC);
+  const int inside_fetch = min(last, p1 + 1) - 32 * P - 1, inside = min(p1, whole) - 32 * P;         // rounds up to these need no look at ends
+  const uint4* lane_wide = wide + lane;
+  const uint32_t lane_ring = smem_u32(ring) + lane * 16;
+  auto copy = [](uint32_t to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); };
   auto fetch = [&](int c0, int stage) {              // pieces of memory c0 .. c0 + 32 P
-    uint8_t* to = ring + stage * kStripStage;
-    if (c0 < p1) {
+    const uint32_t to = lane_ring + stage * STAGE;
+    if (c0 >= first && c0 <= inside_fetch) {
 #pragma unroll
+      for (int h = 0; h < P; ++h) copy(to + h * 512, lane_wide + c0 + h * 32);
+      if (skew && lane == 0) copy(to + P * 512, lane_wide + c0 + P * 32);
+    } else if (c0 < p1) {
+#pragma unroll 1
       for (int h = 0; h <= P; ++h) {
         const int i = h * 32 + lane, at = c0 + i;
-        if (i <= 32 * P && at >= first && at < last && at <= p1)
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to + i * 16)), "l"(wide + at) : "memory");
+        if (i <= 32 * P && at >= first && at < last && at <= p1) copy(to + h * 512, lane_wide + c0 + h * 32);
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
 
   float m = -INFINITY, r = 0.f, s = 0.f;
-  WarpList list = {buf_s[warp], 0, -INFINITY};
-  const int spare = kWarpBuffer - 32;                // keys that leave room for those of another element of all lanes
-  const int enough = min(spare, max(32, 2 * best));  // keys from which on a new threshold is worth its price
-  volatile unsigned* shared_tau = &tau_s;
+  WarpList list = {0, 0};
+  float tau = -INFINITY;                             // of the list's last, once it is full
+  const int deep = (best + WARPS - 1) / WARPS - 1;
+  volatile unsigned* bounds = bound_s;
 #pragma unroll
-  for (int k = 0; k < kStripStages - 1; ++k) fetch(p0 + k * 32 * P, k);
+  for (int k = 0; k < STAGES - 1; ++k) fetch(p0 + k * 32 * P, k);
+  if (p0 >= p1) __syncthreads();                     // that of the others' first round; a warp without elements bounds nothing
   int stage = 0;
   for (int c0 = p0; c0 < p1; c0 += 32 * P) {
-    asm volatile("cp.async.wait_group %0;" ::"n"(kStripStages - 2) : "memory");
+    asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
     __syncwarp();                                    // what lies in the stage, and that the one before has been read
-    fetch(c0 + (kStripStages - 1) * 32 * P, stage == 0 ? kStripStages - 1 : stage - 1);
+    fetch(c0 + (STAGES - 1) * 32 * P, stage == 0 ? STAGES - 1 : stage - 1);
     float v[N];
     {
-      const uint8_t* from = ring + stage * kStripStage;
-      stage = stage + 1 == kStripStages ? 0 : stage + 1;
+      const uint8_t* from = ring + stage * STAGE;
+      stage = stage + 1 == STAGES ? 0 : stage + 1;
+      const uint4* at = reinterpret_cast<const uint4*>(from) + lane;
+      const bool all = c0 >= first && c0 <= inside;
 #pragma unroll
       for (int h = 0; h < P; ++h) {
-        const int piece = c0 + h * 32 + lane;
         Pack<T, VEC> k;
-        if (piece < min(p1, whole) && piece >= first) {
-          const uint4* at = reinterpret_cast<const uint4*>(from) + h * 32 + lane;
-          *reinterpret_cast<uint4*>(&k) = skew == 0 ? *at : load_skewed(at, bytes);
+        const int piece = c0 + h * 32 + lane;
+        if (all || (piece < min(p1, whole) && piece >= first)) {
+          *reinterpret_cast<uint4*>(&k) = skew == 0 ? at[h * 32] : load_skewed(at + h * 32, bytes);
         } else {
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) k.v[e] = piece < p1 && (int64_t)piece * VEC + e < vocab ? x[(int64_t)piece * VEC + e] : from_f<T>(-INFINITY);
+          for (int e = 0; e < VEC; ++e) k.v[e] = from_f<T>(-INFINITY);
+          if (piece < p1) {                          // a row's first or last
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+              if ((int64_t)piece * VEC + e < vocab) k.v[e] = x[(int64_t)piece * VEC + e];
+          }
         }
 #pragma unroll
         for (int e = 0; e < VEC; ++e) v[h * VEC + e] = to_f(k.v[e]);
@@ -195,7 +223,7 @@ __global__ void __launch_bounds__(kStripThreads, 3) beam_strip_kernel(const __gr
     for (int e = 1; e + 1 < N; e += 2) high = max3(high, v[e], v[e + 1]);
     high = fmaxf(high, v[N - 1]);
     if (high > m) {
-      const float to = ceilf(high * kHi);
+      const float to = ceilf(high * kLog2e);
       if (m > -INFINITY) s *= power2(r - to);
       m = high;
       r = to;
@@ -204,86 +232,81 @@ __global__ void __launch_bounds__(kStripThreads, 3) beam_strip_kernel(const __gr
 #pragma unroll
     for (int e = 0; e < N; e += 2) {
       const float2 y = make_float2(v[e], v[e + 1]);
-      const float2 z = __ffma2_rn(y, make_float2(kLo, kLo), __ffma2_rn(y, make_float2(kHi, kHi), make_float2(-r, -r)));
+      const float2 z = __ffma2_rn(y, make_float2(kLog2e, kLog2e), make_float2(-r, -r));
       sum[e >> 1 & 1] = __fadd2_rn(sum[e >> 1 & 1], make_float2(exp2_approx(z.x), exp2_approx(z.y)));
     }
     s += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-    // candidates: later elements of the same value as the threshold lose the tie
-    if (!__any_sync(0xffffffffu, high > list.tau)) continue;
-    // of these elements, those above the threshold and from here on: another warp's threshold bounds the block's best from
-    // below too, but elements equal to it may have lower numbers than that warp's
-    const unsigned theirs = *shared_tau;
-    float from = theirs ? unordered(theirs) : -INFINITY;
-    if (!__any_sync(0xffffffffu, high >= from)) continue;
-    if (list.tau == -INFINITY && theirs == 0) {
-      // at first as many lanes' largest elements bound the best from below, or all lanes' two largest
-      if (best <= 32) {
-        int rank = 0;
+    // Candidates: above the list's last (later elements of the same value lose the tie), and not below what the block's lists
+    // hold together: all warps' elements at place best / 8 and before are `best` at least.
+    auto bound = [&] {
+      const unsigned all = __reduce_min_sync(0xffffffffu, bounds[lane % WARPS]);
+      // one comparison for both: the next float above the list's last, or the bound
+      return fmaxf(all ? unordered(all) : -FLT_MAX, tau == -INFINITY ? -FLT_MAX : unordered(ordered(tau) + 1));
+    };
+    auto key = [&](int i, bool in) {
+      return in ? beam_key(high, (uint32_t)((c0 + i / VEC * 32 + lane) * VEC + i % VEC)) : 0;
+    };
+    int e = 0;
+    auto first_of_high = [&] {                       // the first element of the lane's largest value
+      e = N - 1;
 #pragma unroll
-        for (int d = 0; d < 32; ++d) {
-          const float y = __shfl_sync(0xffffffffu, high, d);
-          rank += y > high || (y == high && d < lane);
-        }
-        from = __shfl_sync(0xffffffffu, high, __ffs(__ballot_sync(0xffffffffu, rank == best - 1)) - 1);
-      } else {
-        float a = -INFINITY, z = -INFINITY;
+      for (int i = N - 2; i >= 0; --i) e = v[i] == high ? i : e;
+    };
+    auto without = [&] {                             // the lane's largest without it
+      float next = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-          z = fmaxf(z, fminf(a, v[e]));
-          a = fmaxf(a, v[e]);
-        }
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1) z = fminf(z, __shfl_xor_sync(0xffffffffu, z, d));
-        from = z;
+      for (int i = 0; i < N; ++i) {
+        v[i] = i == e ? -INFINITY : v[i];
+        next = fmaxf(next, v[i]);
       }
+      high = next;
+    };
+    float least = -FLT_MAX;
+    if (c0 == p0) {
+      // At first the lanes' largest elements, and a bound from all warps'.
+      first_of_high();
+      take_lanes(list, key(e, high > -INFINITY), best);
+      const uint64_t place = list_at(list, deep);
+      if (lane == 0) bounds[warp] = (unsigned)(place >> 32);
+      __syncthreads();
+      least = bound();
+      without();
+    } else {
+      if (!__any_sync(0xffffffffu, high > tau)) continue;
+      least = bound();
     }
-    auto count = [&] {
-      int n = 0;
+    bool some = high >= least;
+    uint32_t who = __ballot_sync(0xffffffffu, some);
+    if (who == 0 && c0 != p0) continue;
+    // Each lane's candidates.  Mostly some lane has one: then that is all.
+    int n = 0;
 #pragma unroll
-      for (int e = 0; e < N; ++e) n += v[e] > list.tau && v[e] >= from;
-      return n;
-    };
-    auto append = [&](int at) {                      // in any order: keys differ
-#pragma unroll
-      for (int h = 0; h < P; ++h)
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          const float y = v[h * VEC + e];
-          if (y > list.tau && y >= from) list.buf[at++] = beam_key(y, (uint32_t)((c0 + h * 32 + lane) * VEC + e));
-        }
-    };
-    const int mine = count(), more = __reduce_add_sync(0xffffffffu, mine);
-    if (list.have + more <= kWarpBuffer) {
-      if (lane == 0) count_s[warp] = list.have;
-      __syncwarp();
-      if (mine) append(atomicAdd(&count_s[warp], mine));
-      list.have += more;
-    } else {                                         // rows that rise, or are all the same: lane by lane
+    for (int i = 0; i < N; ++i) {
+      const bool in = v[i] >= least;
+      e = in ? i : e;
+      n += in;
+    }
+    if (__popc(who) <= 6 && !__any_sync(0xffffffffu, n > 1)) {
+      const uint64_t k = key(e, some);
+      for (uint32_t x = who; x; x &= x - 1) take_one(list, __shfl_sync(0xffffffffu, k, __ffs(x) - 1), best);
+    } else {
 #pragma unroll 1
-      for (int d = 0; d < 32; ++d) {
-        const int now = __shfl_sync(0xffffffffu, count(), d);
-        if (now == 0) continue;
-        if (list.have > spare) {
-          // The threshold is of elements with any numbers then: what is left of this round counts from it on.
-          const float before = list.tau;
-          warp_prune(list, best);
-          from = fmaxf(from, list.tau);
-          list.tau = before;
-          --d;
-          continue;
-        }
-        if (lane == d) append(list.have);
-        list.have += now;
+      for (; who; who = __ballot_sync(0xffffffffu, some)) {
+        first_of_high();
+        take_lanes(list, key(e, some), best);
+        const uint64_t last = list_at(list, best - 1);
+        if (last) least = fmaxf(least, unordered((uint32_t)(last >> 32)));
+        without();
+        some = high >= least;
       }
     }
-    __syncwarp();
-    if (list.have >= enough || (list.tau == -INFINITY && list.have >= best)) {
-      warp_prune(list, best);
-      if (lane == 0 && list.have == best) atomicMax(&tau_s, ordered(list.tau));
-    }
+    const uint64_t end = list_at(list, best - 1);
+    if (end) tau = unordered((uint32_t)(end >> 32));
+    const uint64_t place = list_at(list, deep);
+    if (lane == 0 && place) bounds[warp] = (unsigned)(place >> 32);
   }
-  warp_prune(list, best);
-  if (lane == 0) have_s[warp] = list.have;
+  if (lane < best) list_s[warp][lane] = list.a;
+  if (lane + 32 < best) list_s[warp][lane + 32] = list.z;
   // the threads' sums
   float high = m == -INFINITY ? -INFINITY : r;
 #pragma unroll
@@ -300,19 +323,24 @@ __global__ void __launch_bounds__(kStripThreads, 3) beam_strip_kernel(const __gr
   if (lane == 0) sum_s[warp] = sum;
   // the warps' lists: a key's place is its own and what the others have above it
   uint64_t* out = p.lists + (int64_t)blockIdx.x * best;
-  int all = 0;
-#pragma unroll
-  for (int w = 0; w < WARPS; ++w) all += have_s[w];
-  for (int i = lane; i < list.have; i += 32) {
-    const uint64_t k = list.buf[i];
+  int taken = 0;
+  for (int i = lane; i < best; i += 32) {
+    const uint64_t k = list_s[warp][i];
+    if (k == 0) break;
     int rank = i;
 #pragma unroll
     for (int w = 0; w < WARPS; ++w)
-      if (w != warp) rank += above(buf_s[w], have_s[w], k);
+      if (w != warp) rank += above(list_s[w], best, k);
     if (rank < best) out[rank] = k;
+    ++taken;
   }
-  for (int i = all + tid; i < best; i += kStripThreads) out[i] = 0;
+  taken = __reduce_add_sync(0xffffffffu, taken);
+  if (lane == 0) have_s[warp] = taken;
   __syncthreads();
+  int taken_all = 0;
+#pragma unroll
+  for (int w = 0; w < WARPS; ++w) taken_all += have_s[w];
+  for (int i = taken_all + tid; i < best; i += kStripThreads) out[i] = 0;
   if (tid == 0) {
     for (int w = 1; w < WARPS; ++w) sum += sum_s[w];
     p.sums[blockIdx.x] = {sum, high};
@@ -320,66 +348,74 @@ __global__ void __launch_bounds__(kStripThreads, 3) beam_strip_kernel(const __gr
 }
 
 constexpr int kJoinThreads = 256;
+constexpr int kJoinKeys = 8192;      // of strips' lists that are looked at together
+constexpr int kJoinFew = 512;        // candidates that are compared with each other
+
+// Hypotheses whose strips' lists are looked at together.
+__host__ __device__ constexpr int join_rows(int beams, int strips, int best) {
+  const int n = kJoinKeys / (strips * best);
+  return n < 1 ? 1 : n < beams ? n : beams;
+}
+__host__ __device__ constexpr int join_smem(int beams, int strips, int best) {
+  return 16 * beams * best + 16 * beams * strips + 8 * join_rows(beams, strips, best) * strips * best;
+}
 
 // One group to a block: first the strips of every row, then the rows, each time a candidate's place being how many of the
-// other lists' are before it.
+// other lists' are before it.  Bound by its chain of steps: what a step needs from memory is fetched at once, and only candidates that
+// some `best` are not known to beat look for their place.
 __global__ void __launch_bounds__(kJoinThreads) beam_join_kernel(const __grid_constant__ BeamParams p) {
-  extern __shared__ __align__(16) uint64_t join_smem[];
-  __shared__ double base_s[kBeamMost];               // a row's sum; then what is added to a logit
-  __shared__ float top_s[kBeamMost];
-  __shared__ int taken_s;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, best = p.best, beams = p.beams, strips = p.strips;
+  extern __shared__ __align__(16) uint64_t join_keys[];
+  __shared__ double base_s[kBeamMost];               // what is added to a logit
+  __shared__ int taken_s, left_s, few_s[kJoinFew], reach_s[kBeamMost];
+  const int tid = threadIdx.x, best = p.best, beams = p.beams, strips = p.strips, per = strips * best;
   const int64_t group = blockIdx.x, row0 = group * beams;
-  uint64_t* rows = join_smem;                        // [beams][best]
+  BeamSum* sums = reinterpret_cast<BeamSum*>(join_keys);                         // [beams][strips]
+  uint64_t* rows = reinterpret_cast<uint64_t*>(sums + beams * strips);           // [beams][best]
   uint64_t* values = rows + beams * best;            // the same, as they are ordered: comparing 64-bit floats takes long here
-  uint64_t* lists = values + beams * best;           // [warps][strips][best]
-  if (tid == 0) taken_s = 0;
+  uint64_t* lists = values + beams * best;           // [join_rows][strips][best]
+  const int together = join_rows(beams, strips, best);
+  if (tid == 0) taken_s = left_s = 0;
+  if (tid < kBeamMost) reach_s[tid] = 0;
   pdl_wait();
-  for (int b = warp; b < beams; b += kJoinThreads / 32) {
-    const int64_t row = row0 + b;
-    const bool ended = p.ended && p.ended[row];
-    uint64_t* mine = rows + b * best;
-    if (ended) {
-      for (int i = lane; i < best; i += 32) mine[i] = i == 0 ? beam_key(0.f, (uint32_t)p.end) : 0;
-      if (lane == 0) {
-        base_s[b] = 1.;
-        top_s[b] = 0.f;
-      }
-    } else {
-      const BeamSum part = lane < strips ? p.sums[row * strips + lane] : BeamSum{0., -INFINITY};
-      const uint64_t* from = p.lists + row * strips * best;
-      uint64_t* to = strips == 1 ? mine : lists + warp * strips * best;
-      for (int i = lane; i < strips * best; i += 32) to[i] = from[i];
-      float top = part.r;
-#pragma unroll
-      for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-      double sum = part.s == 0. ? 0. : part.s * (double)power2(part.r - (top == -INFINITY ? 0.f : top));
-#pragma unroll
-      for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-      if (lane == 0) {
-        base_s[b] = sum;
-        top_s[b] = top;
-      }
-      __syncwarp();
-      if (strips > 1) {
-        for (int i = lane; i < best; i += 32) mine[i] = 0;
-        __syncwarp();
-        for (int i = lane; i < strips * best; i += 32) {
-          const uint64_t k = to[i];
-          if (k == 0) continue;
-          const int s = i / best;
-          int rank = i - s * best;
-          for (int t = 0; t < strips && rank < best; ++t)
-            if (t != s) rank += above(to + t * best, best, k);
-          if (rank < best) mine[rank] = k;
-        }
-        __syncwarp();
-      }
+  for (int i = tid; i < beams * strips; i += kJoinThreads) sums[i] = p.sums[row0 * strips + i];
+  for (int b0 = 0; b0 < beams; b0 += together) {
+    const int n = min(together, beams - b0);
+    uint64_t* to = strips == 1 ? rows + b0 * best : lists;
+    const uint64_t* from = p.lists + (row0 + b0) * per;
+#pragma unroll 4
+    for (int i = tid; i < n * per; i += kJoinThreads) to[i] = from[i];
+    if (strips == 1) continue;
+    for (int i = tid; i < n * best; i += kJoinThreads) rows[b0 * best + i] = 0;
+    __syncthreads();
+    for (int i = tid; i < n * per; i += kJoinThreads) {
+      const uint64_t k = lists[i];
+      if (k == 0) continue;
+      const int row = i / per, s = (i - row * per) / best;
+      int rank = i - row * per - s * best;
+      for (int t = 0; t < strips && rank < best; ++t)
+        if (t != s) rank += above(lists + row * per + t * best, best, k);
+      if (rank < best) rows[(b0 + row) * best + rank] = k;
     }
+    __syncthreads();
   }
   __syncthreads();
   // 64-bit arithmetic is slow here: one logarithm for all rows
-  if (tid < beams) base_s[tid] = (double)p.score[row0 + tid] - ((double)top_s[tid] + log2(base_s[tid])) * 0.6931471805599453;
+  if (tid < beams) {
+    const float score = p.score[row0 + tid];
+    if (p.ended && p.ended[row0 + tid]) {
+      for (int i = 0; i < best; ++i) rows[tid * best + i] = i == 0 ? beam_key(0.f, (uint32_t)p.end) : 0;
+      base_s[tid] = (double)score;
+    } else {
+      float top = -INFINITY;
+      for (int s = 0; s < strips; ++s) top = fmaxf(top, sums[tid * strips + s].r);
+      double sum = 0.;
+      for (int s = 0; s < strips; ++s) {
+        const BeamSum part = sums[tid * strips + s];
+        if (part.s != 0.) sum += part.s * (double)power2(part.r - (top == -INFINITY ? 0.f : top));
+      }
+      base_s[tid] = (double)score - ((double)top + log2(sum)) * (1. / (double)kLog2e);
+    }
+  }
   __syncthreads();
   for (int i = tid; i < beams * best; i += kJoinThreads) {
     const uint64_t k = rows[i];
@@ -388,30 +424,82 @@ __global__ void __launch_bounds__(kJoinThreads) beam_join_kernel(const __grid_co
     values[i] = !(v > -INFINITY) ? 0 : u >> 63 ? ~u : u | 1ull << 63;        // 0: none, or NaN
   }
   __syncthreads();
-  int taken = 0;
-  for (int i = tid; i < beams * best; i += kJoinThreads) {
-    const uint64_t v = values[i];
-    if (v == 0) continue;
-    const int b = i / best;
-    int rank = i - b * best;
-    for (int c = 0; c < beams && rank < best; ++c) {
-      if (c == b) continue;
-      const uint64_t* list = values + c * best;      // falling; of equal values those of lower rows come first
-      int a = 0, z = best;
-      while (a < z) {
-        const int mid = (a + z) / 2;
-        if (c < b ? list[mid] >= v : list[mid] > v) a = mid + 1; else z = mid;
-      }
-      rank += a;
+  // What is not wanted: below the largest of the rows' first values that `best` values reach, or below the rows' least at place
+  // best / beams, as those and what is before them are `best`.
+  for (int i = tid; i < beams * beams; i += kJoinThreads) {
+    const int b = i / beams, c = i - b * beams;
+    const uint64_t v = values[b * best];
+    if (v) atomicAdd(&reach_s[b], above(values + c * best, best, v - 1));
+  }
+  __syncthreads();
+  const int deep = (best + beams - 1) / beams - 1, lane = tid & 31;
+  uint64_t least = ~0ull, first = 0;
+  for (int b = lane; b < beams; b += 32) {
+    least = min(least, values[b * best + deep]);
+    if (reach_s[b] >= best) first = max(first, values[b * best]);
+  }
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) {
+    least = min(least, __shfl_xor_sync(0xffffffffu, least, d));
+    first = max(first, __shfl_xor_sync(0xffffffffu, first, d));
+  }
+  least = max(least, first);
+  for (int i = tid; i < beams * best; i += kJoinThreads)
+    if (values[i] != 0 && values[i] >= least) {
+      const int at = atomicAdd(&left_s, 1);
+      if (at < kJoinFew) few_s[at] = i;
     }
-    if (rank >= best) continue;
+  __syncthreads();
+  const int left = left_s;
+  int taken = 0;
+  auto put = [&](int i, int rank) {
     const int64_t o = group * best + rank;
+    const uint64_t v = values[i];
     p.out_score[o] = (float)__longlong_as_double((long long)(v >> 63 ? v & ~(1ull << 63) : ~v));
-    p.out_parent[o] = b;
+    p.out_parent[o] = i / best;
     p.out_token[o] = (int)~(uint32_t)rows[i];
     ++taken;
+  };
+  if (left <= kJoinFew) {                            // few: each is compared with all
+    for (int x = tid; x < left; x += kJoinThreads) {
+      const int i = few_s[x];
+      const uint64_t v = values[i];
+      int rank = 0;
+#pragma unroll 4
+      for (int y = 0; y < left; ++y) {
+        const int j = few_s[y];
+        const uint64_t u = values[j];
+        rank += u > v || (u == v && j < i);
+      }
+      if (rank < best) put(i, rank);
+    }
+  } else {
+    int steps = 1;
+    while (1 << steps <= best) ++steps;
+    for (int i = tid; i < beams * best; i += kJoinThreads) {
+      const uint64_t v = values[i];
+      if (v == 0 || v < least) continue;
+      const int b = i / best;
+      int rank = i - b * best;
+      for (int c0 = 0; c0 < beams && rank < best; c0 += 4) {
+        // four lists side by side: falling; of equal values those of lower rows come first
+        int a[4] = {0, 0, 0, 0}, z[4] = {best, best, best, best};
+        for (int s = 0; s < steps; ++s)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const int c = min(c0 + x, beams - 1), mid = (a[x] + z[x]) / 2;
+            const uint64_t y = values[c * best + min(mid, best - 1)];
+            const bool before = a[x] < z[x] && (c < b ? y >= v : y > v);
+            a[x] = before ? mid + 1 : a[x];
+            z[x] = before ? z[x] : mid;
+          }
+#pragma unroll
+        for (int x = 0; x < 4; ++x) rank += c0 + x < beams && c0 + x != b ? a[x] : 0;
+      }
+      if (rank < best) put(i, rank);
+    }
   }
-  atomicAdd(&taken_s, taken);
+  if (taken) atomicAdd(&taken_s, taken);
   __syncthreads();
   for (int i = taken_s + tid; i < best; i += kJoinThreads) {
     const int64_t o = group * best + i;

@@ -37,6 +37,20 @@ inline bool count_ok(int64_t n) { return n >= 0 && n <= (int64_t)GNN_MAX_COUNT; 
 // Blocks of `per_block` threads (or rows) covering n, computed in 64 bits.
 inline unsigned blocks_for(int64_t n, int64_t per_block) { return (unsigned)((n + per_block - 1) / per_block); }
 
+// Lets a kernel have `bytes` of dynamic shared memory: asked for once on each device.
+template <auto KERNEL>
+cudaError_t allow_smem(int bytes) {
+  static std::atomic<uint64_t> done{0};
+  int device = 0;
+  cudaError_t err = cudaGetDevice(&device);
+  if (err != cudaSuccess) return err;
+  const uint64_t bit = device < 64 ? 1ull << device : 0;
+  if (done.load() & bit) return cudaSuccess;
+  err = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (err == cudaSuccess) done.fetch_or(bit);
+  return err;
+}
+
 // Launch as a programmatic dependent of the previous kernel in the stream: the kernel may start
 // while that one finishes its last CTAs, and waits for it (pdl_wait) before touching its data.
 // Every kernel launched this way calls pdl_wait before its first access to data an earlier

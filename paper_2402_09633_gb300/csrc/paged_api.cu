@@ -117,7 +117,7 @@ bool paged_map(CUtensorMap* map, const gnn_heads& h, int64_t rows, int dtype, in
 
 template <typename T, int DP>
 cudaError_t launch_paged(const PagedParams& p, const PagedPlan& plan, const CUtensorMap* maps, cudaStream_t st) {
-  cudaError_t err = cudaFuncSetAttribute(paged_tile_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, paged_smem_bytes<DP>());
+  cudaError_t err = allow_smem<paged_tile_kernel<T, DP>>(paged_smem_bytes<DP>());
   if (err == cudaSuccess)
     err = launch_pdl(paged_tile_kernel<T, DP>, plan.blocks, kAttendThreads, paged_smem_bytes<DP>(), st, p, plan.g, maps[0], maps[1],
                      maps[2], maps[3], maps[4], maps[5]);
@@ -138,7 +138,7 @@ bool beam_ok(const gnn_beam_call* c) {
 // Strips of a row.  A block's time is a few rounds of its warps' for its start and end, and its strip's rounds; rounds of
 // blocks that do not fill the SMs are lost.
 int beam_strips(const gnn_beam_call* c, int n_sm) {
-  const int64_t rows = c->n_groups * c->beams, slots = 3 * (int64_t)n_sm, round = kStripThreads * kStripPieces * 16 / elem_bytes(c->dtype);
+  const int64_t rows = c->n_groups * c->beams, slots = kStripBlocks * (int64_t)n_sm, round = kStripThreads * kLaneElements;
   const int64_t rounds = (c->vocab + round - 1) / round;
   int64_t best = 1, least = 0;
   for (int64_t s = 1; s <= std::min<int64_t>(kStripsMost, rounds); ++s) {
@@ -148,7 +148,6 @@ int beam_strips(const gnn_beam_call* c, int n_sm) {
   return (int)best;
 }
 
-constexpr int kJoinSmem = 16 * kBeamMost * kBeamMost + 8 * (kJoinThreads / 32) * kStripsMost * kBeamMost;
 constexpr int kMostSms = 152;        // that strips are counted for where no device need be asked
 
 uint64_t beam_bytes(const gnn_beam_call* c) {
@@ -167,7 +166,7 @@ int run_moves(MoveParams& p, int what, int64_t columns, cudaStream_t st) {
   p.segments = (int)std::max<int64_t>(1, std::min<int64_t>(want, (columns + kMoveThreads - 1) / kMoveThreads));
   if (p.groups * what * p.segments >= (int64_t)1 << 31) return GNN_ERR_INVALID_ARG;
   const size_t smem = (size_t)p.beams * kMoveThreads * 16;
-  cudaError_t err = cudaFuncSetAttribute(beam_move_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBeamMost * kMoveThreads * 16);
+  cudaError_t err = allow_smem<beam_move_kernel>(kBeamMost * kMoveThreads * 16);
   if (err == cudaSuccess)
     err = launch_pdl(beam_move_kernel, (unsigned)(p.groups * what * p.segments), kMoveThreads, smem, st, p);
   return err == cudaSuccess ? GNN_OK : cuda_fail(err);
@@ -258,13 +257,22 @@ int gnn_paged_attend(const gnn_pages* c, const gnn_paged_call* a, gnn_stream_t s
   // a scale of zero as one too small to be seen, so that -inf, a score that is not seen, stays -inf
   p.scale_log2 = a->scale == 0.f ? 1e-30f : (float)((double)a->scale * 1.4426950408889634);
   p.err = c->status;
+  // the packs' queries, keys and values; the groups', which are the same where the loads are
   CUtensorMap maps[6];
   const int64_t rows = c->n_pages * c->page_size;
-  if (!paged_map(&maps[0], a->q, a->n_q_rows, c->dtype, p.dim, plan.g.group, plan.g.box_a) ||
-      !paged_map(&maps[1], a->q, a->n_q_rows, c->dtype, p.dim, plan.g.group, plan.g.box_b) ||
-      !paged_map(&maps[2], c->k, rows, c->dtype, p.dim, 1, plan.g.box) || !paged_map(&maps[3], c->v, rows, c->dtype, p.dim, 1, plan.g.box) ||
+  if (!paged_map(&maps[1], a->q, a->n_q_rows, c->dtype, p.dim, plan.g.group, plan.g.box_b) ||
       !paged_map(&maps[4], c->k, rows, c->dtype, p.dim, 1, kPiece) || !paged_map(&maps[5], c->v, rows, c->dtype, p.dim, 1, kPiece))
     return GNN_ERR_INVALID_ARG;
+  maps[0] = maps[1];
+  maps[2] = maps[4];
+  maps[3] = maps[5];
+  if (p.n_groups > 0) {
+    if (plan.g.box_a != plan.g.box_b && !paged_map(&maps[0], a->q, a->n_q_rows, c->dtype, p.dim, plan.g.group, plan.g.box_a))
+      return GNN_ERR_INVALID_ARG;
+    if (plan.g.box != kPiece && (!paged_map(&maps[2], c->k, rows, c->dtype, p.dim, 1, plan.g.box) ||
+                                 !paged_map(&maps[3], c->v, rows, c->dtype, p.dim, 1, plan.g.box)))
+      return GNN_ERR_INVALID_ARG;
+  }
   const cudaStream_t st = (cudaStream_t)stream;
   const cudaError_t err = c->dtype == GNN_DTYPE_BF16
                               ? p.dim <= 64 ? launch_paged<__nv_bfloat16, 64>(p, plan, maps, st) : launch_paged<__nv_bfloat16, 128>(p, plan, maps, st)
@@ -305,15 +313,14 @@ int gnn_beam_select(const gnn_beam_call* c, gnn_stream_t stream) {
   p.out_token = c->out_tokens;
   const cudaStream_t st = (cudaStream_t)stream;
   const unsigned grid = (unsigned)(p.rows * p.strips);
-  auto strips = [&](auto kernel) {
-    const cudaError_t set = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kStripSmem);
-    return set != cudaSuccess ? set : launch_pdl(kernel, grid, kStripThreads, kStripSmem, st, p);
+  auto strips = [&](auto element) {
+    using T = decltype(element);
+    const cudaError_t set = allow_smem<beam_strip_kernel<T>>(strip_smem<T>());
+    return set != cudaSuccess ? set : launch_pdl(beam_strip_kernel<T>, grid, kStripThreads, strip_smem<T>(), st, p);
   };
-  cudaError_t err = c->dtype == GNN_DTYPE_FP32   ? strips(beam_strip_kernel<float>)
-                    : c->dtype == GNN_DTYPE_BF16 ? strips(beam_strip_kernel<__nv_bfloat16>)
-                                                 : strips(beam_strip_kernel<__half>);
-  const size_t smem = 16 * (size_t)p.beams * p.best + (p.strips > 1 ? 8 * (size_t)(kJoinThreads / 32) * p.strips * p.best : 0);
-  if (err == cudaSuccess) err = cudaFuncSetAttribute(beam_join_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kJoinSmem);
+  cudaError_t err = c->dtype == GNN_DTYPE_FP32 ? strips(float()) : c->dtype == GNN_DTYPE_BF16 ? strips(__nv_bfloat16()) : strips(__half());
+  const int smem = join_smem(p.beams, p.strips, p.best);
+  if (err == cudaSuccess) err = allow_smem<beam_join_kernel>(join_smem(kBeamMost, kStripsMost, kBeamMost));
   if (err == cudaSuccess) err = launch_pdl(beam_join_kernel, (unsigned)c->n_groups, kJoinThreads, smem, st, p);
   return err == cudaSuccess ? GNN_OK : cuda_fail(err);
 }

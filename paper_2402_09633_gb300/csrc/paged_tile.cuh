@@ -108,6 +108,7 @@ __device__ __forceinline__ int64_t paged_divide(int64_t a, int64_t b) {
 struct PagedSegment { int q0, lo, limit; };
 struct PagedItem {
   int n, first;                      // blocks of this part (-1: there is no more work), and the first one's number
+  int whole;                         // blocks whose rows all are keys, as far as that is known
   int both, start;                   // two tiles over the same blocks; or one tile, the first block on tile `start`
   int rows[2];                       // of each tile
   int query[2];                      // each tile's first
@@ -404,7 +405,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         if (!ok) return;
         if (lane == 0) {
           PagedItem& to = b.item[slot];
-          to.n = it.n; to.first = it.first; to.both = it.both; to.start = it.start; to.segments = it.segments; to.step = it.step;
+          to.n = it.n; to.first = it.first; to.whole = it.whole; to.both = it.both; to.start = it.start; to.segments = it.segments; to.step = it.step;
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
             to.rows[t] = it.rows[t]; to.query[t] = it.query[t]; to.out[t] = it.out[t]; to.sum[t] = it.sum[t];
@@ -422,6 +423,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         PagedItem it;
         it.n = b1 - b0;
         it.first = b0;
+        it.whole = own ? 0 : w.len / kKeys;
         it.both = e < (uint32_t)w.twos;
         it.start = (int)(turn & 1);
         if (!it.both) turn += (uint32_t)it.n;
@@ -541,7 +543,8 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
         const uint32_t slot = items % kItemSlots;
         ok = wait(&b.item_full[slot], items / kItemSlots);
         if (!ok) break;
-        const int n = uniform(b.item[slot].n), both = uniform(b.item[slot].both), start = uniform(b.item[slot].start);
+        const int n = uniform(b.item[slot].n), both = uniform(b.item[slot].both), start = uniform(b.item[slot].start),
+                  whole = uniform(b.item[slot].whole) - uniform(b.item[slot].first);
         __syncwarp();
         if (lane == 0) mbar_arrive(&b.item_empty[slot]);
         ++items;
@@ -589,22 +592,24 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
             if (!ok) break;
             // Values of rows that are no keys: zeros, so that weights of zero leave no trace of them.  (Where several warps do this,
             // each does before its own products.)
-            const uint32_t there = b.there[vs][lane / 4], row4 = lane % 4 * 4;                // lane l: rows 4 l .. 4 l + 3
-            uint32_t gone = 0;
+            if (i >= whole) {
+              const uint32_t there = b.there[vs][lane / 4], row4 = lane % 4 * 4;                // lane l: rows 4 l .. 4 l + 3
+              uint32_t gone = 0;
 #pragma unroll
-            for (uint32_t r = 0; r < 4; ++r) gone |= row4 + r < (there & 255) || row4 + r >= there >> 8 ? 1u << r : 0u;
-            uint32_t some = __ballot_sync(0xffffffffu, gone != 0);
-            if (some) {
+              for (uint32_t r = 0; r < 4; ++r) gone |= row4 + r < (there & 255) || row4 + r >= there >> 8 ? 1u << r : 0u;
+              uint32_t some = __ballot_sync(0xffffffffu, gone != 0);
+              if (some) {
 #pragma unroll 1
-              for (; some; some &= some - 1) {
-                const int four = __ffs(some) - 1, r = lane / 8;
-                if (__shfl_sync(0xffffffffu, gone, four) >> r & 1u)
-                  for (int h = 0; h < halves; ++h)
-                    *reinterpret_cast<uint4*>(kv_buf + vs * S::kKvBytes + h * kKeys * 128 + (4 * four + r) * 128 + lane % 8 * 16) =
-                        make_uint4(0, 0, 0, 0);
+                for (; some; some &= some - 1) {
+                  const int four = __ffs(some) - 1, r = lane / 8;
+                  if (__shfl_sync(0xffffffffu, gone, four) >> r & 1u)
+                    for (int h = 0; h < halves; ++h)
+                      *reinterpret_cast<uint4*>(kv_buf + vs * S::kKvBytes + h * kKeys * 128 + (4 * four + r) * 128 + lane % 8 * 16) =
+                          make_uint4(0, 0, 0, 0);
+                }
+                fence_async_shared();
+                __syncwarp();
               }
-              fence_async_shared();
-              __syncwarp();
             }
           }
 #pragma unroll

@@ -84,11 +84,19 @@ def _check(rc, what):
         raise GnnError(rc, what)
 
 
-def _bytes(call):
-    """The workspace size that a call of the library writes."""
-    n = _u64()
-    call(ctypes.byref(n))
-    return n.value
+_sizes = {}                                                # workspace bytes of calls, by what they depend on
+
+
+def _workspace(key, ask, device, stream):
+    """Memory for a call whose size `ask(address)` of the library says; the same sizes are asked for once."""
+    n = _sizes.get(key)
+    if n is None:
+        size = _u64()
+        ask(ctypes.byref(size))
+        if len(_sizes) >= 4096:
+            _sizes.clear()
+        n = _sizes[key] = size.value
+    return _empty(n, Q._torch.uint8, device, stream), n
 
 
 def _empty(n, dtype, device, stream):
@@ -117,6 +125,7 @@ class PagedCache:
         self.kv_len_at = Q._vector(kv_len, n, Q._torch.int32, device)
         self.k, self.v, self.table, self.kv_len, self.page_size = k, v, table, kv_len, page_size
         self.dtype, self.device, self.dim, self.lib = dtype, device, dim, lib
+        self.shape = dim, page_size, table.shape, k.shape[1]                     # what sizes depend on
         self.word = Q._torch.zeros(1, dtype=Q._torch.int32, device=k.device)
         Q._torch.cuda.current_stream().synchronize()         # the zero is there before any stream's first call
         self.pages = _PAGES(*Q._fields(k, dtype, device, dim), *Q._fields(v, dtype, device, dim), k.shape[0] // page_size, number,
@@ -172,11 +181,13 @@ class PagedCache:
         where = (Q._vector(groups, n_groups + 1, int32, device), Q._vector(shared, n_groups, int32, device)) if n_groups else (0, 0)
         fields = (*Q._fields(q, dtype, device, dim), *Q._fields(out, dtype, device, dim), self._starts(q_start), *where, n, n_groups,
                   max_q, 1.0 / math.sqrt(dim) if scale is None else scale, 0)
-        size = _bytes(lambda n: _check(self.lib.gnn_paged_workspace(self.pages, _ATTEND(*fields, 0, 0), n),
-                                       "gnn_paged_workspace"))
-        space = _empty(size, Q._torch.uint8, device, stream)
-        _check(self.lib.gnn_paged_attend(self.pages, _ATTEND(*fields, space.data_ptr(), size), Q._stream(stream, device)),
-               "gnn_paged_attend")
+        lib = self.lib
+        space, size = _workspace((device, self.shape, q.shape[1], n, n_groups, max_q),
+                                 lambda at: _check(lib.gnn_paged_workspace(self.pages, _ATTEND(*fields, 0, 0), at), "gnn_paged_workspace"),
+                                 device, stream)
+        rc = lib.gnn_paged_attend(self.pages, _ATTEND(*fields, space.data_ptr(), size), Q._stream(stream, device))
+        if rc != GNN_OK:
+            raise GnnError(rc, "gnn_paged_attend")
         return out
 
     def status(self, stream=None) -> int:
@@ -198,30 +209,44 @@ def beam_select(logits, scores, beams: int, best=None, ended=None, end: int = 0,
     groups, best = rows // beams, beams if best is None else best
     if ended is not None:
         assert ended.dtype in (torch.bool, torch.uint8), "ended: bool or uint8"
+    dtype = Q.DTYPES[logits.dtype]
     at = Q._vector(scores, rows, torch.float32, device), Q._vector(ended, rows, None if ended is None else ended.dtype, device) or 0
     size = max(0, groups * best)
-    out = [_empty(size, t, device, stream) for t in (torch.float32, torch.int32, torch.int32)]
+    out, parents = _empty(size, torch.float32, device, stream), _empty(size, torch.int32, device, stream)
+    tokens = _empty(size, torch.int32, device, stream)
     if rows == 0:
-        return tuple(out)
-    fields = (logits.data_ptr(), logits.stride(0), groups, *at, Q.DTYPES[logits.dtype], beams, vocab, best, end, 0,
-              *(x.data_ptr() for x in out))
-    n = _bytes(lambda n: _check(lib.gnn_beam_workspace(_BEAM(*fields, 0, 0), n), "gnn_beam_workspace"))
-    space = _empty(n, torch.uint8, device, stream)
-    _check(lib.gnn_beam_select(_BEAM(*fields, space.data_ptr(), n), Q._stream(stream, device)), "gnn_beam_select")
-    return tuple(out)
+        return out, parents, tokens
+    fields = (logits.data_ptr(), logits.stride(0), groups, *at, dtype, beams, vocab, best, end, 0, out.data_ptr(), parents.data_ptr(),
+              tokens.data_ptr())
+    space, n = _workspace((device, dtype, groups, beams, vocab, best),
+                          lambda at: _check(lib.gnn_beam_workspace(_BEAM(*fields, 0, 0), at), "gnn_beam_workspace"), device, stream)
+    rc = lib.gnn_beam_select(_BEAM(*fields, space.data_ptr(), n), Q._stream(stream, device))
+    if rc != GNN_OK:
+        raise GnnError(rc, "gnn_beam_select")
+    return out, parents, tokens
 
 
 def _state(x, y, rows, device):
-    assert x.get_device() == device and x.shape[0] == rows, "states: cuda tensors [rows, ...] of the parents' device"
-    if rows == 0 or x.numel() == 0:
+    shape = x.shape
+    assert x.get_device() == device and shape[0] == rows, "states: cuda tensors [rows, ...] of the parents' device"
+    assert y is x or (y.get_device() == device and y.shape == shape and y.dtype == x.dtype), "out: tensors like the states"
+    whole = x.nbytes
+    if whole == 0:
         return _STATE(0, 0, 0, 0, 0)
-    inner = x.numel() // rows * x.element_size()
-    for t in (x, y):
-        assert t.get_device() == device and t.shape == x.shape and t.dtype == x.dtype, "out: tensors like the states"
-        assert rows == 1 or t.stride(0) * t.element_size() >= inner, "rows overlap"
-        assert t[0].is_contiguous(), "a state's row is contiguous"
-    strides = [t.stride(0) * t.element_size() if rows > 1 else inner for t in (x, y)]
+    inner = whole // rows
+    strides = [_row_stride(x, inner), inner]
+    strides[1] = strides[0] if y is x else _row_stride(y, inner)
     return _STATE(x.data_ptr(), y.data_ptr(), *strides, inner)
+
+
+def _row_stride(x, inner):
+    """Bytes from a row to the next."""
+    if x.is_contiguous():
+        return inner
+    stride = x.stride(0) * x.element_size()
+    assert x[0].is_contiguous(), "a state's row is contiguous"
+    assert stride >= inner or x.shape[0] == 1, "rows overlap"
+    return max(stride, inner)
 
 
 def beam_reorder(parents, beams: int, states=(), out=None, caches=(), stream=None):
@@ -237,7 +262,7 @@ def beam_reorder(parents, beams: int, states=(), out=None, caches=(), stream=Non
     at, st = Q._vector(parents, rows, Q._torch.int32, device), Q._stream(stream, device)
     new = list(states if out is None else out)
     assert len(new) == len(states), "as many outputs as states"
-    moves = b"".join(_state(x, y, rows, device) for x, y in zip(states, new))
+    moves = b"".join([_state(x, y, rows, device) for x, y in zip(states, new)])
     for c in caches:
         assert c.device == device and c.table.shape[0] == rows, "caches of as many sequences, on the same device"
     if rows == 0:
