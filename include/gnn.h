@@ -570,7 +570,7 @@ int gnn_paged_append(const gnn_pages* pages, const gnn_rotary* rot, const gnn_ap
  *                    input
  *   q_start          device int32 [n_seqs + 1], not decreasing; rows before the first and from the last on are not written
  *   group_start      device int32 [n_groups + 1], not decreasing, and shared_len, device int32 [n_groups]; both NULL with
- *                    n_groups 0.  n_groups <= n_seqs
+ *                    n_groups 0.  Groups may be empty
  *   max_q            the most queries of a sequence; 0: not known.  A sequence with more is INDEX_RANGE, its rows undefined
  *   workspace        device, 32-byte aligned, of at least the bytes that gnn_paged_workspace says for the same call; written
  *                    before it is read, so its contents need not be anything.  Calls that may overlap have one each.
@@ -639,7 +639,7 @@ int gnn_beam_select(const gnn_beam_call* call, gnn_stream_t stream);
  *   states           host array; data has n_groups * beams rows of row_bytes bytes, `stride` bytes apart (stride >=
  *                    row_bytes); out: the same out_stride bytes apart, or data itself (same strides): in place.  Arrays
  *                    do not overlap otherwise
- *   beams            1..64
+ *   beams            1..64;  n_groups at most 2^26
  * Enqueued on `stream`; no workspace.  Errors: INVALID_ARG, CUDA.
  *
  * gnn_paged_reorder -- the same for caches in pages, whose sequences are the hypotheses: n_caches caches (of a model's

@@ -45,7 +45,7 @@ bool wide_ok(const gnn_heads& v, int dtype) {
 bool attend_ok(const gnn_pages* c, const gnn_paged_call* a) {
   if (!pages_ok(c) || !a || a->reserved != 0 || c->dtype == GNN_DTYPE_FP32) return false;
   if (c->head_dim < 8 || c->head_dim > 128 || c->head_dim % 8 != 0 || !std::isfinite(a->scale)) return false;
-  if (!count_ok(a->n_q_rows) || a->max_q < 0 || a->n_groups < 0 || a->n_groups > c->n_seqs) return false;
+  if (!count_ok(a->n_q_rows) || a->max_q < 0 || a->n_groups < 0 || a->n_groups > 1 << 28) return false;
   if ((a->n_groups > 0) != (a->group_start != nullptr) || (a->group_start != nullptr) != (a->shared_len != nullptr)) return false;
   if ((uintptr_t)a->group_start % 4 || (uintptr_t)a->shared_len % 4) return false;
   if (!wide_ok(c->k, c->dtype) || !wide_ok(c->v, c->dtype)) return false;
@@ -164,7 +164,6 @@ int run_moves(MoveParams& p, int what, int64_t columns, cudaStream_t st) {
   // segments for a few rounds of all SMs, at least a block's columns each
   const int64_t want = (16 * (int64_t)sms + p.groups * what - 1) / (p.groups * what);
   p.segments = (int)std::max<int64_t>(1, std::min<int64_t>(want, (columns + kMoveThreads - 1) / kMoveThreads));
-  if (p.groups * what * p.segments >= (int64_t)1 << 31) return GNN_ERR_INVALID_ARG;
   const size_t smem = (size_t)p.beams * kMoveThreads * 16;
   cudaError_t err = allow_smem<beam_move_kernel>(kBeamMost * kMoveThreads * 16);
   if (err == cudaSuccess)
@@ -327,7 +326,7 @@ int gnn_beam_select(const gnn_beam_call* c, gnn_stream_t stream) {
 
 int gnn_beam_reorder(const int32_t* parents, int64_t n_groups, int32_t beams, const gnn_beam_state* states, int32_t n_states,
                      gnn_stream_t stream) {
-  if (beams < 1 || beams > kBeamMost || !count_ok(n_groups) || !count_ok(n_groups * beams) || n_states < 0 || (n_states > 0 && !states) ||
+  if (beams < 1 || beams > kBeamMost || n_groups < 0 || n_groups > 1 << 26 || n_states < 0 || (n_states > 0 && !states) ||
       (uintptr_t)parents % 4)
     return GNN_ERR_INVALID_ARG;
   for (int i = 0; i < n_states; ++i) {
@@ -363,7 +362,7 @@ int gnn_beam_reorder(const int32_t* parents, int64_t n_groups, int32_t beams, co
 
 int gnn_paged_reorder(const gnn_pages* caches, int32_t n_caches, const int32_t* parents, int64_t n_groups,
                       int32_t beams, gnn_stream_t stream) {
-  if (n_caches < 1 || !caches || beams < 1 || beams > kBeamMost || !count_ok(n_groups) || !count_ok(n_groups * beams) ||
+  if (n_caches < 1 || !caches || beams < 1 || beams > kBeamMost || n_groups < 0 || n_groups > 1 << 26 ||
       (uintptr_t)parents % 4)
     return GNN_ERR_INVALID_ARG;
   const gnn_pages& c = caches[0];

@@ -49,7 +49,9 @@ __device__ __forceinline__ PagedWork paged_group_work(const PagedParams& p, cons
   w.q0 = min(max(first, 0), p.n_q_rows);
   w.nq = min(max(last, w.q0), p.n_q_rows) - w.q0;
   w.table = s0;
-  w.len = paged_shared(p, i, bad);
+  bool outside = false;
+  w.len = paged_shared(p, i, &outside);
+  *bad = *bad || (outside && s1 > s0);
   w.blocks = (w.len + kKeys - 1) / kKeys;
   const int tiles = (w.nq + g.tile_q - 1) / g.tile_q;
   w.twos = tiles / 2;

@@ -54,7 +54,7 @@ def test_append_refusals(lib, bad):
     dict(pages=_pages(head_dim=136)), dict(pages=_pages(k=_view(data=AT + 8))), dict(pages=_pages(v=_view(row_stride=4))),
     dict(pages=_pages(v=_view(row_stride=0))), dict(pages=_pages(k=_view(head_stride=0))), dict(scale=float("inf")),
     dict(scale=float("nan")), dict(n_q_rows=-1), dict(n_q_rows=2 ** 31 - 1), dict(max_q=-1), dict(n_groups=-1),
-    dict(n_groups=3), dict(n_groups=0), dict(group_start=None), dict(shared_len=None), dict(group_start=AT + 1),
+    dict(n_groups=2 ** 28 + 1), dict(n_groups=0), dict(group_start=None), dict(shared_len=None), dict(group_start=AT + 1),
     dict(shared_len=AT + 2), dict(q_start=None), dict(q_start=AT + 2), dict(q=_view(data=AT + 8)), dict(q=_view(row_stride=12)),
     dict(out=_view(data=None)), dict(out=_view(n_heads=4)), dict(q=_view(n_heads=3), out=_view(n_heads=3)),
     dict(q=_view(n_heads=4098), out=_view(n_heads=4098)), dict(q=_view(n_heads=258), out=_view(n_heads=258)), dict(reserved=1)])
