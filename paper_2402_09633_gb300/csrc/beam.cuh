@@ -546,28 +546,27 @@ template <> struct MoveWord<16> { using type = uint4; };
 template <> struct MoveWord<4> { using type = uint32_t; };
 template <> struct MoveWord<1> { using type = uint8_t; };
 
-// Columns [c0, n) in steps of `step`: from(c) and to(c) give a column's address in slot 0.. of the group, by slot.
-template <int W, typename From, typename To>
-__device__ __forceinline__ void move_columns(int64_t c0, int64_t n, int64_t step, int beams, const int8_t* parent, uint64_t need,
-                                             uint64_t get, uint8_t* mine, From from, To to) {
+// Columns [c0, n) in steps of `step`: place(c) is where column c lies in a slot, from[i] and to[i] where slot i lies.
+template <int W, typename Place>
+__device__ __forceinline__ void move_columns(int64_t c0, int64_t n, int64_t step, const int8_t* parent, uint64_t need, uint64_t get,
+                                             uint8_t* mine, char* const* from, char* const* to, Place place) {
   using Word = typename MoveWord<W>::type;
+  const uint32_t mine32 = smem_u32(mine);
   for (int64_t c = c0; c < n; c += step) {
+    const int64_t at = place(c);
     for (uint64_t b = need; b; b &= b - 1) {
       const int i = __ffsll((long long)b) - 1;
-      uint8_t* dst = mine + i * (kMoveThreads * W);
-      if constexpr (W == 1) {
-        *dst = *reinterpret_cast<const uint8_t*>(from(i, c));
-      } else {
-        if constexpr (W == 16)
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(from(i, c)) : "memory");
-        else
-          asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(from(i, c)) : "memory");
-      }
+      if constexpr (W == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(mine32 + i * (kMoveThreads * W)), "l"(from[i] + at) : "memory");
+      else if constexpr (W == 4)
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(mine32 + i * (kMoveThreads * W)), "l"(from[i] + at) : "memory");
+      else
+        mine[i * (kMoveThreads * W)] = *reinterpret_cast<const uint8_t*>(from[i] + at);
     }
     if constexpr (W > 1) asm volatile("cp.async.wait_all;" ::: "memory");
     for (uint64_t b = get; b; b &= b - 1) {
       const int i = __ffsll((long long)b) - 1;
-      *reinterpret_cast<Word*>(to(i, c)) = *reinterpret_cast<const Word*>(mine + parent[i] * (kMoveThreads * W));
+      *reinterpret_cast<Word*>(to[i] + at) = *reinterpret_cast<const Word*>(mine + parent[i] * (kMoveThreads * W));
     }
   }
 }
@@ -576,7 +575,7 @@ __device__ __forceinline__ void move_columns(int64_t c0, int64_t n, int64_t step
 __global__ void __launch_bounds__(kMoveThreads) beam_move_kernel(const __grid_constant__ MoveParams p) {
   extern __shared__ __align__(16) uint8_t move_smem[];
   __shared__ int8_t parent_s[kBeamMost];
-  __shared__ int entry_s[kBeamMost];
+  __shared__ char *from_s[kBeamMost], *to_s[kBeamMost];          // the slots' rows, or open pages
   __shared__ unsigned long long need_s, get_s;
   __shared__ int len_s, uneven_s, bad_s;
   const int tid = threadIdx.x;
@@ -609,13 +608,14 @@ __global__ void __launch_bounds__(kMoveThreads) beam_move_kernel(const __grid_co
   const int64_t c0 = (int64_t)segment * kMoveThreads + tid, step = (int64_t)p.segments * kMoveThreads;
   if (!paged) {
     const MoveState& s = p.state[what];
-    const char* src = s.data + first * s.stride;
-    char* dst = s.out + first * s.out_stride;
+    if (tid < p.beams) {
+      from_s[tid] = s.data + (first + tid) * s.stride;
+      to_s[tid] = s.out + (first + tid) * s.out_stride;
+    }
+    __syncthreads();
     auto go = [&](auto w) {
       constexpr int W = decltype(w)::value;
-      move_columns<W>(c0, s.bytes / W, step, p.beams, parent_s, need, get, move_smem + tid * W,
-                      [&](int i, int64_t c) { return src + i * s.stride + c * W; },
-                      [&](int i, int64_t c) { return dst + i * s.out_stride + c * W; });
+      move_columns<W>(c0, s.bytes / W, step, parent_s, need, get, move_smem + tid * W, from_s, to_s, [](int64_t c) { return c * W; });
     };
     if (s.width == 16) go(std::integral_constant<int, 16>());
     else if (s.width == 4) go(std::integral_constant<int, 4>());
@@ -629,19 +629,17 @@ __global__ void __launch_bounds__(kMoveThreads) beam_move_kernel(const __grid_co
   }
   if (part > 0 && tid < p.beams) {                   // the open page of each slot; nothing writes its entry
     const int e = p.table[(first + tid) * p.table_stride + full];
-    entry_s[tid] = e;
     if (e < 0 || e >= p.n_pages) bad_s = 1;
+    if (what < p.pools) from_s[tid] = p.pool[what].data + ((int64_t)e << p.shift) * p.pool[what].row_bytes;
   }
+  if (what == p.pools && tid < p.beams) from_s[tid] = reinterpret_cast<char*>(p.table + (first + tid) * p.table_stride);
   __syncthreads();
   if (bad_s) {
     if (tid == 0) atomicOr(p.err, DEV_ERR_INDEX_RANGE);
     return;
   }
   if (what == p.pools) {                             // entries of full pages
-    int* t = p.table + first * p.table_stride;
-    move_columns<4>(c0, full, step, p.beams, parent_s, need, get, move_smem + tid * 4,
-                    [&](int i, int64_t c) { return t + i * p.table_stride + c; },
-                    [&](int i, int64_t c) { return t + i * p.table_stride + c; });
+    move_columns<4>(c0, full, step, parent_s, need, get, move_smem + tid * 4, from_s, from_s, [](int64_t c) { return c * 4; });
     return;
   }
   if (part == 0) return;
@@ -649,11 +647,10 @@ __global__ void __launch_bounds__(kMoveThreads) beam_move_kernel(const __grid_co
   auto go = [&](auto w) {
     constexpr int W = decltype(w)::value;
     const unsigned piece = (unsigned)p.dim_bytes / W, row = piece * (unsigned)s.heads;
-    auto at = [&](int i, int64_t c) {
+    move_columns<W>(c0, (int64_t)part * row, step, parent_s, need, get, move_smem + tid * W, from_s, from_s, [&](int64_t c) {
       const unsigned r = (unsigned)c / row, in = (unsigned)c - r * row, h = in / piece;
-      return s.data + (((int64_t)entry_s[i] << p.shift) + r) * s.row_bytes + (int64_t)h * s.head_bytes + (in - h * piece) * W;
-    };
-    move_columns<W>(c0, (int64_t)part * row, step, p.beams, parent_s, need, get, move_smem + tid * W, at, at);
+      return r * s.row_bytes + h * s.head_bytes + (int64_t)((in - h * piece) * W);
+    });
   };
   if (s.width == 16) go(std::integral_constant<int, 16>());
   else if (s.width == 4) go(std::integral_constant<int, 4>());
