@@ -187,7 +187,10 @@ __device__ __forceinline__ PagedShare paged_share(const PagedParams& p, const Pa
   r.own = r.start >= sum[0];
   r.before = r.own ? sum[0] : 0;
   r.at = 0;
-  if (r.start >= r.end) return r;
+  if (r.start >= r.end) {
+    r.before = r.end;
+    return r;
+  }
   const int n = r.own ? p.n_seqs : p.n_groups;
   for (int c = 0; c < n; c += kAttendThreads) {
     int64_t w = 0;

@@ -35,7 +35,10 @@ extern "C" int walk(int grid, int n_q, int n_seqs, int n_groups, const int* q_st
   int n = 0;
   gridDim.x = grid;
   host::launch(grid, kAttendThreads, [&] {
+    if (threadIdx.x == 0) { bars.at = -1000000; bars.before = -7; }           // shared memory holds anything at first
+    __syncthreads();
     const PagedShare share = paged_share(p, g, bars);
+    if (share.start >= share.end && share.before < share.end) std::abort();
     if (threadIdx.x == 0) *share_out = share.share;
     if (threadIdx.x >= 32) return;
     bool ok = true;
