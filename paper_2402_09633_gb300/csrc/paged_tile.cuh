@@ -31,6 +31,7 @@ struct PagedGrid {
   int group;                         // query heads to a key head
   int pack;                          // sequences of a pack, a power of two; 1: a sequence may have several tiles
   int rows_a, rows_b;                // rows of a place
+  int2* group_rows;                  // [group]: its first row and how many, as the first kernel found them
   int2 *first_a, *first_b;           // [ordinal]: the first thread block of an item, and how many have a part
   float *out_a, *out_b;              // [ordinal + thread block][2 places][rows][dim]
   float2 *sum_a, *sum_b;             // the same, [rows]: scaled maximum and sum
@@ -149,6 +150,7 @@ __device__ __forceinline__ PagedShare paged_share(const PagedParams& p, const Pa
       if (i >= p.n_groups) return (int64_t)0;
       const PagedWork w = paged_group_work(p, g, i, &bad);
       if (i < kGroupsKept) s.shared[i] = w;
+      if (blockIdx.x == 0) g.group_rows[i] = make_int2(w.q0, w.nq);
       return paged_weight(p, w);
     }
     PagedOwn o = {p.n_q_rows, 0, 0, 0, 0, 0};
@@ -832,27 +834,52 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
 constexpr int kPagedJoinWarps = 4;
 
 // A row of a head to a warp: the parts of its shared and of its own keys into one, four elements to a lane.  Bound by its chain of
-// dependent loads: offsets, first blocks, sums, outputs.
+// dependent loads, so each step's go out together: what is known of the sequence and group that the row would be of if all were as
+// large (others are searched for), first blocks, sums, outputs.
 template <typename T>
 __global__ void __launch_bounds__(32 * kPagedJoinWarps) paged_join_kernel(const __grid_constant__ PagedParams p,
-                                                                           const __grid_constant__ PagedGrid g, int blocks) {
+                                                                              const __grid_constant__ PagedGrid g, int blocks) {
   __shared__ float q_s[kPagedJoinWarps][128];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t at = (int64_t)blockIdx.x * kPagedJoinWarps + warp;
+  const int row = (int)paged_divide(at, p.heads), head = (int)(at - (int64_t)row * p.heads), kv = head / g.group;
+  int seq = min((int)((float)row / (float)p.n_q_rows * (float)p.n_seqs), p.n_seqs - 1);
+  int group = p.n_groups > 0 ? min((int)((float)seq / (float)p.n_seqs * (float)p.n_groups), p.n_groups - 1) : -1;
   pdl_wait();
   if (at >= (int64_t)p.n_q_rows * p.heads) return;
-  const int row = (int)paged_divide(at, p.heads), head = (int)(at - (int64_t)row * p.heads), kv = head / g.group;
-  const int seq = sequence_of(p.q_start, p.n_seqs, p.n_q_rows, row);
-  if (seq < 0) return;
-  bool bad = false;
-  const PagedSequence sq = paged_sequence(p, seq, &bad);
-  // first rows of the pack and of the group, and the group's last
-  const int pack = g.pack > 1 ? seq / g.pack : seq;
-  int pack0 = p.q_start[pack * g.pack], group0 = 0, group1 = 0;
-  if (sq.shared > 0) {
-    group0 = min(max(p.q_start[min(sq.first, p.n_seqs)], 0), p.n_q_rows);
-    group1 = min(max(p.q_start[min(max(p.group_start[sq.group + 1], sq.first), p.n_seqs)], group0), p.n_q_rows);
+  int s0 = p.q_start[seq], s1 = p.q_start[seq + 1], len = p.kv_len[seq], pack0 = p.q_start[seq / g.pack * g.pack];
+  int g0 = 0, g1 = 0, shared = 0;
+  int2 rows = make_int2(0, 0);
+  if (group >= 0) {
+    g0 = p.group_start[group];
+    g1 = p.group_start[group + 1];
+    shared = p.shared_len[group];
+    rows = g.group_rows[group];
   }
+  if (row < s0 || row >= s1) {
+    seq = sequence_of(p.q_start, p.n_seqs, p.n_q_rows, row);
+    if (seq < 0) return;
+    s0 = p.q_start[seq];
+    s1 = p.q_start[seq + 1];
+    len = p.kv_len[seq];
+    pack0 = p.q_start[seq / g.pack * g.pack];
+  }
+  if (group >= 0 && (seq < g0 || seq >= g1)) {
+    group = sequence_of(p.group_start, p.n_groups, p.n_seqs, seq);
+    if (group >= 0) {
+      g0 = p.group_start[group];
+      shared = p.shared_len[group];
+      rows = g.group_rows[group];
+    }
+  }
+  // as the first kernel cuts them to the arrays
+  PagedSequence sq;
+  sq.q0 = min(max(s0, 0), p.n_q_rows);
+  sq.nq = min(max(s1, sq.q0), p.n_q_rows) - sq.q0;
+  sq.len = min(max(len, 0), paged_room(p));
+  sq.group = group;
+  sq.first = group >= 0 ? max(g0, 0) : seq;
+  sq.shared = group >= 0 ? min(max(shared, 0), paged_room(p)) : 0;
   pack0 = min(max(pack0, 0), p.n_q_rows);
   const int i = row - sq.q0;
   if (i >= p.max_q) return;
@@ -870,15 +897,15 @@ __global__ void __launch_bounds__(32 * kPagedJoinWarps) paged_join_kernel(const 
   int64_t ordinal_a = 0, ordinal_b;
   int row_a = 0, row_b, tile_a = 0, every = 1;       // every: shared parts of both places (1), or of one (2)
   if (sq.shared > 0) {
-    if (row < group0 || row >= group1) return;       // offsets that contradict each other
-    const int tile = (row - group0) / g.tile_q, tiles = (group1 - group0 + g.tile_q - 1) / g.tile_q;
-    row_a = (row - group0 - tile * g.tile_q) * g.group + head % g.group;
+    if (row < rows.x || row >= rows.x + rows.y) return;            // offsets that contradict each other
+    const int tile = (row - rows.x) / g.tile_q, tiles = (rows.y + g.tile_q - 1) / g.tile_q;
+    row_a = (row - rows.x - tile * g.tile_q) * g.group + head % g.group;
     every = (tile | 1) < tiles ? 2 : 1;
     tile_a = tile & 1;
-    ordinal_a = (paged_ordinal_a(g, sq.group, group0) + tile / 2) * p.kv_heads + kv;
+    ordinal_a = (paged_ordinal_a(g, group, rows.x) + tile / 2) * p.kv_heads + kv;
   }
   {
-    const int q0 = g.pack > 1 ? pack0 : sq.q0, tile = g.pack > 1 ? 0 : i / g.tile_q, query = row - q0 - tile * g.tile_q;
+    const int pack = seq / g.pack, q0 = g.pack > 1 ? pack0 : sq.q0, tile = g.pack > 1 ? 0 : i / g.tile_q, query = row - q0 - tile * g.tile_q;
     if (query < 0 || query >= g.box_b) return;
     row_b = query * g.group + head % g.group;
     ordinal_b = (paged_ordinal_b(g, pack, q0) + tile) * p.kv_heads + kv;

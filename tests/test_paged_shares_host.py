@@ -32,6 +32,8 @@ extern "C" int walk(int grid, int n_q, int n_seqs, int n_groups, const int* q_st
   PagedGrid g = {};
   g.group = group; g.tile_q = kTileQ / group; g.box = min(page, kKeys); g.pack = pack;
   static PagedBars bars;
+  std::vector<int2> group_rows(n_groups + 1);
+  g.group_rows = group_rows.data();
   int n = 0;
   gridDim.x = grid;
   host::launch(grid, kAttendThreads, [&] {
