@@ -103,19 +103,6 @@ __device__ __forceinline__ void take_lanes(WarpList& l, uint64_t k, int best) {
     l.a = merge_lanes(max(l.a, k));
   }
 }
-// The same for one key that all lanes know.
-__device__ __forceinline__ void take_one(WarpList& l, uint64_t k, int best) {
-  const int lane = threadIdx.x & 31;
-  if (best > 32) {
-    const uint64_t down = min(k, __shfl_sync(0xffffffffu, l.a, 31));  // what goes past the first 32 places
-    const int at = __popc(__ballot_sync(0xffffffffu, l.z > down));
-    const uint64_t up = __shfl_up_sync(0xffffffffu, l.z, 1);
-    l.z = lane < at ? l.z : lane == at ? down : up;
-  }
-  const int at = __popc(__ballot_sync(0xffffffffu, l.a > k));
-  const uint64_t up = __shfl_up_sync(0xffffffffu, l.a, 1);
-  l.a = lane < at ? l.a : lane == at ? k : up;
-}
 __device__ __forceinline__ uint64_t list_at(const WarpList& l, int i) {
   return __shfl_sync(0xffffffffu, i < 32 ? l.a : l.z, i & 31);
 }
@@ -123,6 +110,7 @@ __device__ __forceinline__ uint64_t list_at(const WarpList& l, int i) {
 // 2^n for a whole number that is not positive, exactly; zero where that is below what floats hold.
 __device__ __forceinline__ float power2(float n) { return n < -126.f ? 0.f : __int_as_float(((int)n + 127) << 23); }
 
+constexpr int kStripHeld = 8;         // candidates that are put in a warp's list together, at least
 constexpr int kLaneElements = 16;    // that a lane takes at a time
 template <typename T> constexpr int strip_stages() { return sizeof(T) == 4 ? 3 : 4; }            // what lets four blocks share an SM
 template <typename T> constexpr int strip_pieces() { return kLaneElements * (int)sizeof(T) / 16; }                // of 16 bytes
@@ -135,7 +123,7 @@ __global__ void __launch_bounds__(kStripThreads, kStripBlocks) beam_strip_kernel
   // Sums are of 2^(c x - r) with c = log2 e rounded, and their logarithm is divided by c again: that leaves 1.3e-8 of the weights'
   // entropy as an error, where c is off by 1.3e-8.  r is a whole number, so that joining sums rounds nothing.
   extern __shared__ __align__(16) uint8_t strip_ring[];
-  __shared__ uint64_t list_s[WARPS][kBeamMost];
+  __shared__ uint64_t list_s[WARPS][kBeamMost];      // at first what is held back
   __shared__ float high_s[WARPS];
   __shared__ double sum_s[WARPS];
   __shared__ int have_s[WARPS];
@@ -182,9 +170,20 @@ __global__ void __launch_bounds__(kStripThreads, kStripBlocks) beam_strip_kernel
 
   float m = -INFINITY, r = 0.f, s = 0.f;
   WarpList list = {0, 0};
-  float tau = -INFINITY;                             // of the list's last, once it is full
+  float least = -FLT_MAX;                            // what candidates are not below
+  int held = 0;                                      // of them in list_s
   const int deep = (best + WARPS - 1) / WARPS - 1;
   volatile unsigned* bounds = bound_s;
+  uint32_t tau = 0;                                  // of the list's last, once it is full
+  auto tell = [&] {                                  // what this warp's list bounds
+    tau = __shfl_sync(0xffffffffu, (uint32_t)((best > 32 ? list.z : list.a) >> 32), (best - 1) & 31);
+    const uint32_t place = __shfl_sync(0xffffffffu, (uint32_t)(list.a >> 32), deep);
+    if (lane == 0) bounds[warp] = place;
+  };
+  auto bound = [&](unsigned past) {                  // past = 1: elements behind those of the list lose a tie with its last
+    const uint32_t all = max(__reduce_min_sync(0xffffffffu, bounds[lane % WARPS]), tau ? tau + past : 0u);
+    return all ? unordered(all) : -FLT_MAX;
+  };
 #pragma unroll
   for (int k = 0; k < STAGES - 1; ++k) fetch(p0 + k * 32 * P, k);
   if (p0 >= p1) __syncthreads();                     // that of the others' first round; a warp without elements bounds nothing
@@ -237,12 +236,9 @@ __global__ void __launch_bounds__(kStripThreads, kStripBlocks) beam_strip_kernel
     }
     s += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
     // Candidates: above the list's last (later elements of the same value lose the tie), and not below what the block's lists
-    // hold together: all warps' elements at place best / 8 and before are `best` at least.
-    auto bound = [&] {
-      const unsigned all = __reduce_min_sync(0xffffffffu, bounds[lane % WARPS]);
-      // one comparison for both: the next float above the list's last, or the bound
-      return fmaxf(all ? unordered(all) : -FLT_MAX, tau == -INFINITY ? -FLT_MAX : unordered(ordered(tau) + 1));
-    };
+    // hold together: all warps' elements at place best / 8 and before are `best` at least.  They are held back, and
+    // put in the list kStripHeld or more at a time: a bound that is somewhat old lets through a few more, which costs less than a
+    // list that is always up to date (16 rows' groups of 300,000: 74.4 us with 8, 79.2 with 1, 75.8 with 32).
     auto key = [&](int i, bool in) {
       return in ? beam_key(high, (uint32_t)((c0 + i / VEC * 32 + lane) * VEC + i % VEC)) : 0;
     };
@@ -261,24 +257,18 @@ __global__ void __launch_bounds__(kStripThreads, kStripBlocks) beam_strip_kernel
       }
       high = next;
     };
-    float least = -FLT_MAX;
     if (c0 == p0) {
       // At first the lanes' largest elements, and a bound from all warps'.
       first_of_high();
       take_lanes(list, key(e, high > -INFINITY), best);
-      const uint64_t place = list_at(list, deep);
-      if (lane == 0) bounds[warp] = (unsigned)(place >> 32);
+      tell();
       __syncthreads();
-      least = bound();
+      least = bound(0);
       without();
     } else {
-      if (!__any_sync(0xffffffffu, high > tau)) continue;
-      least = bound();
+      if (!__any_sync(0xffffffffu, high >= least)) continue;
+      least = fmaxf(least, bound(1));
     }
-    bool some = high >= least;
-    uint32_t who = __ballot_sync(0xffffffffu, some);
-    if (who == 0 && c0 != p0) continue;
-    // Each lane's candidates.  Mostly some lane has one: then that is all.
     int n = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -286,25 +276,30 @@ __global__ void __launch_bounds__(kStripThreads, kStripBlocks) beam_strip_kernel
       e = in ? i : e;
       n += in;
     }
-    if (__popc(who) <= 6 && !__any_sync(0xffffffffu, n > 1)) {
-      const uint64_t k = key(e, some);
-      for (uint32_t x = who; x; x &= x - 1) take_one(list, __shfl_sync(0xffffffffu, k, __ffs(x) - 1), best);
-    } else {
+    const bool single = !__any_sync(0xffffffffu, n > 1);               // mostly no lane has two
 #pragma unroll 1
-      for (; who; who = __ballot_sync(0xffffffffu, some)) {
-        first_of_high();
-        take_lanes(list, key(e, some), best);
-        const uint64_t last = list_at(list, best - 1);
-        if (last) least = fmaxf(least, unordered((uint32_t)(last >> 32)));
-        without();
-        some = high >= least;
+    for (uint32_t who; (who = __ballot_sync(0xffffffffu, high >= least)) != 0;) {
+      if (!single) first_of_high();
+      if (high >= least) list_s[warp][held + __popc(who & ((1u << lane) - 1))] = key(e, true);
+      held += __popc(who);
+      if (held >= kStripHeld) {
+        __syncwarp();
+        take_lanes(list, lane < held ? list_s[warp][lane] : 0, best);
+        const uint64_t rest = list_s[warp][32 + lane];
+        __syncwarp();
+        list_s[warp][lane] = rest;
+        __syncwarp();
+        held = max(held - 32, 0);
+        tell();
+        least = fmaxf(least, bound(0));
       }
+      if (single) break;
+      without();
     }
-    const uint64_t end = list_at(list, best - 1);
-    if (end) tau = unordered((uint32_t)(end >> 32));
-    const uint64_t place = list_at(list, deep);
-    if (lane == 0 && place) bounds[warp] = (unsigned)(place >> 32);
   }
+  __syncwarp();
+  if (held > 0) take_lanes(list, lane < held ? list_s[warp][lane] : 0, best);
+  __syncwarp();
   if (lane < best) list_s[warp][lane] = list.a;
   if (lane + 32 < best) list_s[warp][lane + 32] = list.z;
   // the threads' sums
@@ -323,14 +318,21 @@ __global__ void __launch_bounds__(kStripThreads, kStripBlocks) beam_strip_kernel
   if (lane == 0) sum_s[warp] = sum;
   // the warps' lists: a key's place is its own and what the others have above it
   uint64_t* out = p.lists + (int64_t)blockIdx.x * best;
-  int taken = 0;
+  int taken = 0, top_half = 1;
+  while (2 * top_half <= best) top_half *= 2;
   for (int i = lane; i < best; i += 32) {
     const uint64_t k = list_s[warp][i];
     if (k == 0) break;
-    int rank = i;
+    // all warps' lists side by side, by halves
+    int place[WARPS] = {}, rank = 0;
+    for (int half = top_half; half > 0; half /= 2)
 #pragma unroll
-    for (int w = 0; w < WARPS; ++w)
-      if (w != warp) rank += above(list_s[w], best, k);
+      for (int w = 0; w < WARPS; ++w) {
+        const int at = place[w] + half;
+        if (at <= best && list_s[w][at - 1] > k) place[w] = at;
+      }
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) rank += place[w];
     if (rank < best) out[rank] = k;
     ++taken;
   }
