@@ -349,56 +349,46 @@ __global__ void __launch_bounds__(kStripThreads, kStripBlocks) beam_strip_kernel
   }
 }
 
-constexpr int kJoinThreads = 256;
-constexpr int kJoinKeys = 8192;      // of strips' lists that are looked at together
+constexpr int kJoinThreads = 512;
 constexpr int kJoinFew = 512;        // candidates that are compared with each other
 
-// Hypotheses whose strips' lists are looked at together.
-__host__ __device__ constexpr int join_rows(int beams, int strips, int best) {
-  const int n = kJoinKeys / (strips * best);
-  return n < 1 ? 1 : n < beams ? n : beams;
-}
-__host__ __device__ constexpr int join_smem(int beams, int strips, int best) {
-  return 16 * beams * best + 16 * beams * strips + 8 * join_rows(beams, strips, best) * strips * best;
-}
+__host__ __device__ constexpr int join_smem(int beams, int strips, int best) { return 16 * beams * best + 16 * beams * strips; }
 
-// One group to a block: first the strips of every row, then the rows, each time a candidate's place being how many of the
-// other lists' are before it.  Bound by its chain of steps: what a step needs from memory is fetched at once, and only candidates that
-// some `best` are not known to beat look for their place.
+// One group to a block: first the strips of every row, a row to a warp, which takes the lists' places from the first on until none
+// comes before its list's last; then the rows, a candidate's place being how many of the others are before it.  Bound by its chain
+// of steps: what a step needs from memory is fetched a step ahead, and only candidates that some `best` are not known to
+// beat look for their place.
 __global__ void __launch_bounds__(kJoinThreads) beam_join_kernel(const __grid_constant__ BeamParams p) {
   extern __shared__ __align__(16) uint64_t join_keys[];
   __shared__ double base_s[kBeamMost];               // what is added to a logit
   __shared__ int taken_s, left_s, few_s[kJoinFew], reach_s[kBeamMost];
-  const int tid = threadIdx.x, best = p.best, beams = p.beams, strips = p.strips, per = strips * best;
+  const int tid = threadIdx.x, best = p.best, beams = p.beams, strips = p.strips;
   const int64_t group = blockIdx.x, row0 = group * beams;
   BeamSum* sums = reinterpret_cast<BeamSum*>(join_keys);                         // [beams][strips]
   uint64_t* rows = reinterpret_cast<uint64_t*>(sums + beams * strips);           // [beams][best]
   uint64_t* values = rows + beams * best;            // the same, as they are ordered: comparing 64-bit floats takes long here
-  uint64_t* lists = values + beams * best;           // [join_rows][strips][best]
-  const int together = join_rows(beams, strips, best);
   if (tid == 0) taken_s = left_s = 0;
   if (tid < kBeamMost) reach_s[tid] = 0;
   pdl_wait();
   for (int i = tid; i < beams * strips; i += kJoinThreads) sums[i] = p.sums[row0 * strips + i];
-  for (int b0 = 0; b0 < beams; b0 += together) {
-    const int n = min(together, beams - b0);
-    uint64_t* to = strips == 1 ? rows + b0 * best : lists;
-    const uint64_t* from = p.lists + (row0 + b0) * per;
-#pragma unroll 4
-    for (int i = tid; i < n * per; i += kJoinThreads) to[i] = from[i];
-    if (strips == 1) continue;
-    for (int i = tid; i < n * best; i += kJoinThreads) rows[b0 * best + i] = 0;
-    __syncthreads();
-    for (int i = tid; i < n * per; i += kJoinThreads) {
-      const uint64_t k = lists[i];
-      if (k == 0) continue;
-      const int row = i / per, s = (i - row * per) / best;
-      int rank = i - row * per - s * best;
-      for (int t = 0; t < strips && rank < best; ++t)
-        if (t != s) rank += above(lists + row * per + t * best, best, k);
-      if (rank < best) rows[(b0 + row) * best + rank] = k;
+  if (strips == 1) {
+    for (int i = tid; i < beams * best; i += kJoinThreads) rows[i] = p.lists[row0 * best + i];
+  } else {
+    const int lane = tid & 31, log = 32 - __clz(strips - 1), strip = lane & ((1 << log) - 1), places = 32 >> log;
+    for (int b = tid >> 5; b < beams; b += kJoinThreads / 32) {
+      const uint64_t* from = p.lists + ((row0 + b) * strips + strip) * best;
+      auto fetch = [&](int place) { return strip < strips && place < best ? from[place] : 0; };
+      WarpList list = {0, 0};
+      uint64_t last = 0, next = fetch(lane >> log);
+      for (int i = lane >> log; __any_sync(0xffffffffu, next > last); i += places) {
+        const uint64_t k = next;
+        next = fetch(i + places);
+        take_lanes(list, k, best);
+        last = list_at(list, best - 1);
+      }
+      if (lane < best) rows[b * best + lane] = list.a;
+      if (lane + 32 < best) rows[b * best + 32 + lane] = list.z;
     }
-    __syncthreads();
   }
   __syncthreads();
   // 64-bit arithmetic is slow here: one logarithm for all rows

@@ -136,14 +136,17 @@ bool beam_ok(const gnn_beam_call* c) {
   return count_ok(c->n_groups) && count_ok(c->n_groups * c->beams) && c->row_stride >= 0 && c->row_stride < (int64_t)1 << 39;
 }
 
-// Strips of a row.  A block's time is a few rounds of its warps' for its start and end, and its strip's rounds; rounds of
-// blocks that do not fill the SMs are lost.
+// Strips of a row.  A strip takes its rounds of elements and about eight more for its first lists and its end; two blocks of an SM run
+// beside each other for nothing, more share its issue slots.  In microseconds, by strips of a row (fp32, of 300,000 elements):
+//   16 rows:  1: 53.4  2: 37.0  4: 27.2  9: 21.8  19: 22.4 (taken)  32: 28.4
+//   64 rows:  1: 55.9  2: 39.3  4: 32.8 (taken)  9: 35.6  32: 58.4
+//   256 rows: 1: 67.1 (taken)  2: 74.4  4: 75.8  7: 98.9
 int beam_strips(const gnn_beam_call* c, int n_sm) {
-  const int64_t rows = c->n_groups * c->beams, slots = kStripBlocks * (int64_t)n_sm, round = kStripThreads * kLaneElements;
+  const int64_t rows = c->n_groups * c->beams, round = kStripThreads * kLaneElements;
   const int64_t rounds = (c->vocab + round - 1) / round;
   int64_t best = 1, least = 0;
   for (int64_t s = 1; s <= std::min<int64_t>(kStripsMost, rounds); ++s) {
-    const int64_t time = (rows * s + slots - 1) / slots * ((rounds + s - 1) / s + 8);
+    const int64_t time = std::max<int64_t>(2, (rows * s + n_sm - 1) / n_sm) * ((rounds + s - 1) / s + 8);
     if (s == 1 || time < least) best = s, least = time;
   }
   return (int)best;
