@@ -28,6 +28,23 @@ def test_drawn_calls(seed):
            max_q=r.random() < 0.6)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("groups,beams,vocab,n", [(1, 2, 300001, 64), (1, 16, 140000, 33), (2, 1, 131072, 17), (1, 9, 200003, 7), (3, 5, 70001, 32)])
+def test_choices_of_rows_in_many_strips(dtype, groups, beams, vocab, n):
+    rows = groups * beams
+    g = torch.Generator().manual_seed(vocab)
+    x = torch.randn(rows, vocab, generator=g).to(dtype)
+    x[torch.rand(rows, vocab, generator=g) < 0.3] = -math.inf
+    _select(x, -torch.rand(rows, generator=g), beams, n)
+    few = torch.randint(0, 4, (rows, vocab), generator=g).to(dtype)          # ties: the lowest places win
+    few[:, :vocab // 3] = 0
+    _select(few, torch.zeros(rows), beams, n)
+    rare = torch.full((rows, vocab), -math.inf, dtype=dtype)                  # fewer candidates than places
+    rare[:, vocab - 5:] = 1.0
+    rare[0, vocab // 2] = 2.0
+    _select(rare, torch.zeros(rows), beams, n)
+
+
 @pytest.mark.parametrize("seed", range(25))
 def test_drawn_choices(seed):
     r = random.Random(seed)
