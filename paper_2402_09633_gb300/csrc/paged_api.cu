@@ -55,6 +55,9 @@ bool attend_ok(const gnn_pages* c, const gnn_paged_call* a) {
   return a->q.n_heads / c->k.n_heads <= 128;
 }
 
+int paged_chunks(int64_t n_seqs, int64_t n_groups) {
+  return (int)((n_seqs + kAttendThreads - 1) / kAttendThreads + (n_groups + kAttendThreads - 1) / kAttendThreads);
+}
 // How a call is cut into tiles, and where its parts lie in the workspace; the bytes that takes.
 struct PagedPlan { PagedGrid g; uint64_t bytes; unsigned blocks; };
 PagedPlan paged_plan(const gnn_pages* c, const gnn_paged_call* a, int n_sm) {
@@ -88,6 +91,7 @@ PagedPlan paged_plan(const gnn_pages* c, const gnn_paged_call* a, int n_sm) {
   g.sum_a = reinterpret_cast<float2*>(take(sums_a * 8));
   g.sum_b = reinterpret_cast<float2*>(take(sums_b * 8));
   g.group_rows = reinterpret_cast<int2*>(take((int64_t)a->n_groups * 8));
+  if (c->n_seqs > kPagedKept || a->n_groups > kAttendThreads) g.chunks = reinterpret_cast<int64_t*>(take((int64_t)paged_chunks(c->n_seqs, a->n_groups) * 8));
   g.first_a = reinterpret_cast<int2*>(take(n_a * 8));
   g.first_b = reinterpret_cast<int2*>(take(n_b * 8));
   return r;
@@ -119,14 +123,21 @@ bool paged_map(CUtensorMap* map, const gnn_heads& h, int64_t rows, int dtype, in
 template <typename T, int DP>
 cudaError_t launch_paged(const PagedParams& p, const PagedPlan& plan, const CUtensorMap* maps, cudaStream_t st) {
   cudaError_t err = allow_smem<paged_tile_kernel<T, DP>>(paged_smem_bytes<DP>());
+  if (err == cudaSuccess && plan.g.chunks)
+    err = launch_pdl(paged_weigh_kernel, (unsigned)paged_chunks(p.n_seqs, p.n_groups), kAttendThreads, 0, st, p, plan.g);
   if (err == cudaSuccess)
     err = launch_pdl(paged_tile_kernel<T, DP>, plan.blocks, kAttendThreads, paged_smem_bytes<DP>(), st, p, plan.g, maps[0], maps[1],
                      maps[2], maps[3], maps[4], maps[5]);
+  if (err != cudaSuccess) return err;
+  // One warp goes through a row's parts (up to one of every block) eight at a time; where rows are few, eight warps share a row's (8 rows
+  // over 32,768 keys, one key head: 56.8 -> 27.8 us).  Where the former does not find room for all rows at once, more warps
+  // with two parts each in flight do better (131,072 rows of up to three: 357 -> 298 us for the call; 1,024 rows of 38: 32.6 -> 38.1).
   const int64_t rows = (int64_t)p.n_q_rows * p.heads;
-  if (err == cudaSuccess)
-    err = launch_pdl(paged_join_kernel<T>, (unsigned)((rows + kPagedJoinWarps - 1) / kPagedJoinWarps), 32 * kPagedJoinWarps, 0, st, p,
-                     plan.g, (int)plan.blocks);
-  return err;
+  const unsigned blocks = (unsigned)((rows + kPagedJoinWarps - 1) / kPagedJoinWarps);
+  const int n = (int)plan.blocks;
+  if (rows <= 2 * n) return launch_pdl(paged_join_kernel<T, kPagedJoinSplit, 8, 1>, (unsigned)rows, 32 * kPagedJoinSplit, 0, st, p, plan.g, n);
+  if (rows <= 20 * n) return launch_pdl(paged_join_kernel<T, 1, 8, 1>, blocks, 32 * kPagedJoinWarps, 0, st, p, plan.g, n);
+  return launch_pdl(paged_join_kernel<T, 1, 2, 10>, blocks, 32 * kPagedJoinWarps, 0, st, p, plan.g, n);
 }
 
 bool beam_ok(const gnn_beam_call* c) {

@@ -32,6 +32,7 @@ struct PagedGrid {
   int pack;                          // sequences of a pack, a power of two; 1: a sequence may have several tiles
   int rows_a, rows_b;                // rows of a place
   int2* group_rows;                  // [group]: its first row and how many, as the first kernel found them
+  int64_t* chunks;                   // weights of kAttendThreads groups each, then of as many sequences; null where there are few of both
   int2 *first_a, *first_b;           // [ordinal]: the first thread block of an item, and how many have a part
   float *out_a, *out_b;              // [ordinal + thread block][2 places][rows][dim]
   float2 *sum_a, *sum_b;             // the same, [rows]: scaled maximum and sum
@@ -96,6 +97,22 @@ __device__ __forceinline__ int64_t paged_weight(const PagedParams& p, const Page
   return (int64_t)p.kv_heads * (w.twos + w.ones) * (w.blocks + kPagedCost);
 }
 
+// Of group i, or of the pack of sequence i on its first sequence's thread; all of a warp call it.
+__device__ __forceinline__ int64_t paged_weight_of(const PagedParams& p, const PagedGrid& g, bool own, int i, bool rows, bool* bad, PagedWork& w,
+                                                   PagedOwn& o) {
+  if (!own) {
+    if (i >= p.n_groups) return 0;
+    w = paged_group_work(p, g, i, bad);
+    if (rows) g.group_rows[i] = make_int2(w.q0, w.nq);
+    return paged_weight(p, w);
+  }
+  o = {p.n_q_rows, 0, 0, 0, 0, 0};
+  if (i < p.n_seqs) o = paged_own(p, i, bad);
+  int prefix;
+  w = paged_pack_work(g, o, &prefix);
+  return (threadIdx.x & 31 & (g.pack - 1)) == 0 ? paged_weight(p, w) : 0;
+}
+
 // Ordinals leave room for every item, whatever lies before it: no sum over the groups or sequences is needed.
 __device__ __forceinline__ int64_t paged_ordinal_a(const PagedGrid& g, int group, int q0) { return (int64_t)(q0 / (2 * g.tile_q)) + group; }
 __device__ __forceinline__ int64_t paged_ordinal_b(const PagedGrid& g, int pack, int q0) {
@@ -145,29 +162,28 @@ __device__ __forceinline__ PagedShare paged_share(const PagedParams& p, const Pa
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   constexpr int KEEP = kPagedKept / kAttendThreads;
   bool bad = false;
-  auto weight = [&](bool own, int i) {               // of a group, or of a pack, on its first sequence's thread
-    if (!own) {
-      if (i >= p.n_groups) return (int64_t)0;
-      const PagedWork w = paged_group_work(p, g, i, &bad);
-      if (i < kGroupsKept) s.shared[i] = w;
-      if (blockIdx.x == 0) g.group_rows[i] = make_int2(w.q0, w.nq);
-      return paged_weight(p, w);
-    }
-    PagedOwn o = {p.n_q_rows, 0, 0, 0, 0, 0};
-    if (i < p.n_seqs) o = paged_own(p, i, &bad);
-    if (i < kPagedKept) s.own[i] = o;
-    int prefix;
-    const PagedWork w = paged_pack_work(g, o, &prefix);
-    return (lane & (g.pack - 1)) == 0 ? paged_weight(p, w) : (int64_t)0;
+  auto weight = [&](bool own, int i) {               // and what is kept
+    PagedWork w;
+    PagedOwn o;
+    const int64_t n = paged_weight_of(p, g, own, i, blockIdx.x == 0 && !g.chunks, &bad, w, o);
+    if (own && i < kPagedKept) s.own[i] = o;
+    if (!own && i < min(p.n_groups, kGroupsKept)) s.shared[i] = w;
+    return n;
   };
   int64_t sum[2] = {0, 0}, kept[KEEP] = {};
-  // (groups from the last thread on: where there are few of both, other warps look at them)
-  for (int c = 0; c < p.n_groups; c += kAttendThreads) sum[0] += weight(false, c + kAttendThreads - 1 - tid);
+  const int group_chunks = (p.n_groups + kAttendThreads - 1) / kAttendThreads, seq_chunks = (p.n_seqs + kAttendThreads - 1) / kAttendThreads;
+  if (g.chunks) {
+    for (int c = tid; c < group_chunks; c += kAttendThreads) sum[0] += g.chunks[c];
+    for (int c = tid; c < seq_chunks; c += kAttendThreads) sum[1] += g.chunks[group_chunks + c];
+  } else {
+    // (groups from the last thread on: where there are few of both, other warps look at them)
+    if (p.n_groups > 0) sum[0] = weight(false, kAttendThreads - 1 - tid);
 #pragma unroll
-  for (int k = 0; k < KEEP; ++k)
-    if (k * kAttendThreads < p.n_seqs) sum[1] += kept[k] = weight(true, k * kAttendThreads + tid);
-  for (int c = kPagedKept; c < p.n_seqs; c += kAttendThreads) sum[1] += weight(true, c + tid);
-  if (bad && blockIdx.x == 0) atomicOr(p.err, DEV_ERR_INDEX_RANGE);
+    for (int k = 0; k < KEEP; ++k)
+      if (k * kAttendThreads < p.n_seqs) sum[1] += kept[k] = weight(true, k * kAttendThreads + tid);
+  }
+  if (bad && blockIdx.x == 0 && !g.chunks) atomicOr(p.err, DEV_ERR_INDEX_RANGE);
+  if (tid == 0) s.at = 0, s.before = LLONG_MAX;      // lengths that change under the kernel: no work
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
 #pragma unroll
@@ -193,17 +209,9 @@ __device__ __forceinline__ PagedShare paged_share(const PagedParams& p, const Pa
     r.before = r.end;
     return r;
   }
-  const int n = r.own ? p.n_seqs : p.n_groups;
-  for (int c = 0; c < n; c += kAttendThreads) {
-    int64_t w = 0;
-    if (r.own && c < kPagedKept) {
-#pragma unroll
-      for (int k = 0; k < KEEP; ++k)
-        if (c == k * kAttendThreads) w = kept[k];
-    } else {
-      w = weight(r.own, c + tid);
-    }
-    int64_t upto = w;
+  // Of a value of every thread: those up to this thread's, and all.
+  auto scan = [&](int64_t w, int64_t& upto, int64_t& all) {
+    upto = w;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
       const int64_t y = __shfl_up_sync(0xffffffffu, upto, d);
@@ -211,24 +219,76 @@ __device__ __forceinline__ PagedShare paged_share(const PagedParams& p, const Pa
     }
     if (lane == 31) s.scan[0][warp] = upto;
     __syncthreads();
-    int64_t chunk = 0;
+    all = 0;
     for (int x = 0; x < W; ++x) {
       if (x < warp) upto += s.scan[0][x];
-      chunk += s.scan[0][x];
+      all += s.scan[0][x];
     }
+  };
+  int64_t upto, part;
+  int c0 = 0;
+  if (g.chunks) {                                    // the chunk that the start is in
+    const int64_t* chunks = g.chunks + (r.own ? group_chunks : 0);
+    for (int c = 0, n = r.own ? seq_chunks : group_chunks; c < n; c += kAttendThreads) {
+      const int64_t w = c + tid < n ? chunks[c + tid] : 0, here = r.start - r.before;
+      scan(w, upto, part);
+      if (here >= upto - w && here < upto) {
+        s.at = c + tid;
+        s.before = r.before + upto - w;
+      }
+      __syncthreads();
+      if (here < part) break;
+      r.before += part;
+    }
+    c0 = s.at * kAttendThreads;
+    r.before = s.before;
+    __syncthreads();
+  }
+  for (int c = c0, n = r.own ? p.n_seqs : p.n_groups; c < n; c += kAttendThreads) {
+    int64_t w = 0;
+    if (r.own && !g.chunks) {
+#pragma unroll
+      for (int k = 0; k < KEEP; ++k)
+        if (c == k * kAttendThreads) w = kept[k];
+    } else {
+      w = weight(r.own, c + tid);
+    }
+    scan(w, upto, part);
     const int64_t here = r.start - r.before;
     if (here >= upto - w && here < upto) {
       s.at = r.own ? (c + tid) / g.pack : c + tid;
       s.before = r.before + upto - w;
     }
     __syncthreads();
-    if (here < chunk) break;
-    r.before += chunk;
+    if (here < part) break;
+    r.before += part;
   }
   r.at = s.at;
   r.before = s.before;
   __syncthreads();
   return r;
+}
+
+// Where there are many groups or sequences: their weights, kAttendThreads to a block, so that not every block of the next kernel looks at
+// all of them.  (4,096 groups of four sequences: 1.69 ms without it.)
+__global__ void __launch_bounds__(kAttendThreads) paged_weigh_kernel(const __grid_constant__ PagedParams p, const __grid_constant__ PagedGrid g) {
+  __shared__ int64_t sum_s[kAttendThreads / 32];
+  const int group_chunks = (p.n_groups + kAttendThreads - 1) / kAttendThreads, c = (int)blockIdx.x, tid = threadIdx.x;
+  const bool own = c >= group_chunks;
+  bool bad = false;
+  PagedWork w;
+  PagedOwn o;
+  pdl_wait();
+  pdl_trigger();
+  int64_t sum = paged_weight_of(p, g, own, (own ? c - group_chunks : c) * kAttendThreads + tid, true, &bad, w, o);
+  if (bad) atomicOr(p.err, DEV_ERR_INDEX_RANGE);
+#pragma unroll
+  for (int d = 16; d > 0; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+  if ((tid & 31) == 0) sum_s[tid / 32] = sum;
+  __syncthreads();
+  if (tid > 0) return;
+  for (int x = 1; x < kAttendThreads / 32; ++x) sum += sum_s[x];
+  g.chunks[c] = sum;
 }
 
 // Goes through a share, by one warp: part(work, own, group or pack, its item s, the item's blocks [b0, b1) that the share has,
@@ -257,11 +317,11 @@ __device__ __forceinline__ void paged_walk(const PagedParams& p, const PagedGrid
       bool bad = false;
       if (own) {
         seq = {p.n_q_rows, 0, 0, 0, 0, 0};
-        if (chunk0 + lane < n) seq = chunk0 + lane < kPagedKept ? s_bars.own[chunk0 + lane] : paged_own(p, chunk0 + lane, &bad);
+        if (chunk0 + lane < n) seq = !g.chunks && chunk0 + lane < kPagedKept ? s_bars.own[chunk0 + lane] : paged_own(p, chunk0 + lane, &bad);
         chunk = paged_pack_work(g, seq, &before);
       } else {
         chunk = PagedWork{};
-        if (chunk0 + lane < n) chunk = chunk0 + lane < kGroupsKept ? s_bars.shared[chunk0 + lane] : paged_group_work(p, g, chunk0 + lane, &bad);
+        if (chunk0 + lane < n) chunk = !g.chunks && chunk0 + lane < kGroupsKept ? s_bars.shared[chunk0 + lane] : paged_group_work(p, g, chunk0 + lane, &bad);
       }
     }
     const int from = first - chunk0;
@@ -831,17 +891,19 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
 }
 
 // ------------------------------------------------------------------ join
-constexpr int kPagedJoinWarps = 4;
+constexpr int kPagedJoinWarps = 4, kPagedJoinSplit = 8;
 
 // A row of a head to a warp: the parts of its shared and of its own keys into one, four elements to a lane.  Bound by its chain of
 // dependent loads, so each step's go out together: what is known of the sequence and group that the row would be of if all were as
 // large (others are searched for), first blocks, sums, outputs.
-template <typename T>
-__global__ void __launch_bounds__(32 * kPagedJoinWarps) paged_join_kernel(const __grid_constant__ PagedParams p,
+template <typename T, int SPLIT, int PARTS, int BLOCKS>
+__global__ void __launch_bounds__(32 * (SPLIT > 1 ? SPLIT : kPagedJoinWarps), BLOCKS) paged_join_kernel(const __grid_constant__ PagedParams p,
                                                                               const __grid_constant__ PagedGrid g, int blocks) {
-  __shared__ float q_s[kPagedJoinWarps][128];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t at = (int64_t)blockIdx.x * kPagedJoinWarps + warp;
+  constexpr int WARPS = SPLIT > 1 ? SPLIT : kPagedJoinWarps;       // warps of a block that meet at a barrier have one row
+  __shared__ __align__(16) float q_s[WARPS][128];
+  __shared__ int odd_s[WARPS];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = warp % SPLIT;
+  const int64_t at = (int64_t)blockIdx.x * (WARPS / SPLIT) + warp / SPLIT;
   const int row = (int)paged_divide(at, p.heads), head = (int)(at - (int64_t)row * p.heads), kv = head / g.group;
   int seq = min((int)((float)row / (float)p.n_q_rows * (float)p.n_seqs), p.n_seqs - 1);
   int group = p.n_groups > 0 ? min((int)((float)seq / (float)p.n_seqs * (float)p.n_groups), p.n_groups - 1) : -1;
@@ -890,7 +952,7 @@ __global__ void __launch_bounds__(32 * kPagedJoinWarps) paged_join_kernel(const 
     paged_attend_row<T>(p, sq, seq, i, head, q_s[warp]);
   };
   if (sq.len - sq.nq < sq.shared) {                  // a sequence with queries among the shared positions, or without keys
-    slowly();
+    if (sub == 0) slowly();
     return;
   }
   // where the row's parts lie: of the shared keys, [0, na), and of its own, [na, na + nb)
@@ -936,13 +998,15 @@ __global__ void __launch_bounds__(32 * kPagedJoinWarps) paged_join_kernel(const 
       l = fmaf(s.y, z, l);
       odd = odd || (k0 + lane >= na && !(fabsf(s.y) < INFINITY));
     }
-    // those that count, eight at a time with their loads together
-    for (uint32_t left = __ballot_sync(0xffffffffu, z != 0.f); left;) {
-      float4 x[8];
-      float f[8];
-      bool own[8];
+    // those that count, some at a time with their loads together
+    uint32_t left = __ballot_sync(0xffffffffu, z != 0.f);
+    if (SPLIT > 1) left &= (0xffffffffu / ((1u << SPLIT) - 1)) << sub;             // every SPLIT-th
+    while (left) {
+      float4 x[PARTS];
+      float f[PARTS];
+      bool own[PARTS];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < PARTS; ++e) {
         const int k = left ? __ffs(left) - 1 : 0;
         f[e] = __shfl_sync(0xffffffffu, z, k);
         if (left == 0) f[e] = 0.f;
@@ -953,7 +1017,7 @@ __global__ void __launch_bounds__(32 * kPagedJoinWarps) paged_join_kernel(const 
         left &= left - 1;
       }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < PARTS; ++e) {
         o.x = fmaf(x[e].x, f[e], o.x); o.y = fmaf(x[e].y, f[e], o.y);
         o.z = fmaf(x[e].z, f[e], o.z); o.w = fmaf(x[e].w, f[e], o.w);
         odd = odd || (own[e] && !(fabsf(x[e].x) + fabsf(x[e].y) + fabsf(x[e].z) + fabsf(x[e].w) < INFINITY));
@@ -962,11 +1026,25 @@ __global__ void __launch_bounds__(32 * kPagedJoinWarps) paged_join_kernel(const 
   }
 #pragma unroll
   for (int d = 16; d > 0; d /= 2) l += __shfl_xor_sync(0xffffffffu, l, d);
+  odd = __any_sync(0xffffffffu, odd);
+  if (SPLIT > 1) {                                   // a row's warps have all left before here, or none
+    if (have) *reinterpret_cast<float4*>(&q_s[warp][4 * lane]) = o;
+    if (lane == 0) odd_s[warp] = odd;
+    __syncthreads();
+    if (sub != 0) return;
+#pragma unroll
+    for (int w = 1; w < SPLIT; ++w) {
+      const float4 x = *reinterpret_cast<const float4*>(&q_s[warp + w][have ? 4 * lane : 0]);
+      o = make_float4(o.x + x.x, o.y + x.y, o.z + x.z, o.w + x.w);
+      odd = odd || odd_s[warp + w];
+    }
+    __syncwarp();
+  }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   o = l == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
   // A weight of zero times a value that is not finite is NaN.  A pack's keys, and new rows, are seen by some of its queries only, so
   // a row whose part of its own keys is not finite is done again, key by visible key; shared keys are seen by all.
-  if (__any_sync(0xffffffffu, odd)) {
+  if (odd) {
     slowly();
     return;
   }

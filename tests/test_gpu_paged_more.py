@@ -45,6 +45,19 @@ def test_choices_of_rows_in_many_strips(dtype, groups, beams, vocab, n):
     _select(rare, torch.zeros(rows), beams, n)
 
 
+@pytest.mark.parametrize("seed,n,groups", [(0, 800, 3), (1, 2000, 700), (2, 500, 450), (3, 1500, 0)])
+def test_many_sequences(seed, n, groups):
+    """More than a thread block looks at by itself, and more rows than the join has warps."""
+    r = random.Random(seed)
+    hyps = [r.choice([0, 1, 2, 3]) for _ in range(groups)] if groups > 3 else [r.randint(1, 200) for _ in range(groups)]
+    while sum(hyps) > n:
+        hyps[r.randrange(groups)] = 0
+    shared = [r.choice([0, 1, r.randint(1, 150)]) for _ in hyps]
+    nq = [r.choice([0, 1, 1, 2]) for _ in range(n)]
+    own = [max(q, r.randint(0, 40)) for q in nq]
+    _paged(r.choice([BF16, F16]), nq, own, hyps, shared, 6, 2, 64, 16, seed=seed)
+
+
 @pytest.mark.parametrize("seed", range(25))
 def test_drawn_choices(seed):
     r = random.Random(seed)

@@ -9,6 +9,7 @@ from tests import host_cuda
 
 MAIN = r"""
 #include "ptx.cuh"
+#include <climits>
 #include <cmath>
 using std::max;
 using std::min;
@@ -18,12 +19,14 @@ inline int64_t __shfl_up_sync(unsigned m, int64_t x, int by) {
   const uint32_t lo = __shfl_up_sync(m, (uint32_t)x, by), hi = __shfl_up_sync(m, (uint32_t)(x >> 32), by);
   return (int64_t)((uint64_t)hi << 32 | lo);
 }
+#define __grid_constant__
+namespace gnn { inline void pdl_trigger() {} }
 #include "shares.cuh"
 using namespace gnn;
 // out: own, index, item, b0, b1, first thread block, parts, ordinal, thread block, blocks, both
 extern "C" int walk(int grid, int n_q, int n_seqs, int n_groups, const int* q_start, const int* kv_len, const int* group_start,
                     const int* shared, int max_q, int kv_heads, int group, int pack, int page, int width, long long* out, int most, unsigned* err,
-                    long long* share_out) {
+                    long long* share_out, int counted) {
   PagedParams p = {};
   p.q_start = q_start; p.kv_len = kv_len; p.group_start = group_start; p.shared_len = shared;
   p.n_q_rows = n_q; p.n_seqs = n_seqs; p.n_groups = n_groups; p.width = width; p.max_q = max_q;
@@ -31,10 +34,15 @@ extern "C" int walk(int grid, int n_q, int n_seqs, int n_groups, const int* q_st
   while (1 << p.shift < page) ++p.shift;
   PagedGrid g = {};
   g.group = group; g.tile_q = kTileQ / group; g.box = min(page, kKeys); g.pack = pack;
+  const int n_chunks = (n_seqs + kAttendThreads - 1) / kAttendThreads + (n_groups + kAttendThreads - 1) / kAttendThreads;
+  std::vector<int64_t> chunks(n_chunks, -1);
+  if (n_seqs > kPagedKept || n_groups > kAttendThreads || counted) g.chunks = chunks.data();
   static PagedBars bars;
   std::vector<int2> group_rows(n_groups + 1);
   g.group_rows = group_rows.data();
   int n = 0;
+  gridDim.x = n_chunks;
+  if (g.chunks) host::launch(n_chunks, kAttendThreads, [&] { paged_weigh_kernel(p, g); });
   gridDim.x = grid;
   host::launch(grid, kAttendThreads, [&] {
     if (threadIdx.x == 0) { bars.at = -1000000; bars.before = -7; }           // shared memory holds anything at first
@@ -76,7 +84,7 @@ def lib(tmp_path_factory):
     text += cut(tile, "// Block b's share of the list", "template <typename T, int DP>\n__global__")
     lib = host_cuda.compile_host(tmp_path_factory.mktemp("host"), MAIN, [("shares.cuh", text + "}\n")])
     vp, i = ctypes.c_void_p, ctypes.c_int
-    lib.walk.argtypes = [i] * 4 + [vp] * 4 + [i] * 6 + [vp, i, vp, vp]
+    lib.walk.argtypes = [i] * 4 + [vp] * 4 + [i] * 6 + [vp, i, vp, vp, i]
     lib.walk.restype = i
     return lib
 
@@ -88,7 +96,7 @@ def _pack(max_q, group):
     return n
 
 
-def _walk(lib, grid, nq, kv_len, groups, shared, kv_heads, group, page, max_q=None, width=None, n_q=None, q_start=None):
+def _walk(lib, grid, nq, kv_len, groups, shared, kv_heads, group, page, max_q=None, width=None, n_q=None, q_start=None, counted=0):
     i32 = lambda x: np.ascontiguousarray(x, dtype=np.int32)  # noqa: E731
     q_start = i32(np.concatenate([[0], np.cumsum(nq)])) if q_start is None else i32(q_start)
     kv_len, groups, shared = i32(kv_len), i32(groups), i32(shared)
@@ -98,7 +106,7 @@ def _walk(lib, grid, nq, kv_len, groups, shared, kv_heads, group, page, max_q=No
     at = lambda a: a.ctypes.data_as(ctypes.c_void_p)         # noqa: E731
     n = lib.walk(grid, n_q, kv_len.size, shared.size, at(q_start), at(kv_len), at(groups), at(shared),
                  int(max(nq)) if max_q is None else max_q, kv_heads, group,
-                 _pack(int(max(nq)) if max_q is None else max_q, group), page, width, at(out), len(out), at(err), at(share))
+                 _pack(int(max(nq)) if max_q is None else max_q, group), page, width, at(out), len(out), at(err), at(share), counted)
     return out[:n], int(err[0]), int(share[0]), n_q
 
 
@@ -143,6 +151,7 @@ def test_every_block_once(lib, grid, seed):
     kv_len = part + own
     out, err, share, n_q = _walk(lib, grid, nq, kv_len, cuts, shared, kv_heads, group, page)
     assert err == 0
+    assert np.array_equal(out, _walk(lib, grid, nq, kv_len, cuts, shared, kv_heads, group, page, counted=1)[0])
     pack = _pack(int(max(nq)), group)
     items = _check(out, share, grid, _bounds(n_q, n, len(shared), kv_heads, group, pack))
     tile_q = 128 // group
@@ -169,6 +178,8 @@ def test_offsets_that_contradict_each_other_stay_inside(lib, bad):
     assert _walk(lib, 13, **a)[1] == 0
     out, err, share, n_q = _walk(lib, 13, **{**a, **bad})
     assert err == 1
+    again = _walk(lib, 13, **{**a, **bad}, counted=1)
+    assert np.array_equal(out, again[0]) and again[1] == 1
     bound = _bounds(12, 4, 2, 2, 4, _pack(bad.get("max_q", 3), 4))
     assert all(0 <= r[7] < bound[r[0]] and r[3] < r[4] for r in out.tolist())
 
@@ -176,3 +187,25 @@ def test_offsets_that_contradict_each_other_stay_inside(lib, bad):
 def test_no_work(lib):
     out, err, share, n_q = _walk(lib, 20, [0, 0, 1], [5, 0, 0], [0, 3], [0], 2, 4, 16, n_q=1, max_q=1)
     assert len(out) == 0 and err == 0
+
+
+@pytest.mark.parametrize("n,n_groups", [(400, 1500), (5000, 0), (2500, 400), (769, 1), (770, 385)])
+def test_many_sequences_and_groups(lib, n, n_groups):
+    rng = np.random.default_rng(n)
+    nq = rng.integers(0, 3, n)
+    cuts = np.sort(np.concatenate([[0], rng.integers(0, n + 1, max(0, n_groups - 1)), [n]])) if n_groups else np.array([0])
+    shared = rng.integers(0, 300, n_groups)
+    part = np.zeros(n, int)
+    for g, s in enumerate(shared):
+        part[cuts[g]:cuts[g + 1]] = s
+    kv_len = part + np.maximum(rng.integers(0, 100, n), nq)
+    out, err, share, n_q = _walk(lib, 19, nq, kv_len, cuts, shared, 2, 4, 16)
+    assert err == 0
+    items = _check(out, share, 19, _bounds(n_q, n, n_groups, 2, 4, _pack(2, 4)))
+    with_keys = {(0, g, i) for g, s in enumerate(shared) if s for i in range(2 * (-(-int(nq[cuts[g]:cuts[g + 1]].sum()) // 32)))}
+    packs = _pack(2, 4)
+    pieces = np.where(nq > 0, -(-(kv_len - part // 16 * 16) // 16), 0)
+    with_keys |= {(1, k, i) for k in range(-(-n // packs)) if pieces[k * packs:(k + 1) * packs].sum() for i in range(2)}
+    # (two tiles of a group are one item)
+    assert {k for k in items if k[0]} == {k for k in with_keys if k[0]} and {k for k in items if not k[0]} <= {k for k in with_keys if not k[0]}
+    assert {k[:2] for k in items} == {k[:2] for k in with_keys}
