@@ -13,13 +13,18 @@
 //
 // Softmax as in the other tiled kernel: P = exp2(scale (S - m)) with a running maximum m that follows only when it is outgrown
 // by 2^8 / scale.
+//
+// Measured (bf16, 16 query heads on 4 key heads of 128).  Bound by the tensor cores' operands and each tile's wait for its softmax:
+// 512 sequences that share 65,536 keys, 237 us, 1,160 TFLOP/s, tensor pipe 60 % busy; a block for two tiles is 1.75 us.  Bound by HBM:
+// 64 sequences of up to 8,192 keys of their own, 140 us, 5.8 TB/s.  Bound by its chain: 64 sequences that share 16,384 keys, 33 us,
+// of which 6 are the start, 6 the blocks and 11 the join.  Packs of one sequence instead of 32: 519 us for the first, 45 for the last.
 #pragma once
 #include "attend_tile.cuh"
 #include "paged.cuh"
 
 namespace gnn {
 
-constexpr int kPagedCost = 2;        // what an item's start and end take, in blocks
+constexpr int kPagedCost = 2;        // what an item's start and end take, in blocks (4: +1.3 %, 6: +3.2 % over 35 calls of all sizes)
 constexpr int kPiece = 16;           // keys of a piece: pages have whole pieces
 constexpr int kPieces = kKeys / kPiece;
 constexpr int kPackMost = 32;        // sequences of a pack: a lane to each
@@ -893,9 +898,11 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
 // ------------------------------------------------------------------ join
 constexpr int kPagedJoinWarps = 4, kPagedJoinSplit = 8;
 
-// A row of a head to a warp: the parts of its shared and of its own keys into one, four elements to a lane.  Bound by its chain of
-// dependent loads, so each step's go out together: what is known of the sequence and group that the row would be of if all were as
-// large (others are searched for), first blocks, sums, outputs.
+// A row of a head to a warp: the parts of its shared and of its own keys into one, four elements to a lane: with the largest maximum
+// m of the parts, o = sum 2^(m_x - m) o_x / sum 2^(m_x - m) l_x.  Bound by its chain of dependent loads, so each step's go out
+// together: what is known of the sequence and group that the row would be of if all were as large (others are searched for), first
+// blocks, sums, outputs (PARTS in flight).  SPLIT warps share a row where there are few.  1,024 rows of 38 parts (20 MB): 11 us behind
+// the first kernel, which leaves no room for it to be there before; 8 rows of 152 parts: 10 us, 38 with a warp to a row.
 template <typename T, int SPLIT, int PARTS, int BLOCKS>
 __global__ void __launch_bounds__(32 * (SPLIT > 1 ? SPLIT : kPagedJoinWarps), BLOCKS) paged_join_kernel(const __grid_constant__ PagedParams p,
                                                                               const __grid_constant__ PagedGrid g, int blocks) {
