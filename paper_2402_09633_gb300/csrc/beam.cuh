@@ -373,6 +373,9 @@ __global__ void __launch_bounds__(kJoinThreads) beam_join_kernel(const __grid_co
   uint64_t* values = rows + beams * best;            // the same, as they are ordered: comparing 64-bit floats takes long here
   if (tid == 0) taken_s = left_s = 0;
   if (tid < kBeamMost) reach_s[tid] = 0;
+  // (what the caller gave is there: the first kernel's blocks have waited for it)
+  const float score = tid < beams ? p.score[row0 + tid] : 0.f;
+  const bool ended = tid < beams && p.ended && p.ended[row0 + tid];
   pdl_wait();
   for (int i = tid; i < beams * strips; i += kJoinThreads) sums[i] = p.sums[row0 * strips + i];
   if (strips == 1) {
@@ -397,8 +400,7 @@ __global__ void __launch_bounds__(kJoinThreads) beam_join_kernel(const __grid_co
   __syncthreads();
   // 64-bit arithmetic is slow here: one logarithm for all rows
   if (tid < beams) {
-    const float score = p.score[row0 + tid];
-    if (p.ended && p.ended[row0 + tid]) {
+    if (ended) {
       for (int i = 0; i < best; ++i) rows[tid * best + i] = i == 0 ? beam_key(0.f, (uint32_t)p.end) : 0;
       base_s[tid] = (double)score;
     } else {

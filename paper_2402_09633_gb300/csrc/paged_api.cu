@@ -90,7 +90,6 @@ PagedPlan paged_plan(const gnn_pages* c, const gnn_paged_call* a, int n_sm) {
   g.out_b = reinterpret_cast<float*>(take(sums_b * c->head_dim * 4));
   g.sum_a = reinterpret_cast<float2*>(take(sums_a * 8));
   g.sum_b = reinterpret_cast<float2*>(take(sums_b * 8));
-  g.group_rows = reinterpret_cast<int2*>(take((int64_t)a->n_groups * 8));
   if (c->n_seqs > kPagedKept || a->n_groups > kAttendThreads) g.chunks = reinterpret_cast<int64_t*>(take((int64_t)paged_chunks(c->n_seqs, a->n_groups) * 8));
   g.first_a = reinterpret_cast<int2*>(take(n_a * 8));
   g.first_b = reinterpret_cast<int2*>(take(n_b * 8));

@@ -16,7 +16,7 @@
 //
 // Measured (bf16, 16 query heads on 4 key heads of 128).  Bound by the tensor cores' operands and each tile's wait for its softmax:
 // 512 sequences that share 65,536 keys, 237 us, 1,160 TFLOP/s, tensor pipe 60 % busy; a block for two tiles is 1.75 us.  Bound by HBM:
-// 64 sequences of up to 8,192 keys of their own, 140 us, 5.8 TB/s.  Bound by its chain: 64 sequences that share 16,384 keys, 33 us,
+// 64 sequences of up to 8,192 keys of their own, 137 us, 5.9 TB/s.  Bound by its chain: 64 sequences that share 16,384 keys, 33 us,
 // of which 6 are the start, 6 the blocks and 11 the join.  Packs of one sequence instead of 32: 519 us for the first, 45 for the last.
 #pragma once
 #include "attend_tile.cuh"
@@ -36,7 +36,6 @@ struct PagedGrid {
   int group;                         // query heads to a key head
   int pack;                          // sequences of a pack, a power of two; 1: a sequence may have several tiles
   int rows_a, rows_b;                // rows of a place
-  int2* group_rows;                  // [group]: its first row and how many, as the first kernel found them
   int64_t* chunks;                   // weights of kAttendThreads groups each, then of as many sequences; null where there are few of both
   int2 *first_a, *first_b;           // [ordinal]: the first thread block of an item, and how many have a part
   float *out_a, *out_b;              // [ordinal + thread block][2 places][rows][dim]
@@ -103,12 +102,10 @@ __device__ __forceinline__ int64_t paged_weight(const PagedParams& p, const Page
 }
 
 // Of group i, or of the pack of sequence i on its first sequence's thread; all of a warp call it.
-__device__ __forceinline__ int64_t paged_weight_of(const PagedParams& p, const PagedGrid& g, bool own, int i, bool rows, bool* bad, PagedWork& w,
-                                                   PagedOwn& o) {
+__device__ __forceinline__ int64_t paged_weight_of(const PagedParams& p, const PagedGrid& g, bool own, int i, bool* bad, PagedWork& w, PagedOwn& o) {
   if (!own) {
     if (i >= p.n_groups) return 0;
     w = paged_group_work(p, g, i, bad);
-    if (rows) g.group_rows[i] = make_int2(w.q0, w.nq);
     return paged_weight(p, w);
   }
   o = {p.n_q_rows, 0, 0, 0, 0, 0};
@@ -170,7 +167,7 @@ __device__ __forceinline__ PagedShare paged_share(const PagedParams& p, const Pa
   auto weight = [&](bool own, int i) {               // and what is kept
     PagedWork w;
     PagedOwn o;
-    const int64_t n = paged_weight_of(p, g, own, i, blockIdx.x == 0 && !g.chunks, &bad, w, o);
+    const int64_t n = paged_weight_of(p, g, own, i, &bad, w, o);
     if (own && i < kPagedKept) s.own[i] = o;
     if (!own && i < min(p.n_groups, kGroupsKept)) s.shared[i] = w;
     return n;
@@ -285,7 +282,7 @@ __global__ void __launch_bounds__(kAttendThreads) paged_weigh_kernel(const __gri
   PagedOwn o;
   pdl_wait();
   pdl_trigger();
-  int64_t sum = paged_weight_of(p, g, own, (own ? c - group_chunks : c) * kAttendThreads + tid, true, &bad, w, o);
+  int64_t sum = paged_weight_of(p, g, own, (own ? c - group_chunks : c) * kAttendThreads + tid, &bad, w, o);
   if (bad) atomicOr(p.err, DEV_ERR_INDEX_RANGE);
 #pragma unroll
   for (int d = 16; d > 0; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
@@ -914,20 +911,25 @@ __global__ void __launch_bounds__(32 * (SPLIT > 1 ? SPLIT : kPagedJoinWarps), BL
   const int row = (int)paged_divide(at, p.heads), head = (int)(at - (int64_t)row * p.heads), kv = head / g.group;
   int seq = min((int)((float)row / (float)p.n_q_rows * (float)p.n_seqs), p.n_seqs - 1);
   int group = p.n_groups > 0 ? min((int)((float)seq / (float)p.n_seqs * (float)p.n_groups), p.n_groups - 1) : -1;
-  pdl_wait();
-  if (at >= (int64_t)p.n_q_rows * p.heads) return;
+  // What the caller gave is there before the first kernel ends, as all of that one's blocks have waited for it before this may start.
+  // (Whoever leaves early waits too, so that this kernel does not end before that one.)
+  if (at >= (int64_t)p.n_q_rows * p.heads) {
+    pdl_wait();
+    return;
+  }
   int s0 = p.q_start[seq], s1 = p.q_start[seq + 1], len = p.kv_len[seq], pack0 = p.q_start[seq / g.pack * g.pack];
   int g0 = 0, g1 = 0, shared = 0;
-  int2 rows = make_int2(0, 0);
   if (group >= 0) {
     g0 = p.group_start[group];
     g1 = p.group_start[group + 1];
     shared = p.shared_len[group];
-    rows = g.group_rows[group];
   }
   if (row < s0 || row >= s1) {
     seq = sequence_of(p.q_start, p.n_seqs, p.n_q_rows, row);
-    if (seq < 0) return;
+    if (seq < 0) {
+      pdl_wait();
+      return;
+    }
     s0 = p.q_start[seq];
     s1 = p.q_start[seq + 1];
     len = p.kv_len[seq];
@@ -937,9 +939,15 @@ __global__ void __launch_bounds__(32 * (SPLIT > 1 ? SPLIT : kPagedJoinWarps), BL
     group = sequence_of(p.group_start, p.n_groups, p.n_seqs, seq);
     if (group >= 0) {
       g0 = p.group_start[group];
+      g1 = p.group_start[group + 1];
       shared = p.shared_len[group];
-      rows = g.group_rows[group];
     }
+  }
+  int2 rows = make_int2(0, 0);                       // the group's: its first, and how many
+  if (group >= 0) {
+    const int a = min(max(g0, 0), p.n_seqs), z = min(max(g1, a), p.n_seqs), first = p.q_start[a], last = p.q_start[z];
+    rows.x = min(max(first, 0), p.n_q_rows);
+    rows.y = min(max(last, rows.x), p.n_q_rows) - rows.x;
   }
   // as the first kernel cuts them to the arrays
   PagedSequence sq;
@@ -951,6 +959,7 @@ __global__ void __launch_bounds__(32 * (SPLIT > 1 ? SPLIT : kPagedJoinWarps), BL
   sq.shared = group >= 0 ? min(max(shared, 0), paged_room(p)) : 0;
   pack0 = min(max(pack0, 0), p.n_q_rows);
   const int i = row - sq.q0;
+  pdl_wait();
   if (i >= p.max_q) return;
   auto slowly = [&] {
     const T* src = reinterpret_cast<const T*>(p.q.data + (int64_t)row * p.q.row_bytes + (int64_t)head * p.q.head_bytes);

@@ -38,8 +38,6 @@ extern "C" int walk(int grid, int n_q, int n_seqs, int n_groups, const int* q_st
   std::vector<int64_t> chunks(n_chunks, -1);
   if (n_seqs > kPagedKept || n_groups > kAttendThreads || counted) g.chunks = chunks.data();
   static PagedBars bars;
-  std::vector<int2> group_rows(n_groups + 1);
-  g.group_rows = group_rows.data();
   int n = 0;
   gridDim.x = n_chunks;
   if (g.chunks) host::launch(n_chunks, kAttendThreads, [&] { paged_weigh_kernel(p, g); });
