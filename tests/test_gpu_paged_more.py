@@ -184,6 +184,34 @@ def test_a_graph_is_replayed_with_other_lengths_pages_and_groups():
     assert cache.status() == 0
 
 
+def test_a_graph_of_many_sequences_is_replayed_with_other_lengths():
+    """Their weights are a kernel's of their own; calls that share the graph's stream write lengths right before it."""
+    from paper_2402_09633_gb300 import PagedCache
+    page, H, K, D, n = 16, 6, 2, 64, 900
+    table, pages = _table(n, 4, seed=5)
+    k, v = (_rand(pages * page, K, D, dtype=BF16, seed=s) for s in (1, 2))
+    q = _rand(n, H, D, dtype=BF16, seed=3)
+    length, groups, shared = _i32([50] * n), _i32([0, 300, 900]), _i32([10, 20])
+    cache = PagedCache(k.cuda(), v.cuda(), table.cuda(), length, page)
+    dq, each = q.cuda(), torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        cache.attend(dq, each, groups=groups, shared=shared, max_q=1)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = cache.attend(dq, each, groups=groups, shared=shared, max_q=1)
+    r = random.Random(1)
+    for cut, parts in (([0, 300, 900], [10, 20]), ([0, 899, 900], [33, 0]), ([5, 5, 450], [40, 17])):
+        lengths = [r.randint(max(parts) + 1, 64) for _ in range(n)]
+        length.copy_(_i32(lengths))
+        groups.copy_(_i32(cut))
+        shared.copy_(_i32(parts))
+        graph.replay()
+        P.check_attention(out.cpu(), q, k, v, table, lengths, page, list(range(n + 1)), cut, parts, 1 / math.sqrt(D))
+    assert cache.status() == 0
+
+
 def test_append_of_more_rows_than_the_offsets_say():
     from paper_2402_09633_gb300 import PagedCache, Rotary, binding
     k = _rand(64, 1, 64, dtype=F32, seed=1)
