@@ -605,7 +605,9 @@ int gnn_paged_attend(const gnn_pages* pages, const gnn_paged_call* call, gnn_str
  * (hypothesis, token): out_scores (value), out_parents (hypothesis, 0 .. beams - 1 within the group), out_tokens, each
  * [n_groups * best].  A hypothesis that has ended (ended[b] != 0) has one continuation: token end_token at scores[b]; its
  * logits are not read.  A value of -inf is no continuation; a row whose logits hold NaN or +inf, or whose score is
- * NaN, has none.  Where there are fewer than `best`, the rest is -inf, parent 0, token -1.
+ * NaN, has none.  Where there are fewer than `best`, the rest is -inf, parent 0, token -1.  Logits may have any finite magnitude:
+ * large negative numbers (masks) weigh nothing beside others, and a row of nothing else is an even choice.  (A value that is chosen
+ * and lies below what fp32 holds comes out as -inf, with its parent and token.)
  * Values are held and compared to about 1e-7 (their order within a row is that of the logits, exactly).
  *   dtype, logits    of any gnn_dtype, device [n_groups * beams, vocab], row_stride elements apart, aligned to elements
  *   scores           device float32 [n_groups * beams];  ended  device uint8 [n_groups * beams], or NULL

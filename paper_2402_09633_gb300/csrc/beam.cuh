@@ -23,7 +23,10 @@ constexpr float kLog2e = 1.44269504f;
 constexpr int kStripThreads = 256, kStripBlocks = 4;         // and blocks to an SM
 constexpr int kStripsMost = 32;      // strips of a row: at most one to a lane of the warp that joins them
 
-struct alignas(16) BeamSum { double s; float r; };    // the sum of 2^(x log2 e - r) over a strip
+// A strip's sum of 2^(x log2 e - r); or, where its largest element is `far`, past kBeamFar, of 2^((x - r) log2 e) with r that element.
+struct alignas(16) BeamSum { double s; float r; int far; };
+// Up to here x log2 e is rounded by 1/16 at most, so that its whole part serves as a reference.
+constexpr float kBeamFar = 1048576.f;
 struct BeamParams {
   const void* x;                     // [groups * beams, vocab]
   int64_t stride;                    // elements
@@ -121,11 +124,34 @@ template <typename T> constexpr int strip_pieces() { return kLaneElements * (int
 template <typename T> constexpr int strip_stage() { return (32 * strip_pieces<T>() + 1) * 16; }    // and the one that rows which start between two reach into
 template <typename T> constexpr int strip_smem() { return kStripThreads / 32 * strip_stages<T>() * strip_stage<T>(); }
 
+// A thread's share of the sum of 2^((x - top) log2 e) over its block's strip.  Finds the strip by itself, so that the kernel keeps nothing for it.
+template <typename T>
+__device__ __noinline__ double beam_far_sum(const BeamParams& p, float top) {
+  constexpr int VEC = 16 / sizeof(T);
+  const int64_t row = blockIdx.x / (unsigned)p.strips, strip = blockIdx.x - row * p.strips;
+  const int64_t pieces = ((int64_t)p.vocab + VEC - 1) / VEC, warps = kStripThreads / 32, per = (pieces + p.strips * warps - 1) / (p.strips * warps);
+  const int64_t a = strip * warps * per * VEC, z = min((int64_t)p.vocab, a + warps * per * VEC);
+  const T* x = static_cast<const T*>(p.x) + row * p.stride;
+  double sum = 0.;
+  for (int64_t i = a + threadIdx.x; i < z; i += kLaneElements * kStripThreads) {
+    float some = 0.f;
+#pragma unroll 4
+    for (int e = 0; e < kLaneElements; ++e) {
+      const int64_t at = i + e * kStripThreads;
+      if (at < z) some += exp2_approx((to_f(x[at]) - top) * kLog2e);
+    }
+    sum += some;
+  }
+  return sum;
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kStripThreads, kStripBlocks) beam_strip_kernel(const __grid_constant__ BeamParams p) {
   constexpr int VEC = 16 / sizeof(T), P = strip_pieces<T>(), N = kLaneElements, WARPS = kStripThreads / 32, STAGE = strip_stage<T>(), STAGES = strip_stages<T>();
   // Sums are of 2^(c x - r) with c = log2 e rounded, and their logarithm is divided by c again: that leaves 1.3e-8 of the weights'
-  // entropy as an error, where c is off by 1.3e-8.  r is a whole number, so that joining sums rounds nothing.
+  // entropy as an error, where c is off by 1.3e-8.  r is a whole number, so that joining sums rounds nothing.  Finite elements far below
+  // zero (masks) have the reference of -kBeamFar, beside which they weigh nothing.  A strip whose largest element is past kBeamFar on either
+  // side is summed up once more at its end, with that element taken off before the product is rounded.
   extern __shared__ __align__(16) uint8_t strip_ring[];
   __shared__ uint64_t list_s[WARPS][kBeamMost];      // at first what is held back
   __shared__ float high_s[WARPS];
@@ -172,7 +198,7 @@ __global__ void __launch_bounds__(kStripThreads, kStripBlocks) beam_strip_kernel
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
 
-  float m = -INFINITY, r = 0.f, s = 0.f;
+  float m = -kBeamFar, r = ceilf(-kBeamFar * kLog2e), s = 0.f;
   WarpList list = {0, 0};
   float least = -FLT_MAX;                            // what candidates are not below
   int held = 0;                                      // of them in list_s
@@ -227,7 +253,7 @@ __global__ void __launch_bounds__(kStripThreads, kStripBlocks) beam_strip_kernel
     high = fmaxf(high, v[N - 1]);
     if (high > m) {
       const float to = ceilf(high * kLog2e);
-      if (m > -INFINITY) s *= power2(r - to);
+      s *= power2(r - to);
       m = high;
       r = to;
     }
@@ -307,7 +333,7 @@ __global__ void __launch_bounds__(kStripThreads, kStripBlocks) beam_strip_kernel
   if (lane < best) list_s[warp][lane] = list.a;
   if (lane + 32 < best) list_s[warp][lane + 32] = list.z;
   // the threads' sums
-  float high = m == -INFINITY ? -INFINITY : r;
+  float high = r;
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, d));
   if (lane == 0) high_s[warp] = high;
@@ -315,8 +341,17 @@ __global__ void __launch_bounds__(kStripThreads, kStripBlocks) beam_strip_kernel
   high = high_s[0];
 #pragma unroll
   for (int w = 1; w < WARPS; ++w) high = fmaxf(high, high_s[w]);
-  // (a power of two below what floats hold is below what counts, and an infinite r has made s NaN)
-  double sum = s == 0.f ? 0. : (double)(s * power2(r - (high == -INFINITY ? 0.f : high)));
+  // (a power of two below what floats hold is below what counts; an infinite r, of an infinite element, has made s NaN)
+  double sum = (double)(s * power2(r - high));
+  bool far = false;
+  if constexpr (!std::is_same_v<T, __half>) {        // (what fp16 holds is not far)
+    const unsigned most = __reduce_max_sync(0xffffffffu, (unsigned)(list_s[lane % WARPS][0] >> 32));         // 0: no element above -inf
+    far = most != 0 && !(fabsf(unordered(most)) <= kBeamFar);
+    if (far) {                                       // +inf: NaN, as it has to be
+      high = unordered(most);
+      sum = beam_far_sum<T>(p, high);
+    }
+  }
 #pragma unroll
   for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
   if (lane == 0) sum_s[warp] = sum;
@@ -349,7 +384,7 @@ __global__ void __launch_bounds__(kStripThreads, kStripBlocks) beam_strip_kernel
   for (int i = taken_all + tid; i < best; i += kStripThreads) out[i] = 0;
   if (tid == 0) {
     for (int w = 1; w < WARPS; ++w) sum += sum_s[w];
-    p.sums[blockIdx.x] = {sum, high};
+    p.sums[blockIdx.x] = {sum, high, far};
   }
 }
 
@@ -358,13 +393,30 @@ constexpr int kJoinFew = 512;        // candidates that are compared with each o
 
 __host__ __device__ constexpr int join_smem(int beams, int strips, int best) { return 16 * beams * best + 16 * beams * strips; }
 
+// A row some strip of which is far: its sum beside the largest reference, which is taken off the logits before anything is added to them:
+// it may be so large that nothing added to it is seen.
+__device__ __noinline__ void beam_far_join(const BeamSum* sums, int strips, float score, double& base, double& from) {
+  auto ref = [](const BeamSum& part) { return part.far ? (double)part.r : (double)part.r * (1. / (double)kLog2e); };
+  double top = -INFINITY, sum = 0.;
+  int far = 0;
+  for (int s = 0; s < strips; ++s) {
+    far |= sums[s].far;
+    if (sums[s].s != 0.) top = fmax(top, ref(sums[s]));              // (strips without elements have a reference too)
+  }
+  if (!far) return;
+  for (int s = 0; s < strips; ++s)
+    if (sums[s].s != 0.) sum += sums[s].s * exp(ref(sums[s]) - top);
+  base = (double)score - log(sum);
+  from = top;
+}
+
 // One group to a block: first the strips of every row, a row to a warp, which takes the lists' places from the first on until none
 // comes before its list's last; then the rows, a candidate's place being how many of the others are before it.  Bound by its chain
 // of steps: what a step needs from memory is fetched a step ahead, and only candidates that some `best` are not known to
 // beat look for their place.  4.3 us for 4 rows in one strip.
 __global__ void __launch_bounds__(kJoinThreads) beam_join_kernel(const __grid_constant__ BeamParams p) {
   extern __shared__ __align__(16) uint64_t join_keys[];
-  __shared__ double base_s[kBeamMost];               // what is added to a logit
+  __shared__ double base_s[kBeamMost], from_s[kBeamMost];        // what is added to a logit, and what is taken off before
   __shared__ int taken_s, left_s, few_s[kJoinFew], reach_s[kBeamMost];
   const int tid = threadIdx.x, best = p.best, beams = p.beams, strips = p.strips;
   const int64_t group = blockIdx.x, row0 = group * beams;
@@ -377,7 +429,11 @@ __global__ void __launch_bounds__(kJoinThreads) beam_join_kernel(const __grid_co
   const float score = tid < beams ? p.score[row0 + tid] : 0.f;
   const bool ended = tid < beams && p.ended && p.ended[row0 + tid];
   pdl_wait();
-  for (int i = tid; i < beams * strips; i += kJoinThreads) sums[i] = p.sums[row0 * strips + i];
+  int far = 0;                                       // (of rows that have ended, too: whatever was there)
+  for (int i = tid; i < beams * strips; i += kJoinThreads) {
+    sums[i] = p.sums[row0 * strips + i];
+    far |= sums[i].far;
+  }
   if (strips == 1) {
     for (int i = tid; i < beams * best; i += kJoinThreads) rows[i] = p.lists[row0 * best + i];
   } else {
@@ -397,27 +453,32 @@ __global__ void __launch_bounds__(kJoinThreads) beam_join_kernel(const __grid_co
       if (lane + 32 < best) rows[b * best + 32 + lane] = list.z;
     }
   }
-  __syncthreads();
+  far = __syncthreads_or(far);
   // 64-bit arithmetic is slow here: one logarithm for all rows
   if (tid < beams) {
     if (ended) {
       for (int i = 0; i < best; ++i) rows[tid * best + i] = i == 0 ? beam_key(0.f, (uint32_t)p.end) : 0;
       base_s[tid] = (double)score;
+      from_s[tid] = 0.;
     } else {
       float top = -INFINITY;
       for (int s = 0; s < strips; ++s) top = fmaxf(top, sums[tid * strips + s].r);
       double sum = 0.;
       for (int s = 0; s < strips; ++s) {
         const BeamSum part = sums[tid * strips + s];
-        if (part.s != 0.) sum += part.s * (double)power2(part.r - (top == -INFINITY ? 0.f : top));
+        if (part.s != 0.) sum += part.s * (double)power2(part.r - top);
       }
       base_s[tid] = (double)score - ((double)top + log2(sum)) * (1. / (double)kLog2e);
+      from_s[tid] = 0.;
+      if (far) beam_far_join(sums + tid * strips, strips, score, base_s[tid], from_s[tid]);
     }
   }
   __syncthreads();
   for (int i = tid; i < beams * best; i += kJoinThreads) {
     const uint64_t k = rows[i];
-    const double v = k ? base_s[i / best] + (double)unordered((uint32_t)(k >> 32)) : -INFINITY;
+    double x = (double)unordered((uint32_t)(k >> 32));
+    if (far) x -= from_s[i / best];
+    const double v = k ? base_s[i / best] + x : -INFINITY;
     const uint64_t u = (uint64_t)__double_as_longlong(v + 0.);
     values[i] = !(v > -INFINITY) ? 0 : u >> 63 ? ~u : u | 1ull << 63;        // 0: none, or NaN
   }
