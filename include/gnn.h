@@ -649,8 +649,8 @@ int gnn_beam_select(const gnn_beam_call* call, gnn_stream_t stream);
  * pages become the parent's (such pages are shared from then on: append writes none of them), and the rows of the
  * page that the parent has begun are copied into the slot's own page of the same number.  So every slot has, from its first page
  * that is not full on, pages of its own.  kv_len is not written: the slots of a group have the same (a group whose
- * slots have not is INDEX_RANGE, in the first cache's status, and is left as it is, and so is one where such a slot's own
- * page is outside the pages).
+ * slots have not, or whose length is outside the table's, is INDEX_RANGE, in the first cache's status, whether any of its slots
+ * moves or not, and is left as it is; so is one with slots that move where a slot's own page is outside the pages).
  * Types: any gnn_dtype.
  */
 typedef struct gnn_beam_state {

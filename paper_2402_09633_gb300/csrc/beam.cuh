@@ -664,6 +664,11 @@ __global__ void __launch_bounds__(kMoveThreads) beam_move_kernel(const __grid_co
   }
   __syncthreads();
   const uint64_t need = need_s, get = get_s;
+  const int len = paged ? len_s : 0, full = len >> p.shift, part = len & ((1 << p.shift) - 1);
+  if (paged && (uneven_s || len < 0 || full > p.table_width || (full == p.table_width && part > 0))) {
+    if (tid == 0) atomicOr(p.err, DEV_ERR_INDEX_RANGE);            // whether anything moves or not
+    return;
+  }
   if (get == 0) return;
   const int64_t c0 = (int64_t)segment * kMoveThreads + tid, step = (int64_t)p.segments * kMoveThreads;
   if (!paged) {
@@ -680,11 +685,6 @@ __global__ void __launch_bounds__(kMoveThreads) beam_move_kernel(const __grid_co
     if (s.width == 16) go(std::integral_constant<int, 16>());
     else if (s.width == 4) go(std::integral_constant<int, 4>());
     else go(std::integral_constant<int, 1>());
-    return;
-  }
-  const int len = len_s, full = len >> p.shift, part = len & ((1 << p.shift) - 1);
-  if (uneven_s || len < 0 || full > p.table_width || (full == p.table_width && part > 0)) {
-    if (tid == 0) atomicOr(p.err, DEV_ERR_INDEX_RANGE);
     return;
   }
   if (part > 0 && tid < p.beams) {                   // the open page of each slot; nothing writes its entry
