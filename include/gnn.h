@@ -642,7 +642,7 @@ int gnn_beam_select(const gnn_beam_call* call, gnn_stream_t stream);
  *                    row_bytes); out: the same out_stride bytes apart, or data itself (same strides): in place.  Arrays
  *                    do not overlap otherwise
  *   beams            1..64;  n_groups at most 2^26
- * Enqueued on `stream`; no workspace.  Errors: INVALID_ARG, CUDA.
+ * Enqueued on `stream`; no workspace.  With n_groups == 0 the arguments are checked and nothing is done.  Errors: INVALID_ARG, CUDA.
  *
  * gnn_paged_reorder -- the same for caches in pages, whose sequences are the hypotheses: n_caches caches (of a model's
  * layers) that share one table and kv_len, n_seqs = n_groups * beams.  In place: a slot's entries for its parent's full

@@ -253,23 +253,26 @@ def beam_reorder(parents, beams: int, states=(), out=None, caches=(), stream=Non
     """States of hypotheses moved to those that continue them: row i of a group of `beams` rows of each tensor of `states`
     [rows, ...] gets what row parents[i] of the group held (parents: cuda int32 [rows]), in place or, with `out`, in
     tensors like them.  caches: PagedCaches with one table and kv_len, whose sequences are the rows, always in place: full pages
-    are shared with the parent, the rows of the page that it has begun are copied (see gnn_paged_reorder).  Returns the states'
-    new tensors."""
+    are shared with the parent, the rows of the page that it has begun are copied (see gnn_paged_reorder).  Where a state or a
+    cache is refused, nothing moves.  Returns the states' new tensors."""
     lib = _library()
     device, rows = parents.get_device(), parents.numel()
     assert device >= 0 and device == Q._current_device(), "a cuda tensor of the current device"
     assert beams >= 1 and rows % beams == 0, "rows are whole groups of beams"
     at, st = Q._vector(parents, rows, Q._torch.int32, device), Q._stream(stream, device)
-    new = list(states if out is None else out)
+    states, caches = list(states), list(caches)
+    new = states if out is None else list(out)
     assert len(new) == len(states), "as many outputs as states"
     moves = b"".join([_state(x, y, rows, device) for x, y in zip(states, new)])
     for c in caches:
         assert c.device == device and c.table.shape[0] == rows, "caches of as many sequences, on the same device"
     if rows == 0:
         return new
+    if caches:                                               # nothing moves unless both calls are taken: the states' as one of no groups first
+        if states:
+            _check(lib.gnn_beam_reorder(at, 0, beams, moves, len(new), st), "gnn_beam_reorder")
+        _check(lib.gnn_paged_reorder(b"".join([c.pages for c in caches]), len(caches), at, rows // beams, beams, st),
+               "gnn_paged_reorder")
     if states:
         _check(lib.gnn_beam_reorder(at, rows // beams, beams, moves, len(new), st), "gnn_beam_reorder")
-    if caches:
-        _check(lib.gnn_paged_reorder(b"".join(c.pages for c in caches), len(caches), at, rows // beams, beams, st),
-               "gnn_paged_reorder")
     return new
