@@ -640,12 +640,13 @@ int gnn_beam_select(const gnn_beam_call* call, gnn_stream_t stream);
  *                    outside that keeps its own
  *   states           host array; data has n_groups * beams rows of row_bytes bytes, `stride` bytes apart (stride >=
  *                    row_bytes); out: the same out_stride bytes apart, or data itself (same strides): in place.  Arrays
- *                    do not overlap otherwise
+ *                    do not overlap otherwise; two states with one out are refused
  *   beams            1..64;  n_groups at most 2^26
  * Enqueued on `stream`; no workspace.  With n_groups == 0 the arguments are checked and nothing is done.  Errors: INVALID_ARG, CUDA.
  *
  * gnn_paged_reorder -- the same for caches in pages, whose sequences are the hypotheses: n_caches caches (of a model's
- * layers) that share one table and kv_len, n_seqs = n_groups * beams.  In place: a slot's entries for its parent's full
+ * layers) that share one table and kv_len, n_seqs = n_groups * beams.  Views of keys or values that are the same (data, type, sizes and
+ * strides) are moved once; such that have only the same data are refused, and views do not overlap otherwise.  In place: a slot's entries for its parent's full
  * pages become the parent's (such pages are shared from then on: append writes none of them), and the rows of the
  * page that the parent has begun are copied into the slot's own page of the same number.  So every slot has, from its first page
  * that is not full on, pages of its own.  kv_len is not written: the slots of a group have the same (a group whose

@@ -169,6 +169,21 @@ uint64_t beam_bytes(const gnn_beam_call* c) {
   return strips * (sizeof(BeamSum) + 8 * (uint64_t)c->best);
 }
 
+// Keys (even i) or values of the caches that move together.  Layers may have one cache, and a cache one pool of keys and values: such are
+// moved once.
+const gnn_heads& pool_of(const gnn_pages* caches, int i) { return i % 2 ? caches[i / 2].v : caches[i / 2].k; }
+int pool_before(const gnn_pages* caches, int i) {
+  for (int j = 0; j < i; ++j)
+    if (pool_of(caches, j).data == pool_of(caches, i).data) return j;
+  return -1;
+}
+bool same_pool(const gnn_pages* caches, int i, int j) {
+  const gnn_pages &a = caches[i / 2], &b = caches[j / 2];
+  const gnn_heads &x = pool_of(caches, i), &y = pool_of(caches, j);
+  return a.dtype == b.dtype && a.head_dim == b.head_dim && x.n_heads == y.n_heads && x.row_stride == y.row_stride &&
+         (x.n_heads == 1 || x.head_stride == y.head_stride);
+}
+
 int width_of(uintptr_t bits) { return bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 1; }
 
 // Launches over `what` states or pools of columns of at most `columns` each.
@@ -350,6 +365,8 @@ int gnn_beam_reorder(const int32_t* parents, int64_t n_groups, int32_t beams, co
         (s.out == s.data && s.out_stride != s.stride))
       return GNN_ERR_INVALID_ARG;
     if (n_groups > 0 && s.row_bytes > 0 && (!s.data || !s.out)) return GNN_ERR_INVALID_ARG;
+    for (int j = 0; j < i && s.row_bytes > 0; ++j)
+      if (states[j].row_bytes > 0 && states[j].out == s.out) return GNN_ERR_INVALID_ARG;     // moved twice at once
   }
   if (n_groups == 0) return GNN_OK;
   if (!parents) return GNN_ERR_INVALID_ARG;
@@ -386,6 +403,10 @@ int gnn_paged_reorder(const gnn_pages* caches, int32_t n_caches, const int32_t* 
         x.table_stride != c.table_stride || x.table_width != c.table_width || x.n_pages != c.n_pages)
       return GNN_ERR_INVALID_ARG;
   }
+  for (int i = 1; i < 2 * n_caches; ++i) {
+    const int j = pool_before(caches, i);
+    if (j >= 0 && !same_pool(caches, i, j)) return GNN_ERR_INVALID_ARG;
+  }
   if (n_groups == 0) return GNN_OK;
   if (!parents) return GNN_ERR_INVALID_ARG;
   MoveParams p = {};
@@ -403,8 +424,9 @@ int gnn_paged_reorder(const gnn_pages* caches, int32_t n_caches, const int32_t* 
     int64_t columns = 1;
     p.pools = 0;
     for (; i < 2 * n_caches && p.pools < kMoveStates; ++i) {
+      if (pool_before(caches, i) >= 0) continue;
       const gnn_pages& x = caches[i / 2];
-      const HeadsView v = view(i % 2 ? x.v : x.k, x.dtype);
+      const HeadsView v = view(pool_of(caches, i), x.dtype);
       const int bytes = x.head_dim * elem_bytes(x.dtype);
       const int w = width_of((uintptr_t)v.data | (uintptr_t)v.row_bytes | (uintptr_t)v.head_bytes | (uintptr_t)bytes);
       if (p.pools > 0 && bytes != p.dim_bytes) break;

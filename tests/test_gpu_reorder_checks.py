@@ -72,3 +72,27 @@ def test_nothing_moves_where_a_state_is_refused():
     beam_reorder(parents, 2, states, caches=caches)          # and with what is right it goes through
     assert states[0].tolist() == [1.0, 0.0] and wide[0, :4].tolist() == [10.0, 11.0, 12.0, 13.0]
     assert all(torch.equal(d[16:17].cpu(), p[48:49]) for d, p in zip(dev, pools))
+
+
+def test_a_cache_that_two_layers_have_is_moved_once():
+    """Every slot's begun page changes places with another's: moved twice, it would be where it was."""
+    from paper_2402_09633_gb300 import PagedCache, beam_reorder
+    page, n = 64, 32
+    table, pages = _table(n, 2, seed=3)
+    k, v, more = (_rand(pages * page, 2, 64, dtype=F32, seed=s) for s in (1, 2, 3))
+    parents = [i ^ 1 for i in range(n)]
+    want = []
+    for x in (k, v, more):
+        y = x.clone()
+        for i in range(n):
+            a, b = int(table[i, 1]) * page, int(table[parents[i], 1]) * page
+            y[a:a + 50] = x[b:b + 50]
+        want.append(y)
+    new = table.clone()
+    new[:, 0] = table[parents, 0]
+    dk, dv, dm = k.cuda(), v.cuda(), more.cuda()
+    on, length = table.cuda(), _i32([page + 50] * n)
+    both, tied = PagedCache(dk, dv, on, length, page), PagedCache(dm, dm, on, length, page)
+    beam_reorder(_i32(parents), n, caches=[both, tied] + [both] * 20)
+    assert both.status() == 0 and torch.equal(on.cpu(), new)
+    assert all(torch.equal(x.cpu(), y) for x, y in zip((dk, dv, dm), want))
