@@ -504,9 +504,9 @@ void gnn_attention_destroy(gnn_attention* att);
  *                 read.  Sequences may have pages in common
  *   kv_len        device int32 [n_seqs]: each sequence's positions, those of new rows among them
  *   status        device uint32, zero before the first call: where calls report what they find
- * Entries outside [0, n_pages), lengths outside the table's and offsets outside the views that a call is given are
- * reported as INDEX_RANGE; no such row is read or written, and the results of the sequences that they belong to are
- * undefined.  A cache is these arrays and nothing else: there is no handle, and calls on several streams may use one at once.
+ * Entries outside [0, n_pages), lengths below zero or past the table's, and offsets that fall or lie outside the views that a call
+ * is given are reported as INDEX_RANGE, of whichever sequence; no such row is read or written, and the results of the sequences
+ * that they belong to are undefined.  A cache is these arrays and nothing else: there is no handle, and calls on several streams may use one at once.
  *
  * gnn_paged_status -- read a status word behind the work of `stream` so far, clear it, and return what it said: GNN_OK,
  * GNN_ERR_INDEX_RANGE, GNN_ERR_DEVICE_TIMEOUT or GNN_ERR_CUDA.  Waits for `stream`.  Errors: INVALID_ARG (NULL, misaligned).
@@ -537,8 +537,8 @@ int gnn_paged_status(uint32_t* status, gnn_stream_t stream);
  *   positions        device, of the rotation, int32 [n_rows] or, with positions_float != 0, float32 [n_rows]; NULL: those in
  *                    the sequences
  *   q_start          device int32 [n_seqs + 1], not decreasing; rows before the first and from the last on are skipped
- * A row whose position is below zero (a sequence with fewer positions than rows) is not written.  No place may be that of
- * two rows.  Types, head_dim and limits as for gnn_rope.  Enqueued on `stream`; n_rows == 0 or n_seqs == 0 is a no-op.
+ * The key and value of a row whose position is below zero (a sequence with fewer positions than rows) are not written; its query
+ * is, to q_out.  No place may be that of two rows.  Types, head_dim and limits as for gnn_rope.  Enqueued on `stream`; n_rows == 0 or n_seqs == 0 is a no-op.
  * Errors: INVALID_ARG, CUDA.
  */
 typedef struct gnn_append_call {

@@ -63,7 +63,6 @@ __device__ __forceinline__ PagedPlace paged_place(const PagedRows& g, int64_t ro
   PagedPlace at = {sequence_of(g.q_start, g.n_seqs, rows, t), 0, -1};
   if (at.seq < 0) return at;
   const int end = g.q_start[at.seq + 1];
-  if (end > rows) atomicOr(g.err, DEV_ERR_INDEX_RANGE);
   at.pos = (int)((int64_t)g.kv_len[at.seq] - min((int64_t)end, rows) + t);
   if (at.pos < 0) return at;                           // a sequence shorter than its rows: what has no position
   const int entry = at.pos >> g.shift;
@@ -124,9 +123,22 @@ __device__ __forceinline__ float turns_whole(int x, uint64_t fixed) {
   return (float)(int)((fixed * (uint64_t)(int64_t)x + 0x80000000u) >> 32) * 0x1p-32f;
 }
 
+// Reports every sequence whose rows lie outside the array or fall, or whose length its row of the table cannot have: by the blocks that copy
+// values, which have the least to do, behind their rows.  Apart from the kernel, whose registers it need not have.
+template <typename T>
+__device__ __noinline__ void paged_report(const RotaryParams& p) {
+  if (blockIdx.x < p.block0[2]) return;
+  const PagedRows& g = p.pages;
+  const unsigned step = (p.block0[3] - p.block0[2]) * kRotThreads;
+  for (unsigned b = (blockIdx.x - p.block0[2]) * kRotThreads + threadIdx.x; b < (unsigned)g.n_seqs; b += step) {
+    const int a = g.q_start[b], z = g.q_start[b + 1], len = g.kv_len[b];
+    if (a < 0 || z < a || z > p.tokens || len < 0 || len > (int64_t)g.width << g.shift) atomicOr(g.err, DEV_ERR_INDEX_RANGE);
+  }
+}
+
 // PAGED: rows are those of sequences, and keys and values go to their places in pages; without positions of their own
 // the rows' are those in their sequences.  Four dependent loads lie before a key's store (a sequence's start, length, page, the row):
-// 256 rows of 256 sequences 4.2 us.  30,011 rows of seven, 6 + 2 + 2 heads of 96 in fp16, 40 rotated in pairs: 33 us, 3.5 TB/s, bound by
+// 256 rows of 256 sequences 4.3 us.  30,011 rows of seven, 6 + 2 + 2 heads of 96 in fp16, 40 rotated in pairs: 33 us, 3.5 TB/s, bound by
 // instructions (issue 71 %); four heads to a task instead of two, and accesses of 16 bytes for pairs, were slower.
 //
 // V pairs to a unit.  V == 1 takes any even R and any alignment that elements have; larger V need R and D to
@@ -324,6 +336,7 @@ __global__ void __launch_bounds__(kRotThreads, V >= 8 ? 4 : 5) rotary_kernel(con
         }
       }
   }
+  if constexpr (PAGED) paged_report<T>(p);
 }
 
 }  // namespace gnn
