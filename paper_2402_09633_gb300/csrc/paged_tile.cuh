@@ -39,7 +39,7 @@ struct PagedGrid {
   int64_t* chunks;                   // weights of kAttendThreads groups each, then of as many sequences; null where there are few of both
   int2 *first_a, *first_b;           // [ordinal]: the first thread block of an item, and how many have a part
   float *out_a, *out_b;              // [ordinal + thread block][2 places][rows][dim]
-  float2 *sum_a, *sum_b;             // the same, [rows]: scaled maximum and sum
+  float2 *sum_a, *sum_b;             // the same, [rows]: scaled maximum and sum (with a minus: some output is not finite)
 };
 
 // What a group has to do over its shared keys, or a pack over its own: `twos` items of two tiles and `ones` of one for each key
@@ -864,26 +864,35 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
       if (!ok) break;
       const bool some = blocks > 0 && row < rows && m > -INFINITY;   // NaN too: a sum of it is, with the maximum of what is not
       const bool odd = blocks > 0 && row < rows && l != 0.f;
+      // Whether the row sees keys of the part at all: then its outputs are there, though they may weigh nothing, and a sum below zero
+      // says that not all of them are finite, which the join has to know whatever they weigh.
+      const bool sees = blocks > 0 && lo < limit && limit > first * kKeys && lo < (first + (both ? blocks : 2 * blocks - 1)) * kKeys;
+      float2 spoilt = make_float2(0.f, 0.f);         // stays zero, or becomes NaN
       if (blocks > 0) {
         ok = wait(&b.pv_done[wg], n - 1);
         if (!ok) break;
         tc_fence_after();
-        if (__any_sync(0xffffffffu, some || odd)) {
+        if (__any_sync(0xffffffffu, sees)) {
 #pragma unroll 1
           for (int c = 0; c < DP; c += 32) {
             float o[32];
             tmem_ld_32x32(to + c, o);
             tmem_wait_ld_32(o);
-            if (some || odd) {
+            if (sees) {
 #pragma unroll
               for (int e = 0; e < 32; e += 8)
-                if (c + e < p.dim) st_global_32b(out + c + e, reinterpret_cast<const uint32_t*>(o + e));
+                if (c + e < p.dim) {
+                  st_global_32b(out + c + e, reinterpret_cast<const uint32_t*>(o + e));
+#pragma unroll
+                  for (int x = 0; x < 8; x += 2) spoilt = __ffma2_rn(make_float2(o[e + x], o[e + x + 1]), make_float2(0.f, 0.f), spoilt);
+                }
             }
           }
         }
         tc_fence_before();
       }
-      if (row < rows) *sum_at = some || odd ? make_float2(some ? m * scale : 0.f, l) : make_float2(-INFINITY, 0.f);
+      if (row < rows)
+        *sum_at = make_float2(some ? m * scale : odd ? 0.f : -INFINITY, spoilt.x + spoilt.y == 0.f ? l : -l);
     }
   }
   tc_fence_before();
@@ -1008,14 +1017,16 @@ __global__ void __launch_bounds__(32 * (SPLIT > 1 ? SPLIT : kPagedJoinWarps), BL
   bool odd = false;                                  // something of its own keys' part is not finite
   for (int k0 = 0; k0 < na + nb; k0 += 32) {
     float z = 0.f;
+    bool spoilt = false;
     if (k0 + lane < na + nb) {
       const float2 s = k0 == 0 ? mine : sums(k0 + lane);
       z = s.x == -INFINITY ? 0.f : exp2f(s.x - ref);
-      l = fmaf(s.y, z, l);
-      odd = odd || (k0 + lane >= na && !(fabsf(s.y) < INFINITY));
+      l = fmaf(fabsf(s.y), z, l);
+      spoilt = __float_as_int(s.y) < 0;              // a minus: its outputs are not all finite
+      odd = odd || (k0 + lane >= na && (spoilt || !(fabsf(s.y) < INFINITY)));
     }
-    // those that count, some at a time with their loads together
-    uint32_t left = __ballot_sync(0xffffffffu, z != 0.f);
+    // those that count, some at a time with their loads together; outputs that are not finite count even where they weigh nothing
+    uint32_t left = __ballot_sync(0xffffffffu, z != 0.f || spoilt);
     if (SPLIT > 1) left &= (0xffffffffu / ((1u << SPLIT) - 1)) << sub;             // every SPLIT-th
     while (left) {
       float4 x[PARTS];
@@ -1028,7 +1039,7 @@ __global__ void __launch_bounds__(32 * (SPLIT > 1 ? SPLIT : kPagedJoinWarps), BL
         if (left == 0) f[e] = 0.f;
         own[e] = k0 + k >= na;
         x[e] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (have && f[e] != 0.f)
+        if (have && left != 0)
           x[e] = __ldcs(reinterpret_cast<const float4*>(own[e] ? ob + (k0 + k - na) * step_b * p.dim : oa + (k0 + k) * step_a * p.dim) + lane);
         left &= left - 1;
       }
