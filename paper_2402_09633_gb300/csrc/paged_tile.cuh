@@ -734,6 +734,9 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
     const uint32_t ts = tmem + lanes + kKeys * wg, tp = tmem + lanes + S::kP + S::kPStep * wg, to = tmem + lanes + S::kO + DP * wg;
     const float scale = fabsf(p.scale_log2);
     const float slack = 8.f / scale;                 // scores may outgrow the running maximum by 2^8
+    // Weights in fp16 are taken up by 2^7, to 2^15 at most, which the sum has too, so that those down to 2^-31 of the largest are still
+    // held (a weight of 2^-26 to within 2^-6 of itself) and many faint keys count in the product as they do in the sum.
+    constexpr float kUp = std::is_same_v<T, __half> ? 7.f : 0.f;
     uint32_t n = 0, items = 0;                       // blocks this tile has gone through
     bool ok = true;
     while (ok) {
@@ -849,7 +852,7 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
             for (int c = 0; c < DP; c += 8) tmem_scale_32x8(to + c, shrink);
           }
         }
-        const float off = m == -INFINITY ? 0.f : -m * scale;
+        const float off = m == -INFINITY ? kUp : fmaf(-m, scale, kUp);
         float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
         for (int c = 0; c < PARTS; ++c) {
