@@ -996,7 +996,11 @@ __global__ void __launch_bounds__(32 * (SPLIT > 1 ? SPLIT : kPagedJoinWarps), BL
   }
   {
     const int pack = seq / g.pack, q0 = g.pack > 1 ? pack0 : sq.q0, tile = g.pack > 1 ? 0 : i / g.tile_q, query = row - q0 - tile * g.tile_q;
-    if (query < 0 || query >= g.box_b) return;
+    if (query < 0) return;
+    if (query >= g.box_b) {                          // behind a sequence of the pack that has more queries than announced
+      if (sub == 0) slowly();
+      return;
+    }
     row_b = query * g.group + head % g.group;
     ordinal_b = (paged_ordinal_b(g, pack, q0) + tile) * p.kv_heads + kv;
   }
