@@ -77,7 +77,8 @@ PagedPlan paged_plan(const gnn_pages* c, const gnn_paged_call* a, int n_sm) {
   g.rows_b = g.box_b * g.group;
   const int64_t n_a = a->n_groups > 0 ? (n / (2 * g.tile_q) + a->n_groups) * c->k.n_heads : 0;
   const int64_t n_b = (g.pack > 1 ? (c->n_seqs + g.pack - 1) / g.pack : n / g.tile_q + c->n_seqs) * (int64_t)c->k.n_heads;
-  const int64_t sums_a = n_a > 0 ? 2 * (n_a + r.blocks) * g.rows_a : 0, sums_b = 2 * (n_b + r.blocks) * g.rows_b;
+  const int64_t sums_a = n_a > 0 ? 2 * (n * a->q.n_heads + (int64_t)r.blocks * g.rows_a) : 0,
+                sums_b = 2 * (n * a->q.n_heads + (int64_t)r.blocks * g.rows_b);
   char* at = static_cast<char*>(a->workspace);
   auto take = [&](int64_t bytes) {
     char* here = at;

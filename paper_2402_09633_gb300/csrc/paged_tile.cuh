@@ -35,11 +35,11 @@ struct PagedGrid {
   int box;                           // rows of a load of shared keys: of a page, at most a block's
   int group;                         // query heads to a key head
   int pack;                          // sequences of a pack, a power of two; 1: a sequence may have several tiles
-  int rows_a, rows_b;                // rows of a place
+  int rows_a, rows_b;                // the most rows of a tile
   int64_t* chunks;                   // weights of kAttendThreads groups each, then of as many sequences; null where there are few of both
   int2 *first_a, *first_b;           // [ordinal]: the first thread block of an item, and how many have a part
-  float *out_a, *out_b;              // [ordinal + thread block][2 places][rows][dim]
-  float2 *sum_a, *sum_b;             // the same, [rows]: scaled maximum and sum (with a minus: some output is not finite)
+  float *out_a, *out_b;              // outputs of parts, [rows][dim]: see paged_places
+  float2 *sum_a, *sum_b;             // [rows]: scaled maximum and sum (with a minus: some output is not finite)
 };
 
 // What a group has to do over its shared keys, or a pack over its own: `twos` items of two tiles and `ones` of one for each key
@@ -73,7 +73,7 @@ __device__ __forceinline__ PagedOwn paged_own(const PagedParams& p, int b, bool*
   const int base = s.shared / kPiece * kPiece;
   // queries below the shared length are left to the join, row by row
   const int pieces = s.nq == 0 || s.len - s.nq < s.shared ? 0 : (s.len - base + kPiece - 1) / kPiece;
-  return {s.q0, min(s.nq, p.max_q), base, s.shared, s.len, pieces};
+  return {s.q0, s.nq, base, s.shared, s.len, pieces};
 }
 
 // A pack's work, on every one of its lanes (a lane to a sequence, `pack` lanes side by side); prefix: pieces of those before.
@@ -120,6 +120,14 @@ __device__ __forceinline__ int64_t paged_ordinal_a(const PagedGrid& g, int group
 __device__ __forceinline__ int64_t paged_ordinal_b(const PagedGrid& g, int pack, int q0) {
   return g.pack > 1 ? (int64_t)pack : (int64_t)(q0 / g.tile_q) + pack;
 }
+// Where a part of an item leaves its outputs: tile t's (or of one tile, those of its blocks on tile t of tensor memory) row r in row
+// first + thread block * 2 * (the most rows of a tile) + 2 r + t.  Items have room for twice their own rows, behind those of all items
+// before them in the list: a thread block's parts follow its earlier ones, and an item's parts lie a whole part apart.  So all
+// that is needed is two places for each row and head, and two to a thread block, whatever number of sequences or groups the rows are of.
+// row0, have: the item's first query, and how many there are from it on in the group, pack or sequence.
+__device__ __forceinline__ int64_t paged_places(const PagedParams& p, const PagedGrid& g, bool own, int row0, int have, int head) {
+  return (int64_t)row0 * (2 * p.heads) + head * min(have, own ? g.box_b : 2 * g.tile_q) * (2 * g.group);
+}
 // Divisions of what is not negative, in 32 bits where that does: 64 bits take a warp with few registers thousands of cycles.
 __device__ __forceinline__ int64_t paged_divide(int64_t a, int64_t b) {
   return (a | b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
@@ -135,8 +143,8 @@ struct PagedItem {
   int rows[2];                       // of each tile
   int query[2];                      // each tile's first
   int segments, step;
-  float* out[2];
-  float2* sum[2];
+  float* out;
+  float2* sum;
   PagedSegment seg[kPackMost];
 };
 
@@ -476,9 +484,8 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
           PagedItem& to = b.item[slot];
           to.n = it.n; to.first = it.first; to.whole = it.whole; to.both = it.both; to.start = it.start; to.segments = it.segments; to.step = it.step;
 #pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            to.rows[t] = it.rows[t]; to.query[t] = it.query[t]; to.out[t] = it.out[t]; to.sum[t] = it.sum[t];
-          }
+          for (int t = 0; t < 2; ++t) to.rows[t] = it.rows[t], to.query[t] = it.query[t];
+          to.out = it.out; to.sum = it.sum;
         }
         if (lane < it.segments) b.item[slot].seg[lane] = segment;
         __syncwarp();
@@ -510,13 +517,9 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
           segment = {mine.q0 - w.q0, mine.pieces ? key0 + mine.shared : INT_MAX, mine.pieces ? key0 + mine.len - mine.nq + 1 : 0};
         }
         const int64_t ordinal = ((own ? paged_ordinal_b(g, index, w.q0) : paged_ordinal_a(g, index, w.q0)) + e) * p.kv_heads + head;
-        const int64_t place = 2 * (ordinal + blockIdx.x);
-        const int place_rows = own ? g.rows_b : g.rows_a;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          it.out[t] = (own ? g.out_b : g.out_a) + (place + t) * place_rows * p.dim;
-          it.sum[t] = (own ? g.sum_b : g.sum_a) + (place + t) * place_rows;
-        }
+        const int64_t place = paged_places(p, g, own, row0, have, head) + (int64_t)blockIdx.x * (2 * (own ? g.rows_b : g.rows_a));
+        it.out = (own ? g.out_b : g.out_a) + place * p.dim;
+        it.sum = (own ? g.sum_b : g.sum_a) + place;
         if (b0 == 0 && lane == 0 && kind == 0) {
           const int64_t last = u0 + w.blocks - 1;
           (own ? g.first_b : g.first_a)[ordinal] =
@@ -746,8 +749,8 @@ __global__ void __launch_bounds__(kAttendThreads, 1)
       const PagedItem& item = b.item[slot];
       const int all = item.n, both = item.both, rows = item.rows[wg];
       const int skip = both || item.start == wg ? 0 : 1, first = item.first + skip;
-      float* out = item.out[wg] + (int64_t)row * p.dim;
-      float2* sum_at = item.sum[wg] + row;
+      float* out = item.out + (2 * row + wg) * p.dim;
+      float2* sum_at = item.sum + 2 * row + wg;
       int lo = INT_MAX, limit = 0;                   // the keys that the row sees; none where the tile has no such row
       if (all > 0 && row < rows) {
         const int query = item.query[wg] + row_query;
@@ -929,7 +932,12 @@ __global__ void __launch_bounds__(32 * (SPLIT > 1 ? SPLIT : kPagedJoinWarps), BL
     pdl_wait();
     return;
   }
-  int s0 = p.q_start[seq], s1 = p.q_start[seq + 1], len = p.kv_len[seq], pack0 = p.q_start[seq / g.pack * g.pack];
+  // of the sequence's pack: its first row, and the one behind its last (a pack that is not full goes on to the array's end)
+  auto pack_end = [&] {
+    const int64_t end = ((int64_t)(seq / g.pack) + 1) * g.pack;
+    return end <= p.n_seqs ? p.q_start[end] : p.n_q_rows;
+  };
+  int s0 = p.q_start[seq], s1 = p.q_start[seq + 1], len = p.kv_len[seq], pack0 = p.q_start[seq / g.pack * g.pack], pack1 = pack_end();
   int g0 = 0, g1 = 0, shared = 0;
   if (group >= 0) {
     g0 = p.group_start[group];
@@ -946,6 +954,7 @@ __global__ void __launch_bounds__(32 * (SPLIT > 1 ? SPLIT : kPagedJoinWarps), BL
     s1 = p.q_start[seq + 1];
     len = p.kv_len[seq];
     pack0 = p.q_start[seq / g.pack * g.pack];
+    pack1 = pack_end();
   }
   if (group >= 0 && (seq < g0 || seq >= g1)) {
     group = sequence_of(p.group_start, p.n_groups, p.n_seqs, seq);
@@ -970,6 +979,7 @@ __global__ void __launch_bounds__(32 * (SPLIT > 1 ? SPLIT : kPagedJoinWarps), BL
   sq.first = group >= 0 ? max(g0, 0) : seq;
   sq.shared = group >= 0 ? min(max(shared, 0), paged_room(p)) : 0;
   pack0 = min(max(pack0, 0), p.n_q_rows);
+  pack1 = min(max(pack1, pack0), p.n_q_rows);
   const int i = row - sq.q0;
   pdl_wait();
   if (i >= p.max_q) return;
@@ -985,33 +995,37 @@ __global__ void __launch_bounds__(32 * (SPLIT > 1 ? SPLIT : kPagedJoinWarps), BL
   }
   // where the row's parts lie: of the shared keys, [0, na), and of its own, [na, na + nb)
   int64_t ordinal_a = 0, ordinal_b;
-  int row_a = 0, row_b, tile_a = 0, every = 1;       // every: shared parts of both places (1), or of one (2)
+  int64_t row_a = 0, row_b;
+  int every = 1;                                     // shared parts of both places (1), or of one (2)
   if (sq.shared > 0) {
     if (row < rows.x || row >= rows.x + rows.y) return;            // offsets that contradict each other
-    const int tile = (row - rows.x) / g.tile_q, tiles = (rows.y + g.tile_q - 1) / g.tile_q;
-    row_a = (row - rows.x - tile * g.tile_q) * g.group + head % g.group;
+    const int tile = (row - rows.x) / g.tile_q, tiles = (rows.y + g.tile_q - 1) / g.tile_q, before = tile / 2 * 2 * g.tile_q;
     every = (tile | 1) < tiles ? 2 : 1;
-    tile_a = tile & 1;
+    row_a = paged_places(p, g, false, rows.x + before, rows.y - before, kv) + 2 * ((row - rows.x - tile * g.tile_q) * g.group + head % g.group) + (every == 2 ? tile & 1 : 0);
     ordinal_a = (paged_ordinal_a(g, group, rows.x) + tile / 2) * p.kv_heads + kv;
   }
   {
     const int pack = seq / g.pack, q0 = g.pack > 1 ? pack0 : sq.q0, tile = g.pack > 1 ? 0 : i / g.tile_q, query = row - q0 - tile * g.tile_q;
-    if (query < 0) return;
+    const int have = (g.pack > 1 ? pack1 - pack0 : sq.nq) - tile * g.tile_q;
+    if (query < 0 || query >= have) return;          // offsets that contradict each other
     if (query >= g.box_b) {                          // behind a sequence of the pack that has more queries than announced
       if (sub == 0) slowly();
       return;
     }
-    row_b = query * g.group + head % g.group;
+    row_b = paged_places(p, g, true, q0 + tile * g.tile_q, have, kv) + 2 * (query * g.group + head % g.group);
     ordinal_b = (paged_ordinal_b(g, pack, q0) + tile) * p.kv_heads + kv;
   }
   const int2 fa = sq.shared > 0 ? g.first_a[ordinal_a] : make_int2(0, 0), fb = g.first_b[ordinal_b];
   const int first_a = min(max(fa.x, 0), blocks - 1), first_b = min(max(fb.x, 0), blocks - 1);
   const int na = min(max(fa.y, 0), blocks - first_a) * (2 / every), nb = min(max(fb.y, 0), blocks - first_b) * 2;
-  const int64_t place_a = 2 * (ordinal_a + first_a) + (every == 2 ? tile_a : 0), place_b = 2 * (ordinal_b + first_b);
-  const float2 *sa = g.sum_a + place_a * g.rows_a + row_a, *sb = g.sum_b + place_b * g.rows_b + row_b;
-  const float *oa = g.out_a + (place_a * g.rows_a + row_a) * p.dim, *ob = g.out_b + (place_b * g.rows_b + row_b) * p.dim;
-  const int64_t step_a = (int64_t)every * g.rows_a, step_b = g.rows_b;
-  auto sums = [&](int k) { return k < na ? sa[k * step_a] : sb[(k - na) * step_b]; };
+  const int step_a = 2 * g.rows_a, step_b = 2 * g.rows_b;          // from one thread block's part to the next's
+  row_a += first_a * step_a;
+  row_b += first_b * step_b;
+  const float2 *sa = g.sum_a + row_a, *sb = g.sum_b + row_b;
+  const float *oa = g.out_a + row_a * p.dim, *ob = g.out_b + row_b * p.dim;
+  auto at_a = [&](int k) { return every == 2 ? k * step_a : (k >> 1) * step_a + (k & 1); };
+  auto at_b = [&](int k) { return (k >> 1) * step_b + (k & 1); };
+  auto sums = [&](int k) { return k < na ? sa[at_a(k)] : sb[at_b(k - na)]; };
   const float2 mine = lane < na + nb ? sums(lane) : make_float2(-INFINITY, 0.f);           // the first parts, kept
   float top = mine.x;
   for (int k = lane + 32; k < na + nb; k += 32) top = fmaxf(top, sums(k).x);
@@ -1047,7 +1061,7 @@ __global__ void __launch_bounds__(32 * (SPLIT > 1 ? SPLIT : kPagedJoinWarps), BL
         own[e] = k0 + k >= na;
         x[e] = make_float4(0.f, 0.f, 0.f, 0.f);
         if (have && left != 0)
-          x[e] = __ldcs(reinterpret_cast<const float4*>(own[e] ? ob + (k0 + k - na) * step_b * p.dim : oa + (k0 + k) * step_a * p.dim) + lane);
+          x[e] = __ldcs(reinterpret_cast<const float4*>(own[e] ? ob + at_b(k0 + k - na) * p.dim : oa + at_a(k0 + k) * p.dim) + lane);
         left &= left - 1;
       }
 #pragma unroll
