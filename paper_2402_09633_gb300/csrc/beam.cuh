@@ -268,7 +268,7 @@ __global__ void __launch_bounds__(kStripThreads, kStripBlocks) beam_strip_kernel
     // Candidates: above the list's last (later elements of the same value lose the tie), and not below what the block's lists
     // hold together: all warps' elements at place best / 8 and before are `best` at least.  They are held back, and
     // put in the list kStripHeld or more at a time: a bound that is somewhat old lets through a few more, which costs less than a
-    // list that is always up to date (16 rows' groups of 300,000: 74.4 us with 8, 79.2 with 1, 75.8 with 32).
+    // list that is always up to date (16 rows' groups of 300,000: 67.1 us with 8, 75.2 with 1, 67.7 with 16, 69.4 with 32).
     auto key = [&](int i, bool in) {
       return in ? beam_key(high, (uint32_t)((c0 + i / VEC * 32 + lane) * VEC + i % VEC)) : 0;
     };

@@ -15,9 +15,10 @@
 // by 2^8 / scale.
 //
 // Measured (bf16, 16 query heads on 4 key heads of 128).  Bound by the tensor cores' operands and each tile's wait for its softmax:
-// 512 sequences that share 65,536 keys, 237 us, 1,160 TFLOP/s, tensor pipe 60 % busy; a block for two tiles is 1.75 us.  Bound by HBM:
-// 64 sequences of up to 8,192 keys of their own, 137 us, 5.9 TB/s.  Bound by its chain: 64 sequences that share 16,384 keys, 33 us,
-// of which 6 are the start, 6 the blocks and 11 the join.  Packs of one sequence instead of 32: 519 us for the first, 45 for the last.
+// 512 sequences that share 65,536 keys, 234 us, 1,175 TFLOP/s, tensor pipe 60 % busy; a block for two tiles is 1.75 us.  Bound by HBM:
+// 64 sequences of up to 8,192 keys of their own, 136 us, 5.9 TB/s.  Bound by its chain: 64 sequences that share 16,384 keys, 33 us,
+// of which 6 are the start, 6 the blocks and 11 the join.  Packs of one sequence (where the most queries are not known) instead of 32:
+// 262 us for the first, 36 for the last.
 #pragma once
 #include "attend_tile.cuh"
 #include "paged.cuh"
@@ -280,7 +281,7 @@ __device__ __forceinline__ PagedShare paged_share(const PagedParams& p, const Pa
 }
 
 // Where there are many groups or sequences: their weights, kAttendThreads to a block, so that not every block of the next kernel looks at
-// all of them.  (4,096 groups of four sequences: 1.69 ms without it.)
+// all of them.  (20,000 sequences: 277 us without it, 192 with it.)
 __global__ void __launch_bounds__(kAttendThreads) paged_weigh_kernel(const __grid_constant__ PagedParams p, const __grid_constant__ PagedGrid g) {
   __shared__ int64_t sum_s[kAttendThreads / 32];
   const int group_chunks = (p.n_groups + kAttendThreads - 1) / kAttendThreads, c = (int)blockIdx.x, tid = threadIdx.x;

@@ -167,7 +167,7 @@ class PagedCache:
         """Attention of q [rows, heads, dim]: row i of the nq rows q_start[b] .. q_start[b + 1] - 1 sees sequence b's keys up to
         its own position kv_len[b] - nq + i.  groups: cuda int32 [groups + 1], shared: cuda int32 [groups]: sequences
         groups[g] .. groups[g + 1] - 1 have their first shared[g] positions in common, which are read once, through the
-        first one's pages.  max_q: the most queries of a sequence, when known."""
+        first one's pages.  max_q: the most queries of a sequence, when known: short sequences are computed together only then."""
         device, dtype, dim = self.device, self.dtype, self.dim
         assert Q._current_device() == device, "the cache's device is not the current one"
         assert (groups is None) == (shared is None), "groups and shared go together"
